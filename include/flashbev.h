@@ -312,6 +312,162 @@ typedef struct flashbev_vt_multires_params {
 
 flashbev_status flashbev_sampling_vt_multires(const flashbev_vt_multires_params *p, void *stream);
 
+/* ---- the operators of a transformer layer around the cross-attention ------------------------
+ * flashbev_sca is the core of a BEV transformer layer.  The matrix products that make its value maps,
+ * offsets and attention logits, take its output back into the queries' rows and form the feed-forward
+ * part are `flashbev_linear`; what joins one block of the layer to the next is `flashbev_block_norm`.
+ * Rows may be cells, image texels or tokens; a stride of 0 stands for dense rows. */
+
+typedef enum flashbev_act {
+    FLASHBEV_ACT_NONE = 0,
+    FLASHBEV_ACT_RELU = 1, /* max(z, 0) */
+    FLASHBEV_ACT_GELU = 2, /* z Phi(z), Phi the standard normal distribution function (no tanh form) */
+    FLASHBEV_ACT_SILU = 3  /* z / (1 + exp(-z)) */
+} flashbev_act;
+
+/*
+ *     z = x weight^T + bias,     out = residual + act(z)
+ *
+ * Sums are fp32 in tensor memory, bias, activation and residual are applied to them unrounded, `out` and
+ * `preact_out` are rounded once.  bf16 products are exact; float32 operands are taken apart into three bf16
+ * pieces each and the six products above 2^-24 of the whole are summed (a finite operand beyond 3.38e38 and
+ * an infinite one give NaN there).  The result is reproducible bit for bit.
+ *
+ * Enqueues one kernel, or two where a long sum is shared by several thread blocks (see `workspace`).  rows = 0
+ * is allowed and enqueues nothing.  `out` and `preact_out` may not overlap any input, but `out` may be
+ * `residual` itself (same address and stride).  All pointers element-aligned, else FLASHBEV_MISALIGNED; 16-byte
+ * aligned addresses and strides of whole 16-byte vectors are the fast layout (TMA loads for bf16).  rows < 2^31
+ * and in_features, out_features <= 2^24, else FLASHBEV_UNSUPPORTED.
+ */
+typedef struct flashbev_linear_params {
+    size_t struct_size;        /* sizeof(flashbev_linear_params) of the caller's header */
+    const void *x;             /* device, [rows][in_features], element type dtype */
+    const void *weight;        /* device, [out_features][in_features], dtype */
+    const void *bias;          /* optional device, [out_features], dtype */
+    const void *residual;      /* optional device, [rows][out_features], out_dtype */
+    void *out;                 /* device, [rows][out_features], out_dtype */
+    void *preact_out;          /* optional device, [rows][out_features], dtype: z, which the backward of an activation needs */
+    int64_t rows;
+    int32_t in_features, out_features;
+    int64_t ld_x, ld_weight, ld_residual, ld_out, ld_preact; /* distance of rows in elements; 0: dense */
+    int32_t dtype, out_dtype;  /* flashbev_dtype */
+    int32_t act;               /* flashbev_act */
+    int32_t reserved;          /* 0 */
+    void *workspace;           /* optional DEVICE scratch, 16-byte aligned: with flashbev_linear_workspace_bytes(p) bytes calls of few
+                                  rows and long sums are shared by more thread blocks.  Calls that may overlap on the GPU (two
+                                  streams, two graphs) need scratch of their own */
+    size_t workspace_bytes;
+    uint32_t *error_word;      /* optional DEVICE word: counts thread blocks whose waits for their own loads or products did not end
+                                  within seconds (the block gives up instead of hanging; its results are not valid) */
+} flashbev_linear_params;
+
+flashbev_status flashbev_linear(const flashbev_linear_params *p, void *stream);
+size_t flashbev_linear_workspace_bytes(const flashbev_linear_params *p); /* 0 if nothing is gained, or `p` is invalid */
+
+/*
+ * Gradients of flashbev_linear:
+ *
+ *     dz = grad_out * act'(preact),   grad_x = dz weight,   grad_weight = dz^T x,   grad_bias = column sums of dz
+ *
+ * (the residual's gradient is grad_out itself).  For bf16 operands dz is rounded to bf16 before the products -- one rounding per
+ * element, as large as that of the gradients themselves; grad_bias sums it unrounded.  act'(0) = 0 for ReLU, and where that slope is
+ * 0, dz is 0 whatever grad_out holds.  Each gradient is optional; rows = 0 sets grad_weight and grad_bias to zero.  Reproducible bit
+ * for bit.  Enqueues up to five kernels.  Limits as for flashbev_linear; gradients may not overlap inputs or one another.
+ */
+typedef struct flashbev_linear_backward_params {
+    size_t struct_size;        /* sizeof(flashbev_linear_backward_params) of the caller's header */
+    const void *grad_out;      /* device, [rows][out_features], grad_dtype */
+    const void *x;             /* device, [rows][in_features], dtype; may be NULL without grad_weight */
+    const void *weight;        /* device, [out_features][in_features], dtype; may be NULL without grad_x */
+    const void *preact;        /* device, [rows][out_features], dtype: z of the forward call; NULL for FLASHBEV_ACT_NONE only */
+    void *grad_x;              /* optional device, [rows][in_features], dtype */
+    void *grad_weight;         /* optional device, [out_features][in_features], dtype */
+    void *grad_bias;           /* optional device, [out_features], dtype */
+    int64_t rows;
+    int32_t in_features, out_features;
+    int64_t ld_grad_out, ld_x, ld_weight, ld_preact, ld_grad_x, ld_grad_weight; /* distance of rows in elements; 0: dense */
+    int32_t dtype, grad_dtype; /* flashbev_dtype: of the operands and gradients; of grad_out (FLASHBEV_F32 where dtype is) */
+    int32_t act;               /* flashbev_act */
+    int32_t reserved;          /* 0 */
+    void *workspace;           /* DEVICE scratch, 16-byte aligned, flashbev_linear_backward_workspace_bytes(p) bytes, else
+                                  FLASHBEV_TOO_SMALL; NULL only where that is 0 */
+    size_t workspace_bytes;
+    uint32_t *error_word;      /* as in flashbev_linear_params */
+} flashbev_linear_backward_params;
+
+flashbev_status flashbev_linear_backward(const flashbev_linear_backward_params *p, void *stream);
+size_t flashbev_linear_backward_workspace_bytes(const flashbev_linear_backward_params *p);
+
+typedef enum flashbev_norm {
+    FLASHBEV_NORM_NONE = 0,
+    FLASHBEV_NORM_LAYER = 1, /* (v - mean) / sqrt(variance + eps) * weight + bias, variance over C (not C - 1) */
+    FLASHBEV_NORM_RMS = 2    /* v / sqrt(mean of v^2 + eps) * weight + bias */
+} flashbev_norm;
+
+/*
+ * What joins one residual block to the next, row by row:
+ *
+ *     h = x + scale * gate * after(y),     n = before(h)
+ *
+ * y is the block's output, x the rows that passed it by, `after` the norm behind the block (or none), `before` the norm ahead of
+ * the next block (or none).  gate has gate_groups rows of C, row g for the rows g * rows / gate_groups and up: 1 for a gate per
+ * channel, a batch's size for one per sample, `rows` for one per row.  Without y, h = x and only n is computed.  Statistics and h are
+ * fp32 and n is formed from the unrounded h; the mean is taken off before the squares are summed; h and n are rounded once.  One kernel;
+ * rows = 0 enqueues nothing.  h may be x and n may be y (same address and stride); no other overlap.  Pointers element-aligned,
+ * else FLASHBEV_MISALIGNED.  C <= FLASHBEV_NORM_MAX_CHANNELS and rows < 2^31, else FLASHBEV_UNSUPPORTED.
+ */
+#define FLASHBEV_NORM_MAX_CHANNELS 4096
+typedef struct flashbev_block_norm_params {
+    size_t struct_size;        /* sizeof(flashbev_block_norm_params) of the caller's header */
+    const void *x;             /* device, [rows][C], dtype */
+    const void *y;             /* optional device, [rows][C], branch_dtype */
+    const void *gate;          /* optional device, [gate_groups][C], param_dtype (needs y) */
+    const void *after_weight, *after_bias;   /* device, [C], param_dtype; each optional (1 and 0); `after` NONE: NULL */
+    const void *before_weight, *before_bias; /* device, [C], param_dtype; each optional; `before` NONE: NULL */
+    void *h;                   /* optional device, [rows][C], dtype (needs y) */
+    void *n;                   /* device, [rows][C], branch_dtype; NULL exactly if `before` is NONE */
+    int64_t rows, gate_groups; /* gate_groups divides rows (ignored without a gate) */
+    int32_t C;
+    int32_t after, before;     /* flashbev_norm */
+    int32_t dtype, branch_dtype, param_dtype; /* flashbev_dtype: of x and h; of y and n (bf16 beside a float32 dtype allowed, not
+                                  the reverse); of the parameters (FLASHBEV_F32, or branch_dtype) */
+    int64_t ld_x, ld_y, ld_h, ld_n; /* distance of rows in elements; 0: dense */
+    double scale, eps;         /* finite; eps >= 0 */
+} flashbev_block_norm_params;
+
+flashbev_status flashbev_block_norm(const flashbev_block_norm_params *p, void *stream);
+
+/*
+ * Gradients of flashbev_block_norm at the same inputs, from those at h and n.  Nothing is kept from the forward call: the statistics
+ * are taken again from x and y, which have to be read for the parameters' gradients anyway.  Enqueues one kernel, and a second one
+ * where gradients of parameters are wanted (they are sums over rows).  Reproducible bit for bit.  Gradients may not overlap inputs or
+ * one another, but grad_x may be grad_h and grad_y may be grad_n (same address and stride).  rows = 0 sets the parameters' gradients to zero.
+ */
+typedef struct flashbev_block_norm_backward_params {
+    size_t struct_size;        /* sizeof(flashbev_block_norm_backward_params) of the caller's header */
+    const void *grad_h;        /* optional device, [rows][C], dtype */
+    const void *grad_n;        /* device, [rows][C], branch_dtype; NULL exactly if `before` is NONE */
+    const void *x, *y, *gate;  /* as in the forward call */
+    const void *after_weight, *after_bias, *before_weight;
+    void *grad_x;              /* optional device, [rows][C], dtype */
+    void *grad_y;              /* optional device, [rows][C], branch_dtype (needs y) */
+    void *grad_gate;           /* optional device, [gate_groups][C], param_dtype (needs gate) */
+    void *grad_after_weight, *grad_after_bias;   /* optional device, [C], param_dtype (need the norm) */
+    void *grad_before_weight, *grad_before_bias;
+    int64_t rows, gate_groups;
+    int32_t C;
+    int32_t after, before;
+    int32_t dtype, branch_dtype, param_dtype;
+    int64_t ld_grad_h, ld_grad_n, ld_x, ld_y, ld_grad_x, ld_grad_y; /* distance of rows in elements; 0: dense */
+    double scale, eps;
+    void *workspace;           /* DEVICE scratch, 16-byte aligned, flashbev_block_norm_backward_workspace_bytes(p) bytes, else
+                                  FLASHBEV_TOO_SMALL; NULL only where that is 0 */
+    size_t workspace_bytes;
+} flashbev_block_norm_backward_params;
+
+flashbev_status flashbev_block_norm_backward(const flashbev_block_norm_backward_params *p, void *stream);
+size_t flashbev_block_norm_backward_workspace_bytes(const flashbev_block_norm_backward_params *p);
+
 /* Number of kernels the last successful call of flashbev_sampling_vt[_host] on this thread
  * enqueued (always 1), and a short name of the kernel instance it chose (static storage). */
 int flashbev_last_launch_count(void);

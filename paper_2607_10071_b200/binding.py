@@ -22,6 +22,9 @@ F32, BF16 = 0, 1
 NHWC, NCHW = 0, 1
 REDUCE_SUM, REDUCE_MEAN_OVER_VALID, REDUCE_CAMERA_MEAN_Z_SUM = 0, 1, 2
 KERNEL_AUTO, KERNEL_PER_OUTPUT, KERNEL_TILED = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = range(4)
+NORM_NONE, NORM_LAYER, NORM_RMS = range(3)
+NORM_MAX_CHANNELS = 4096
 
 
 class VtParams(ctypes.Structure):
@@ -104,6 +107,76 @@ class VtMultiresParams(ctypes.Structure):
     ]
 
 
+class LinearParams(ctypes.Structure):
+    """Mirror of ``flashbev_linear_params``."""
+    _fields_ = [
+        ("struct_size", ctypes.c_size_t),
+        ("x", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("residual", ctypes.c_void_p),
+        ("out", ctypes.c_void_p), ("preact_out", ctypes.c_void_p),
+        ("rows", ctypes.c_int64),
+        ("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32),
+        ("ld_x", ctypes.c_int64), ("ld_weight", ctypes.c_int64), ("ld_residual", ctypes.c_int64), ("ld_out", ctypes.c_int64),
+        ("ld_preact", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("error_word", ctypes.c_void_p),
+    ]
+
+
+class LinearBackwardParams(ctypes.Structure):
+    """Mirror of ``flashbev_linear_backward_params``."""
+    _fields_ = [
+        ("struct_size", ctypes.c_size_t),
+        ("grad_out", ctypes.c_void_p), ("x", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("preact", ctypes.c_void_p),
+        ("grad_x", ctypes.c_void_p), ("grad_weight", ctypes.c_void_p), ("grad_bias", ctypes.c_void_p),
+        ("rows", ctypes.c_int64),
+        ("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32),
+        ("ld_grad_out", ctypes.c_int64), ("ld_x", ctypes.c_int64), ("ld_weight", ctypes.c_int64), ("ld_preact", ctypes.c_int64),
+        ("ld_grad_x", ctypes.c_int64), ("ld_grad_weight", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("error_word", ctypes.c_void_p),
+    ]
+
+
+class BlockNormParams(ctypes.Structure):
+    """Mirror of ``flashbev_block_norm_params``."""
+    _fields_ = [
+        ("struct_size", ctypes.c_size_t),
+        ("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("gate", ctypes.c_void_p),
+        ("after_weight", ctypes.c_void_p), ("after_bias", ctypes.c_void_p),
+        ("before_weight", ctypes.c_void_p), ("before_bias", ctypes.c_void_p),
+        ("h", ctypes.c_void_p), ("n", ctypes.c_void_p),
+        ("rows", ctypes.c_int64), ("gate_groups", ctypes.c_int64),
+        ("C", ctypes.c_int32),
+        ("after", ctypes.c_int32), ("before", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("branch_dtype", ctypes.c_int32), ("param_dtype", ctypes.c_int32),
+        ("ld_x", ctypes.c_int64), ("ld_y", ctypes.c_int64), ("ld_h", ctypes.c_int64), ("ld_n", ctypes.c_int64),
+        ("scale", ctypes.c_double), ("eps", ctypes.c_double),
+    ]
+
+
+class BlockNormBackwardParams(ctypes.Structure):
+    """Mirror of ``flashbev_block_norm_backward_params``."""
+    _fields_ = [
+        ("struct_size", ctypes.c_size_t),
+        ("grad_h", ctypes.c_void_p), ("grad_n", ctypes.c_void_p),
+        ("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("gate", ctypes.c_void_p),
+        ("after_weight", ctypes.c_void_p), ("after_bias", ctypes.c_void_p), ("before_weight", ctypes.c_void_p),
+        ("grad_x", ctypes.c_void_p), ("grad_y", ctypes.c_void_p), ("grad_gate", ctypes.c_void_p),
+        ("grad_after_weight", ctypes.c_void_p), ("grad_after_bias", ctypes.c_void_p),
+        ("grad_before_weight", ctypes.c_void_p), ("grad_before_bias", ctypes.c_void_p),
+        ("rows", ctypes.c_int64), ("gate_groups", ctypes.c_int64),
+        ("C", ctypes.c_int32),
+        ("after", ctypes.c_int32), ("before", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("branch_dtype", ctypes.c_int32), ("param_dtype", ctypes.c_int32),
+        ("ld_grad_h", ctypes.c_int64), ("ld_grad_n", ctypes.c_int64), ("ld_x", ctypes.c_int64), ("ld_y", ctypes.c_int64),
+        ("ld_grad_x", ctypes.c_int64), ("ld_grad_y", ctypes.c_int64),
+        ("scale", ctypes.c_double), ("eps", ctypes.c_double),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
 MAX_LEVELS = 8
 
 
@@ -131,6 +204,13 @@ def _declare(L: ctypes.CDLL) -> ctypes.CDLL:
     L.flashbev_sampling_vt_multires.argtypes = [ctypes.POINTER(VtMultiresParams), ctypes.c_void_p]
     L.flashbev_sca.restype = ctypes.c_int
     L.flashbev_sca.argtypes = [ctypes.POINTER(ScaParams), ctypes.c_void_p]
+    L.flashbev_block_norm.restype = ctypes.c_int
+    L.flashbev_block_norm.argtypes = [ctypes.POINTER(BlockNormParams), ctypes.c_void_p]
+    for name, params in (("linear", LinearParams), ("linear_backward", LinearBackwardParams),
+                         ("block_norm_backward", BlockNormBackwardParams)):
+        call, need = getattr(L, f"flashbev_{name}"), getattr(L, f"flashbev_{name}_workspace_bytes")
+        call.restype, call.argtypes = ctypes.c_int, [ctypes.POINTER(params), ctypes.c_void_p]
+        need.restype, need.argtypes = ctypes.c_size_t, [ctypes.POINTER(params)]
     L.flashbev_workspace_bytes.restype = ctypes.c_size_t
     L.flashbev_workspace_bytes.argtypes = [P]
     L.flashbev_host_staging_bytes.restype = ctypes.c_size_t
@@ -311,6 +391,86 @@ def sca(value, level_hw, lidar2img, offsets, weights, img_hw, bev_range, grid, o
     level_hw: sequence of (H_l, W_l).  Returns CUDA float32 [B, Q, heads*Dh] (marshalling only)."""
     return _result((_native or native()).sca(value, level_hw, lidar2img, offsets, weights, img_hw, bev_range, grid, out, hits,
                                              stream, chunk_records), "flashbev_sca")
+
+
+def flashbev_linear(params: LinearParams, stream: int | None = None, check: bool = True) -> int:
+    """Enqueue a matrix product with its epilogue on ``stream``."""
+    st = lib().flashbev_linear(ctypes.byref(params), ctypes.c_void_p(stream or 0))
+    if check and st != OK:
+        raise FlashBevError(st, "flashbev_linear")
+    return st
+
+
+def flashbev_linear_workspace_bytes(params: LinearParams) -> int:
+    return int(lib().flashbev_linear_workspace_bytes(ctypes.byref(params)))
+
+
+def flashbev_linear_backward(params: LinearBackwardParams, stream: int | None = None, check: bool = True) -> int:
+    """Enqueue the gradients of a matrix product on ``stream``."""
+    st = lib().flashbev_linear_backward(ctypes.byref(params), ctypes.c_void_p(stream or 0))
+    if check and st != OK:
+        raise FlashBevError(st, "flashbev_linear_backward")
+    return st
+
+
+def flashbev_linear_backward_workspace_bytes(params: LinearBackwardParams) -> int:
+    return int(lib().flashbev_linear_backward_workspace_bytes(ctypes.byref(params)))
+
+
+def linear(x, weight, bias=None, act=ACT_NONE, residual=None, out=None, out_dtype=None, preact=None, stream=None):
+    """``residual + act(x weight^T + bias)``: x CUDA [..., K], weight [N, K], bias [N] of one type (float32 or bfloat16), residual
+    and result [..., N] of ``out_dtype`` (F32, BF16; None: that of ``out``, or of x).  Rows may be any equal distance apart.
+    ``preact``: [..., N] tensor of x's type that receives ``x weight^T + bias``, for ``linear_backward``.  ``out`` may be
+    ``residual``.  ``stream``: a raw cudaStream_t, as for ``sampling_vt``."""
+    return _result((_native or native()).linear(x, weight, bias, act, residual, out, out_dtype, preact, stream), "flashbev_linear")
+
+
+def linear_backward(grad_out, x, weight, act=ACT_NONE, preact=None, grad_x=True, grad_weight=True, grad_bias=True, stream=None):
+    """Gradients of ``linear`` at x, weight and bias from that at its result (float32 or bfloat16; the residual's is that gradient
+    itself).  ``preact``: what the forward call kept; needed with an activation.  Returns (grad_x, grad_weight, grad_bias) of
+    x's type, None for those not wanted."""
+    return _result((_native or native()).linear_backward(grad_out, x, weight, act, preact, grad_x, grad_weight, grad_bias, stream),
+                   "flashbev_linear_backward")
+
+
+def flashbev_block_norm(params: BlockNormParams, stream: int | None = None, check: bool = True) -> int:
+    """Enqueue the norms and the sum between two blocks on ``stream``."""
+    st = lib().flashbev_block_norm(ctypes.byref(params), ctypes.c_void_p(stream or 0))
+    if check and st != OK:
+        raise FlashBevError(st, "flashbev_block_norm")
+    return st
+
+
+def flashbev_block_norm_backward(params: BlockNormBackwardParams, stream: int | None = None, check: bool = True) -> int:
+    """Enqueue the gradients of the norms and the sum between two blocks on ``stream``."""
+    st = lib().flashbev_block_norm_backward(ctypes.byref(params), ctypes.c_void_p(stream or 0))
+    if check and st != OK:
+        raise FlashBevError(st, "flashbev_block_norm_backward")
+    return st
+
+
+def flashbev_block_norm_backward_workspace_bytes(params: BlockNormBackwardParams) -> int:
+    return int(lib().flashbev_block_norm_backward_workspace_bytes(ctypes.byref(params)))
+
+
+def block_norm(x, y=None, gate=None, scale=1.0, after=NORM_NONE, after_weight=None, after_bias=None, before=NORM_LAYER,
+               before_weight=None, before_bias=None, eps=1e-5, h=None, n=None, keep_h=True, stream=None):
+    """Between two residual blocks: ``h = x + scale * gate * after(y)``, ``n = before(h)``; returns (h, n).
+
+    x, h: CUDA [..., C], float32 or bfloat16; y, n: the same shape, of x's type or bfloat16; rows may be any equal distance apart.
+    gate: [C], or [gates, C] for equal runs of rows (one per sample, or one per row).  ``after`` and ``before``: NORM_NONE,
+    NORM_LAYER or NORM_RMS, with optional parameters [C]; all parameters are float32 or of y's type.  Without y only ``n = before(x)``
+    is made.  ``keep_h=False``: h is not written (None) unless given as a tensor.  h may be x and n may be y."""
+    return _result((_native or native()).block_norm(x, y, gate, scale, after, after_weight, after_bias, before, before_weight, before_bias,
+                                                    eps, h, n, keep_h, stream), "flashbev_block_norm")
+
+
+def block_norm_backward(grad_h, grad_n, x, y=None, gate=None, scale=1.0, after=NORM_NONE, after_weight=None, after_bias=None,
+                        before=NORM_LAYER, before_weight=None, before_bias=None, eps=1e-5, stream=None):
+    """Gradients of ``block_norm`` at the same arguments from those at h and n (None: no such gradient).  Returns those at (x, y,
+    gate, after_weight, after_bias, before_weight, before_bias), None for arguments that are None."""
+    return _result((_native or native()).block_norm_backward(x, y, gate, scale, after, after_weight, after_bias, before, before_weight,
+                                                             before_bias, eps, grad_h, grad_n, stream), "flashbev_block_norm_backward")
 
 
 def flashbev_workspace_bytes(params: VtParams) -> int:

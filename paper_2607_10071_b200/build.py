@@ -10,13 +10,13 @@ import sysconfig
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
-SOURCES = [os.path.join(_HERE, "csrc", "flashbev.cu")]
-HEADERS = [os.path.join(ROOT, "include", "flashbev.h"), os.path.join(_HERE, "csrc", "vt_tiled.cuh"),
-           os.path.join(_HERE, "csrc", "vt_backward.cuh")]
+SOURCES = [os.path.join(_HERE, "csrc", f) for f in ("flashbev.cu", "linear.cu", "block_norm.cu")]
+HEADERS = [os.path.join(ROOT, "include", "flashbev.h")] + [
+    os.path.join(_HERE, "csrc", f) for f in ("vt_tiled.cuh", "vt_backward.cuh", "launch.cuh", "tcgen05.cuh")]
 LIB = os.path.join(_HERE, "libflashbev.so")
 
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-              "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include")]
+              "-Xcompiler", "-fPIC", "-shared", "--threads", "4", "-I", os.path.join(ROOT, "include")]
 
 
 LIB_DEBUG_BOUNDS = os.path.join(_HERE, "libflashbev_debug_bounds.so")

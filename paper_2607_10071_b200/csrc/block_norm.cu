@@ -1,0 +1,725 @@
+// The norms behind and ahead of a residual block, fused with its gate, its residual scale and the sum (flashbev_block_norm of
+// flashbev.h), and their gradients.
+//
+// All of a row is in the registers of a team of threads, eight elements each: every tensor is read once and written once, and the
+// two or three statistics of a row are sums over the team (shuffles; across warps through shared memory).  Bound by memory traffic.  A
+// team is the power of two of threads, from 4 to 1024, that holds the row, so that narrow rows share a warp; blocks stay and
+// walk over the rows with the parameters in registers, and the next row's loads are under way while one is worked on.
+#include "flashbev.h"
+#include "launch.cuh"
+
+#include <cuda_bf16.h>
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+#include <initializer_list>
+#include <type_traits>
+
+using namespace flashbev_host;
+
+namespace {
+
+using bf16 = __nv_bfloat16;
+
+constexpr int kE = 8;  // elements of a row per thread
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(bf16 v) { return __bfloat162float(v); }
+template <typename T>
+__device__ __forceinline__ T from_float(float v)
+{
+    if constexpr (std::is_same<T, float>::value) return v;
+    else return __float2bfloat16_rn(v);
+}
+
+struct NormParams {
+    const void *x, *y, *gate, *wa, *ba, *wb, *bb;
+    void *h, *n;
+    const void *gh, *gn;        // backward: gradients at h and n, then those at x, y and (per row) the gate
+    void *gx, *gy, *ggate;
+    float *sums;                // backward: [array][block][C] partial sums of the parameters' gradients
+    int want;                   // which arrays: bit 0 after weight, 1 after bias, 2 before weight, 3 before bias, 4 gate
+    long long rows, per_gate;   // per_gate: rows that share a gate
+    long long ld_x, ld_y, ld_h, ld_n, ld_gh, ld_gn, ld_gx, ld_gy;
+    int C, after, before, team; // team: threads per row
+    int chunks, direct;         // backward: blocks per gate; or `direct`: a team takes whole gates
+    long long gates;
+    float scale, eps, inv_c;
+};
+
+// The eight elements of a thread: neighbours (VEC: 16-byte accesses; C a multiple of 8) or every team-th.
+template <typename T>
+struct Raw {
+    T v[kE];
+};
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void read(Raw<T> &r, const T *row, int t, int team, int C)
+{
+    if constexpr (VEC) {
+        constexpr int Q = kE * (int)sizeof(T) / 16;
+        if (t * kE < C) {
+            uint4 q[Q];
+#pragma unroll
+            for (int i = 0; i < Q; ++i) q[i] = reinterpret_cast<const uint4 *>(row + t * kE)[i];
+            memcpy(r.v, q, sizeof(q));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kE; ++i)
+            if (t + i * team < C) r.v[i] = row[t + i * team];
+    }
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void write(T *row, const float (&f)[kE], int t, int team, int C)
+{
+    if constexpr (VEC) {
+        constexpr int Q = kE * (int)sizeof(T) / 16;
+        if (t * kE < C) {
+            Raw<T> r;
+#pragma unroll
+            for (int i = 0; i < kE; ++i) r.v[i] = from_float<T>(f[i]);
+            uint4 q[Q];
+            memcpy(q, r.v, sizeof(q));
+#pragma unroll
+            for (int i = 0; i < Q; ++i) reinterpret_cast<uint4 *>(row + t * kE)[i] = q[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kE; ++i)
+            if (t + i * team < C) row[t + i * team] = from_float<T>(f[i]);
+    }
+}
+
+// Whether element i of this thread is one of the row's
+template <bool VEC>
+__device__ __forceinline__ bool has(int i, int t, int team, int C)
+{
+    return VEC ? t * kE < C : t + i * team < C;
+}
+
+// The norms' parameters lie in shared memory as floats, `count` vectors one after another, 1 or 0 where there is none: in registers
+// they would be 32 of a thread, and of the gradients' kernel 72 with their sums.
+template <typename P>
+__device__ __forceinline__ void stage_params(float *to, const void *const (&from)[4], int count, int C)
+{
+    for (int j = 0; j < count; ++j)
+        for (int c = threadIdx.x; c < C; c += blockDim.x)
+            to[j * C + c] = from[j] ? to_float(static_cast<const P *>(from[j])[c]) : (j % 2 ? 0.0f : 1.0f);
+    __syncthreads();
+}
+
+template <bool VEC>
+__device__ __forceinline__ void read_param(float (&f)[kE], const float *p, int t, int team, int C)
+{
+    if constexpr (VEC) {
+        const float4 *const q = reinterpret_cast<const float4 *>(p + (t * kE < C ? t * kE : 0));
+        const float4 a = q[0], b = q[1];
+        f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kE; ++i) f[i] = p[t + i * team < C ? t + i * team : 0];
+    }
+}
+
+// The gate of row `g`, times the scale.  It is read for every row (from L1, where rows share it).
+template <typename P, bool VEC>
+__device__ __forceinline__ void read_gate(float (&f)[kE], const void *gate, long long g, float scale, int t, int team, int C)
+{
+    Raw<P> r;
+    if (gate) read<P, VEC>(r, static_cast<const P *>(gate) + g * C, t, team, C);
+#pragma unroll
+    for (int i = 0; i < kE; ++i) f[i] = gate ? (has<VEC>(i, t, team, C) ? scale * to_float(r.v[i]) : 0.0f) : scale;
+}
+
+// Sums over a team.  WIDE: teams of several warps.
+template <bool WIDE>
+struct Team {
+    int threads, t, slot;       // threads of a team; this one's place in it; the team's place in the block
+    float2 *shared;             // WIDE: [2][32] of this team
+    int turn;
+
+    __device__ __forceinline__ float2 sum(float a, float b)
+    {
+        const int most = WIDE ? 16 : threads / 2;
+#pragma unroll
+        for (int d = 16; d; d /= 2)
+            if (d <= most) a += __shfl_xor_sync(0xffffffffu, a, d), b += __shfl_xor_sync(0xffffffffu, b, d);
+        if constexpr (WIDE) {
+            // (two buffers in turn: who writes the one again has passed the barrier of the other, after everybody read the one)
+            float2 *const buf = shared + 32 * turn;
+            turn ^= 1;
+            const int warps = threads / 32;
+            if (t % 32 == 0) buf[t / 32] = make_float2(a, b);
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + slot), "r"(threads) : "memory");
+            const float2 v = t % 32 < warps ? buf[t % 32] : make_float2(0.0f, 0.0f);
+            a = v.x, b = v.y;
+#pragma unroll
+            for (int d = 16; d; d /= 2) a += __shfl_xor_sync(0xffffffffu, a, d), b += __shfl_xor_sync(0xffffffffu, b, d);
+        }
+        return make_float2(a, b);
+    }
+    __device__ __forceinline__ float sum(float a)
+    {
+        const int most = WIDE ? 16 : threads / 2;
+#pragma unroll
+        for (int d = 16; d; d /= 2)
+            if (d <= most) a += __shfl_xor_sync(0xffffffffu, a, d);
+        if constexpr (WIDE) {
+            float2 *const buf = shared + 32 * turn;
+            turn ^= 1;
+            if (t % 32 == 0) buf[t / 32].x = a;
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + slot), "r"(threads) : "memory");
+            a = t % 32 < threads / 32 ? buf[t % 32].x : 0.0f;
+#pragma unroll
+            for (int d = 16; d; d /= 2) a += __shfl_xor_sync(0xffffffffu, a, d);
+        }
+        return a;
+    }
+};
+
+// v becomes (v - mean) / deviation (or v / root mean square); returns 1 / deviation.  Elements behind the row's end are 0 before and after.
+template <bool VEC, bool WIDE>
+__device__ __forceinline__ float whiten(float (&v)[kE], int kind, const NormParams &p, Team<WIDE> &team)
+{
+    float s = 0.0f;
+    if (kind == FLASHBEV_NORM_LAYER) {
+#pragma unroll
+        for (int i = 0; i < kE; ++i) s += v[i];
+        const float mean = team.sum(s) * p.inv_c;
+#pragma unroll
+        for (int i = 0; i < kE; ++i) v[i] = has<VEC>(i, team.t, team.threads, p.C) ? v[i] - mean : 0.0f;
+    }
+    s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kE; ++i) s = fmaf(v[i], v[i], s);
+    const float r = 1.0f / sqrtf(team.sum(s) * p.inv_c + p.eps);
+#pragma unroll
+    for (int i = 0; i < kE; ++i) v[i] *= r;
+    return r;
+}
+
+// Gradient at the input of `whiten` from that at its result t: r (g - mean(g) - t mean(g t)), without mean(g) for root mean squares.
+template <bool VEC, bool WIDE>
+__device__ __forceinline__ void whiten_back(float (&g)[kE], const float (&t)[kE], float r, int kind, const NormParams &p, Team<WIDE> &team)
+{
+    float a = 0.0f, b = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kE; ++i) a += g[i], b = fmaf(g[i], t[i], b);
+    const float2 s = team.sum(a, b);
+    const float mean = kind == FLASHBEV_NORM_LAYER ? s.x * p.inv_c : 0.0f, along = s.y * p.inv_c;
+#pragma unroll
+    for (int i = 0; i < kE; ++i) g[i] = has<VEC>(i, team.t, team.threads, p.C) ? r * (g[i] - mean - t[i] * along) : 0.0f;
+}
+
+template <bool WIDE>
+__device__ __forceinline__ Team<WIDE> make_team(const NormParams &p, float2 *shared)
+{
+    Team<WIDE> team;
+    team.threads = p.team, team.slot = threadIdx.x / p.team, team.t = threadIdx.x % p.team, team.turn = 0;
+    team.shared = shared + (WIDE ? 64 * team.slot : 0);
+    return team;
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void widen(float (&f)[kE], const Raw<T> &r, int t, int team, int C)
+{
+#pragma unroll
+    for (int i = 0; i < kE; ++i) f[i] = has<VEC>(i, t, team, C) ? to_float(r.v[i]) : 0.0f;
+}
+
+constexpr int kMostThreads = FLASHBEV_NORM_MAX_CHANNELS / kE;
+
+// S, T, P: types of x and h, of y and n, of the parameters.
+template <typename S, typename T, typename P, bool VEC, bool WIDE>
+__global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 3) norm_kernel(const __grid_constant__ NormParams p)
+{
+    __shared__ float2 shared[WIDE ? 64 * 4 : 1];  // (at most four teams of 64 threads in a block)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+    Team<WIDE> team = make_team<WIDE>(p, shared);
+    const int t = team.t, threads = p.team, C = p.C, teams = blockDim.x / threads;
+    extern __shared__ __align__(16) float params[];  // before weight, before bias, after weight, after bias
+    stage_params<P>(params, {p.wb, p.bb, p.wa, p.ba}, p.after != FLASHBEV_NORM_NONE ? 4 : 2, C);
+    const long long step = (long long)gridDim.x * teams, first = (long long)blockIdx.x * teams + team.slot;
+    // (narrow teams share a warp's shuffles: all of them go as long as one has a row)
+    const long long lead = WIDE ? first : first - (threadIdx.x % 32) / threads;
+    Raw<S> xr;
+    Raw<T> yr;
+    const auto bring = [&](long long row) {
+        if (row >= p.rows) return;
+        read<S, VEC>(xr, static_cast<const S *>(p.x) + row * p.ld_x, t, threads, C);
+        if (p.y) read<T, VEC>(yr, static_cast<const T *>(p.y) + row * p.ld_y, t, threads, C);
+    };
+    bring(first);
+    for (long long row = first, at = lead; at < p.rows; row += step, at += step) {
+        const bool live = row < p.rows;
+        float h[kE], m[kE];
+        widen<S, VEC>(h, xr, t, threads, live ? C : 0);
+        if (p.y) widen<T, VEC>(m, yr, t, threads, live ? C : 0);
+        bring(row + step);
+        if (p.y) {
+            if (p.after != FLASHBEV_NORM_NONE) {
+                whiten<VEC, WIDE>(m, p.after, p, team);
+                float w[kE], b[kE];
+                read_param<VEC>(w, params + 2 * C, t, threads, C);
+                read_param<VEC>(b, params + 3 * C, t, threads, C);
+#pragma unroll
+                for (int i = 0; i < kE; ++i) m[i] = fmaf(m[i], w[i], b[i]);
+            }
+            if (p.gate) {
+                float gate[kE];
+                read_gate<P, VEC>(gate, p.gate, live ? (int)row / (int)p.per_gate : 0, p.scale, t, threads, C);
+#pragma unroll
+                for (int i = 0; i < kE; ++i) m[i] *= gate[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < kE; ++i) m[i] *= p.scale;
+            }
+#pragma unroll
+            for (int i = 0; i < kE; ++i) h[i] = has<VEC>(i, t, threads, C) ? h[i] + m[i] : 0.0f;
+            if (p.h && live) write<S, VEC>(static_cast<S *>(p.h) + row * p.ld_h, h, t, threads, C);
+        }
+        if (p.before != FLASHBEV_NORM_NONE) {
+            whiten<VEC, WIDE>(h, p.before, p, team);
+            float w[kE], b[kE];
+            read_param<VEC>(w, params, t, threads, C);
+            read_param<VEC>(b, params + C, t, threads, C);
+#pragma unroll
+            for (int i = 0; i < kE; ++i) h[i] = fmaf(h[i], w[i], b[i]);
+            if (live) write<T, VEC>(static_cast<T *>(p.n) + row * p.ld_n, h, t, threads, C);
+        }
+    }
+}
+
+// Gradients.  The rows of a gate are shared by `chunks` blocks, whose teams take every so manieth row; sums over rows stay in
+// registers until the block's end, when they are added up over its teams in a fixed order.  `direct`: there are many gates with few rows, and a
+// team takes the rows of one gate after another and writes the gate's gradient itself.
+template <typename S, typename T, typename P, bool VEC, bool WIDE>
+__global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 2) norm_backward_kernel(const __grid_constant__ NormParams p)
+{
+    __shared__ float2 shared[WIDE ? 64 * 4 : 1];
+    __shared__ float joined[2048];  // [teams (warps, where a warp has several)][C]
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+    Team<WIDE> team = make_team<WIDE>(p, shared);
+    const int t = team.t, threads = p.team, C = p.C, teams = blockDim.x / threads;
+    extern __shared__ __align__(16) float params[];  // before weight, after bias, after weight
+    stage_params<P>(params, {p.wb, p.ba, p.wa, nullptr}, p.after != FLASHBEV_NORM_NONE ? 3 : 1, C);
+    float dwa[kE], dba[kE], dwb[kE], dbb[kE], dg[kE];
+#pragma unroll
+    for (int i = 0; i < kE; ++i) dwa[i] = dba[i] = dwb[i] = dbb[i] = dg[i] = 0.0f;
+
+    const int inside = WIDE ? 0 : (threadIdx.x % 32) / threads;  // place of the team in its warp
+    long long g, g_step, g_lead;
+    if (p.direct) {
+        g = (long long)blockIdx.x * teams + team.slot, g_step = (long long)gridDim.x * teams;
+        g_lead = g - inside;
+    } else {
+        g = g_lead = blockIdx.x / p.chunks, g_step = p.gates;
+    }
+    for (; g_lead < p.gates; g += g_step, g_lead += g_step) {
+        long long row, end, step, lead;
+        const bool mine = g < p.gates;
+        if (p.direct) {
+            row = g * p.per_gate, end = mine ? row + p.per_gate : 0, step = 1;
+            lead = 0;
+        } else {
+            const int chunk = (int)(blockIdx.x - g * p.chunks);
+            const long long base = g * p.per_gate, share = (p.per_gate + p.chunks - 1) / p.chunks;
+            end = base + min(p.per_gate, (chunk + 1) * share);
+            row = base + chunk * share + team.slot, step = teams;
+            lead = 0;
+        }
+        // every team of a warp goes around as often
+        const long long rounds = p.direct ? p.per_gate : (end - (row - inside) + step - 1) / step;
+        Raw<S> xr, ghr;
+        Raw<T> yr, gnr;
+        const auto bring = [&](long long at) {
+            if (at >= end) return;
+            read<S, VEC>(xr, static_cast<const S *>(p.x) + at * p.ld_x, t, threads, C);
+            if (p.y) read<T, VEC>(yr, static_cast<const T *>(p.y) + at * p.ld_y, t, threads, C);
+            if (p.gn) read<T, VEC>(gnr, static_cast<const T *>(p.gn) + at * p.ld_gn, t, threads, C);
+            if (p.gh) read<S, VEC>(ghr, static_cast<const S *>(p.gh) + at * p.ld_gh, t, threads, C);
+        };
+        bring(row);
+        for (; lead < rounds; ++lead, row += step) {
+            const bool live = row < end;
+            const int have = live ? C : 0;
+            float u[kE], v[kE], gn[kE], gh[kE];
+            widen<S, VEC>(u, xr, t, threads, have);
+            if (p.y) widen<T, VEC>(v, yr, t, threads, have);
+            if (p.gn) widen<T, VEC>(gn, gnr, t, threads, have);
+            if (p.gh) {
+                widen<S, VEC>(gh, ghr, t, threads, have);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kE; ++i) gh[i] = 0.0f;
+            }
+            bring(row + step);
+            // after(y), of which v keeps the part without the parameters
+            const auto branch = [&](float (&m)[kE]) {
+                if (p.after != FLASHBEV_NORM_NONE) {
+                    float w[kE], b[kE];
+                    read_param<VEC>(w, params + 2 * C, t, threads, C);
+                    read_param<VEC>(b, params + C, t, threads, C);
+#pragma unroll
+                    for (int i = 0; i < kE; ++i) m[i] = fmaf(v[i], w[i], b[i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kE; ++i) m[i] = v[i];
+                }
+            };
+            float ra = 0.0f;
+            if (p.after != FLASHBEV_NORM_NONE) ra = whiten<VEC, WIDE>(v, p.after, p, team);
+            if (p.before != FLASHBEV_NORM_NONE) {
+                if (p.y) {
+                    float m[kE], gate[kE];
+                    branch(m);
+                    read_gate<P, VEC>(gate, p.gate, mine ? g : 0, p.scale, t, threads, C);
+#pragma unroll
+                    for (int i = 0; i < kE; ++i) u[i] = has<VEC>(i, t, threads, have) ? fmaf(m[i], gate[i], u[i]) : 0.0f;
+                }
+                const float rb = whiten<VEC, WIDE>(u, p.before, p, team);
+                float w[kE];
+                read_param<VEC>(w, params, t, threads, C);
+#pragma unroll
+                for (int i = 0; i < kE; ++i) {
+                    dwb[i] = fmaf(gn[i], u[i], dwb[i]), dbb[i] += gn[i];
+                    gn[i] *= w[i];
+                }
+                whiten_back<VEC, WIDE>(gn, u, rb, p.before, p, team);
+                if (live)
+#pragma unroll
+                    for (int i = 0; i < kE; ++i) gh[i] += gn[i];
+            }
+            if (p.gx && live) write<S, VEC>(static_cast<S *>(p.gx) + row * p.ld_gx, gh, t, threads, C);
+            if (!p.y) continue;
+            if (live && p.ggate) {
+                float m[kE];
+                branch(m);
+#pragma unroll
+                for (int i = 0; i < kE; ++i) dg[i] = fmaf(gh[i] * p.scale, m[i], dg[i]);
+            }
+            {
+                float gate[kE];
+                read_gate<P, VEC>(gate, p.gate, mine ? g : 0, p.scale, t, threads, C);
+#pragma unroll
+                for (int i = 0; i < kE; ++i) gh[i] *= gate[i];
+            }
+            if (p.after != FLASHBEV_NORM_NONE) {
+                float w[kE];
+                read_param<VEC>(w, params + 2 * C, t, threads, C);
+#pragma unroll
+                for (int i = 0; i < kE; ++i) {
+                    if (live) dwa[i] = fmaf(gh[i], v[i], dwa[i]), dba[i] += gh[i];
+                    gh[i] *= w[i];
+                }
+                whiten_back<VEC, WIDE>(gh, v, ra, p.after, p, team);
+            }
+            if (p.gy && live) write<T, VEC>(static_cast<T *>(p.gy) + row * p.ld_gy, gh, t, threads, C);
+        }
+        if (p.direct) {
+            if (p.ggate && mine) write<P, VEC>(static_cast<P *>(p.ggate) + g * C, dg, t, threads, C);
+#pragma unroll
+            for (int i = 0; i < kE; ++i) dg[i] = 0.0f;
+        }
+    }
+    // sums over the block's teams, one array after another
+    long long array = 0;
+    const int slots = WIDE ? teams : blockDim.x / 32, slot = WIDE ? team.slot : threadIdx.x / 32;
+    const auto put = [&](float (&d)[kE], int bit) {
+        if (!(p.want >> bit & 1)) return;
+        float *const out = p.sums + (array++ * gridDim.x + blockIdx.x) * (long long)C;
+        if (!WIDE) {
+#pragma unroll
+            for (int s = 16; s; s /= 2)
+                if (s >= threads)
+#pragma unroll
+                    for (int i = 0; i < kE; ++i) d[i] += __shfl_xor_sync(0xffffffffu, d[i], s);
+        }
+        if (slots == 1) {
+            write<float, false>(out, d, VEC ? t * kE : t, VEC ? 1 : threads, C);
+            return;
+        }
+        __syncthreads();  // (the array before has been read)
+        if (WIDE || inside == 0) write<float, false>(joined + slot * C, d, VEC ? t * kE : t, VEC ? 1 : threads, C);
+        __syncthreads();
+        for (int c = threadIdx.x; c < C; c += blockDim.x) {
+            float s = 0.0f;
+            for (int w = 0; w < slots; ++w) s += joined[w * C + c];
+            out[c] = s;
+        }
+    };
+    put(dwa, 0), put(dba, 1), put(dwb, 2), put(dbb, 3), put(dg, 4);
+}
+
+struct SumJobs {
+    void *out[5];
+    int first[6];               // blocks of job j: first[j] .. first[j + 1], 32 columns of one output row each
+    int blocks, per, C;         // partial rows of an array; those of one output row of the gate (job 4 sums every `per` of them)
+};
+
+// Adds the blocks' sums up in a fixed order: 16 warps take every sixteenth.
+template <typename P>
+__global__ void __launch_bounds__(512) norm_sum_kernel(const float *__restrict__ sums, const __grid_constant__ SumJobs q)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+    __shared__ float part[16][33];
+    int j = 0, array = 0;
+    while (j < 4 && (int)blockIdx.x >= q.first[j + 1]) array += q.first[j + 1] > q.first[j], ++j;
+    const int across = (q.C + 31) / 32, b = blockIdx.x - q.first[j], line = b / across, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int col = (b - line * across) * 32 + lane, rows = j == 4 ? q.per : q.blocks;
+    const float *const src = sums + ((long long)array * q.blocks + (long long)line * rows) * q.C;
+    float v = 0.0f;
+    if (col < q.C)
+#pragma unroll 8
+        for (int r = warp; r < rows; r += 16) v += src[(long long)r * q.C + col];
+    part[warp][lane] = v;
+    __syncthreads();
+    if (warp == 0 && col < q.C) {
+        v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) v += part[w][lane];
+        static_cast<P *>(q.out[j])[(long long)line * q.C + col] = from_float<P>(v);
+    }
+}
+
+// ---- host -------------------------------------------------------------------------------------------------------------------
+
+bool dtype_ok(int d) { return d == FLASHBEV_F32 || d == FLASHBEV_BF16; }
+size_t elem_size(int d) { return d == FLASHBEV_F32 ? 4 : 2; }
+bool aligned(const void *p, int dtype) { return (uintptr_t)p % elem_size(dtype) == 0; }
+bool whole(const void *p, long long ld, int dtype) { return ((uintptr_t)p | (uintptr_t)(ld * (long long)elem_size(dtype))) % 16 == 0; }
+long long dense(long long ld, int C) { return ld ? ld : C; }
+
+int team_threads(int C)
+{
+    int team = 4;
+    while (team * kE < C) team *= 2;
+    return team;
+}
+
+// What the forward and the backward call have in common.
+template <typename Q>
+flashbev_status check_common(const Q *p, std::initializer_list<int64_t> strides)
+{
+    if (p->rows < 0 || p->C <= 0) return FLASHBEV_INVALID_ARG;
+    if (p->after < 0 || p->after > FLASHBEV_NORM_RMS || p->before < 0 || p->before > FLASHBEV_NORM_RMS) return FLASHBEV_INVALID_ARG;
+    if (!dtype_ok(p->dtype) || !dtype_ok(p->branch_dtype) || !dtype_ok(p->param_dtype)) return FLASHBEV_INVALID_ARG;
+    if (!isfinite(p->scale) || !isfinite(p->eps) || p->eps < 0.0) return FLASHBEV_INVALID_ARG;
+    for (long long ld : strides)
+        if (ld != 0 && ld < p->C) return FLASHBEV_INVALID_ARG;
+    if (p->gate && (p->gate_groups <= 0 || p->rows % p->gate_groups || !p->y)) return FLASHBEV_INVALID_ARG;
+    if (!p->y && p->after != FLASHBEV_NORM_NONE && p->rows) return FLASHBEV_INVALID_ARG;
+    if (p->after == FLASHBEV_NORM_NONE && (p->after_weight || p->after_bias)) return FLASHBEV_INVALID_ARG;
+    if (p->before == FLASHBEV_NORM_NONE && p->before_weight) return FLASHBEV_INVALID_ARG;
+    if (p->dtype == FLASHBEV_BF16 && p->branch_dtype == FLASHBEV_F32) return FLASHBEV_UNSUPPORTED;
+    if (p->param_dtype == FLASHBEV_BF16 && p->branch_dtype == FLASHBEV_F32) return FLASHBEV_UNSUPPORTED;
+    if (p->C > FLASHBEV_NORM_MAX_CHANNELS || p->rows > 2147483647LL) return FLASHBEV_UNSUPPORTED;
+    for (long long ld : strides)
+        if ((double)p->rows * (double)dense(ld, p->C) >= 2305843009213693952.0) return FLASHBEV_UNSUPPORTED;
+    const void *const params[] = {p->gate, p->after_weight, p->after_bias, p->before_weight};
+    for (const void *v : params)
+        if (!aligned(v, p->param_dtype)) return FLASHBEV_MISALIGNED;
+    if (!aligned(p->x, p->dtype) || !aligned(p->y, p->branch_dtype)) return FLASHBEV_MISALIGNED;
+    return FLASHBEV_OK;
+}
+
+flashbev_status check_norm(const flashbev_block_norm_params *p)
+{
+    if (!p || p->struct_size < sizeof(*p)) return FLASHBEV_INVALID_ARG;
+    const flashbev_status st = check_common(p, {p->ld_x, p->ld_y, p->ld_h, p->ld_n});
+    if (st != FLASHBEV_OK) return st;
+    if (p->before == FLASHBEV_NORM_NONE && p->before_bias) return FLASHBEV_INVALID_ARG;
+    if (p->rows) {
+        if (!p->x || (p->n != nullptr) != (p->before != FLASHBEV_NORM_NONE)) return FLASHBEV_INVALID_ARG;
+        if ((p->h && !p->y) || (!p->h && !p->n)) return FLASHBEV_INVALID_ARG;
+    }
+    if (!aligned(p->before_bias, p->param_dtype) || !aligned(p->h, p->dtype) || !aligned(p->n, p->branch_dtype)) return FLASHBEV_MISALIGNED;
+    return FLASHBEV_OK;
+}
+
+flashbev_status check_backward(const flashbev_block_norm_backward_params *p)
+{
+    if (!p || p->struct_size < sizeof(*p)) return FLASHBEV_INVALID_ARG;
+    const flashbev_status st = check_common(p, {p->ld_grad_h, p->ld_grad_n, p->ld_x, p->ld_y, p->ld_grad_x, p->ld_grad_y});
+    if (st != FLASHBEV_OK) return st;
+    if (p->rows) {
+        if (!p->x || (p->grad_n != nullptr) != (p->before != FLASHBEV_NORM_NONE)) return FLASHBEV_INVALID_ARG;
+        if ((p->grad_y && !p->y) || (!p->grad_h && !p->grad_n)) return FLASHBEV_INVALID_ARG;
+    }
+    if (p->grad_gate && !p->gate) return FLASHBEV_INVALID_ARG;
+    if ((p->grad_after_weight || p->grad_after_bias) && p->after == FLASHBEV_NORM_NONE) return FLASHBEV_INVALID_ARG;
+    if ((p->grad_before_weight || p->grad_before_bias) && p->before == FLASHBEV_NORM_NONE) return FLASHBEV_INVALID_ARG;
+    const void *const outs[] = {p->grad_gate, p->grad_after_weight, p->grad_after_bias, p->grad_before_weight, p->grad_before_bias};
+    for (const void *v : outs)
+        if (!aligned(v, p->param_dtype)) return FLASHBEV_MISALIGNED;
+    if (!aligned(p->grad_h, p->dtype) || !aligned(p->grad_x, p->dtype) || !aligned(p->grad_n, p->branch_dtype) || !aligned(p->grad_y, p->branch_dtype) ||
+        (uintptr_t)p->workspace % 16)
+        return FLASHBEV_MISALIGNED;
+    return FLASHBEV_OK;
+}
+
+// The instance for the call's types, alignment and width.
+template <bool BACKWARD, typename S, typename T, typename P>
+auto pick(bool vec, bool wide)
+{
+    if constexpr (BACKWARD) {
+        if (vec) return wide ? norm_backward_kernel<S, T, P, true, true> : norm_backward_kernel<S, T, P, true, false>;
+        return wide ? norm_backward_kernel<S, T, P, false, true> : norm_backward_kernel<S, T, P, false, false>;
+    } else {
+        if (vec) return wide ? norm_kernel<S, T, P, true, true> : norm_kernel<S, T, P, true, false>;
+        return wide ? norm_kernel<S, T, P, false, true> : norm_kernel<S, T, P, false, false>;
+    }
+}
+
+template <bool BACKWARD>
+cudaError_t launch_norm(const NormParams &k, int dtype, int branch, int param, bool vec, unsigned blocks, int threads, cudaStream_t stream)
+{
+    const bool wide = k.team > 32;
+    void (*kernel)(NormParams);
+    if (dtype == FLASHBEV_F32 && branch == FLASHBEV_F32) kernel = pick<BACKWARD, float, float, float>(vec, wide);
+    else if (dtype == FLASHBEV_F32 && param == FLASHBEV_F32) kernel = pick<BACKWARD, float, bf16, float>(vec, wide);
+    else if (dtype == FLASHBEV_F32) kernel = pick<BACKWARD, float, bf16, bf16>(vec, wide);
+    else if (param == FLASHBEV_F32) kernel = pick<BACKWARD, bf16, bf16, float>(vec, wide);
+    else kernel = pick<BACKWARD, bf16, bf16, bf16>(vec, wide);
+    const size_t vectors = BACKWARD ? (k.after != FLASHBEV_NORM_NONE ? 3 : 1) : (k.after != FLASHBEV_NORM_NONE ? 4 : 2);
+    const size_t smem = vectors * k.C * sizeof(float);
+    if (smem > 36 * 1024) {  // (beside up to 10 KB that the kernels declare themselves)
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_dependent(kernel, dim3(blocks), dim3((unsigned)threads), smem, stream, k);
+}
+
+// Blocks and rows of a backward call.
+struct BackwardShape {
+    int team, threads, teams, arrays, want;
+    long long gates;            // gates whose rows are kept apart (1 without a gate)
+    int chunks;
+    bool direct;
+    long long blocks;
+    size_t bytes;
+};
+
+BackwardShape backward_shape(const flashbev_block_norm_backward_params *p)
+{
+    BackwardShape s = {};
+    s.team = team_threads(p->C), s.threads = std::max(256, s.team), s.teams = s.threads / s.team;
+    s.gates = p->gate ? p->gate_groups : 1;
+    const long long per = p->rows / s.gates;
+    const long long resident = s.threads > 512 ? sm_count() : 2LL * sm_count();
+    // Few rows per gate, or more gates than teams: a team sums a gate's rows by itself.
+    s.direct = p->gate && (per <= 4 || s.gates >= resident * s.teams);
+    const void *const outs[5] = {p->grad_after_weight, p->grad_after_bias, p->grad_before_weight, p->grad_before_bias, p->grad_gate};
+    for (int i = 0; i < 5; ++i)
+        if (outs[i] && !(i == 4 && s.direct)) s.want |= 1 << i, ++s.arrays;
+    if (s.direct) {
+        s.chunks = 1;
+        s.blocks = std::min(resident, (s.gates + s.teams - 1) / s.teams);
+    } else {
+        s.chunks = (int)std::max(1LL, std::min(resident / s.gates, (per + s.teams - 1) / s.teams));
+        s.blocks = s.gates * s.chunks;
+    }
+    s.bytes = (size_t)s.arrays * (size_t)s.blocks * (size_t)p->C * sizeof(float);
+    return s;
+}
+
+}  // namespace
+
+extern "C" {
+
+flashbev_status flashbev_block_norm(const flashbev_block_norm_params *p, void *stream)
+{
+    const flashbev_status st = check_norm(p);
+    if (st != FLASHBEV_OK) return st;
+    if (!p->rows) {
+        t_last_launches = 0;
+        return FLASHBEV_OK;
+    }
+    NormParams k = {};
+    k.x = p->x, k.y = p->y, k.gate = p->gate, k.wa = p->after_weight, k.ba = p->after_bias, k.wb = p->before_weight, k.bb = p->before_bias;
+    k.h = p->h, k.n = p->n, k.rows = p->rows, k.per_gate = p->gate ? p->rows / p->gate_groups : p->rows;
+    k.ld_x = dense(p->ld_x, p->C), k.ld_y = dense(p->ld_y, p->C), k.ld_h = dense(p->ld_h, p->C), k.ld_n = dense(p->ld_n, p->C);
+    k.C = p->C, k.after = p->after, k.before = p->before, k.scale = (float)p->scale, k.eps = (float)p->eps, k.inv_c = 1.0f / (float)p->C;
+    k.team = team_threads(p->C);
+    bool vec = p->C % kE == 0 && whole(p->x, k.ld_x, p->dtype) && (!p->y || whole(p->y, k.ld_y, p->branch_dtype)) &&
+               (!p->h || whole(p->h, k.ld_h, p->dtype)) && (!p->n || whole(p->n, k.ld_n, p->branch_dtype));
+    vec = vec && (uintptr_t)p->gate % 16 == 0;
+    const int threads = std::max(256, k.team), teams = threads / k.team;
+    const long long blocks = std::min<long long>((p->rows + teams - 1) / teams, (long long)sm_count() * (threads > 512 ? 2 : 6));
+    const cudaError_t e = launch_norm<false>(k, p->dtype, p->branch_dtype, p->param_dtype, vec, (unsigned)blocks, threads, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess || cudaGetLastError() != cudaSuccess) {
+        cudaGetLastError();
+        return FLASHBEV_CUDA_ERROR;
+    }
+    t_last_launches = 1;
+    t_last_kernel = vec ? "block_norm" : "block_norm_scalar";
+    return FLASHBEV_OK;
+}
+
+size_t flashbev_block_norm_backward_workspace_bytes(const flashbev_block_norm_backward_params *p)
+{
+    return check_backward(p) == FLASHBEV_OK && p->rows ? backward_shape(p).bytes : 0;
+}
+
+flashbev_status flashbev_block_norm_backward(const flashbev_block_norm_backward_params *p, void *stream_)
+{
+    const flashbev_status st = check_backward(p);
+    if (st != FLASHBEV_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    void *const outs[5] = {p->grad_after_weight, p->grad_after_bias, p->grad_before_weight, p->grad_before_bias, p->grad_gate};
+    if (!p->rows) {
+        for (int i = 0; i < 5; ++i)
+            if (outs[i] && cudaMemsetAsync(outs[i], 0, (i == 4 ? p->gate_groups : 1) * p->C * elem_size(p->param_dtype), stream) != cudaSuccess) {
+                cudaGetLastError();
+                return FLASHBEV_CUDA_ERROR;
+            }
+        t_last_launches = 0;
+        return FLASHBEV_OK;
+    }
+    const BackwardShape s = backward_shape(p);
+    if (s.blocks > 2147483647LL / 256) return FLASHBEV_UNSUPPORTED;
+    if (s.bytes && (!p->workspace || p->workspace_bytes < s.bytes)) return FLASHBEV_TOO_SMALL;
+    NormParams k = {};
+    k.x = p->x, k.y = p->y, k.gate = p->gate, k.wa = p->after_weight, k.ba = p->after_bias, k.wb = p->before_weight;
+    k.gh = p->grad_h, k.gn = p->grad_n, k.gx = p->grad_x, k.gy = p->grad_y, k.ggate = p->grad_gate;
+    k.sums = static_cast<float *>(p->workspace), k.want = s.want;
+    k.rows = p->rows, k.gates = s.gates, k.per_gate = p->rows / s.gates, k.chunks = s.chunks, k.direct = s.direct;
+    k.ld_x = dense(p->ld_x, p->C), k.ld_y = dense(p->ld_y, p->C), k.ld_gh = dense(p->ld_grad_h, p->C), k.ld_gn = dense(p->ld_grad_n, p->C);
+    k.ld_gx = dense(p->ld_grad_x, p->C), k.ld_gy = dense(p->ld_grad_y, p->C);
+    k.C = p->C, k.after = p->after, k.before = p->before, k.scale = (float)p->scale, k.eps = (float)p->eps, k.inv_c = 1.0f / (float)p->C;
+    k.team = s.team;
+    bool vec = p->C % kE == 0 && whole(p->x, k.ld_x, p->dtype) && (!p->y || whole(p->y, k.ld_y, p->branch_dtype)) &&
+               (!p->grad_h || whole(p->grad_h, k.ld_gh, p->dtype)) && (!p->grad_n || whole(p->grad_n, k.ld_gn, p->branch_dtype)) &&
+               (!p->grad_x || whole(p->grad_x, k.ld_gx, p->dtype)) && (!p->grad_y || whole(p->grad_y, k.ld_gy, p->branch_dtype));
+    vec = vec && (uintptr_t)p->gate % 16 == 0 && (uintptr_t)p->grad_gate % 16 == 0;
+    cudaError_t e = launch_norm<true>(k, p->dtype, p->branch_dtype, p->param_dtype, vec, (unsigned)s.blocks, s.threads, stream);
+    int launches = 1;
+    if (e == cudaSuccess && s.arrays) {
+        SumJobs q = {};
+        const long long across = (p->C + 31) / 32;
+        long long at = 0;
+        for (int i = 0; i < 5; ++i) {
+            q.out[i] = outs[i], q.first[i] = (int)at;
+            if (s.want >> i & 1) at += across * (i == 4 ? s.gates : 1);
+        }
+        q.first[5] = (int)at, q.blocks = (int)s.blocks, q.per = s.chunks, q.C = p->C;
+        if (p->param_dtype == FLASHBEV_F32) e = launch_dependent(norm_sum_kernel<float>, dim3((unsigned)at), dim3(512), 0, stream, k.sums, q);
+        else e = launch_dependent(norm_sum_kernel<bf16>, dim3((unsigned)at), dim3(512), 0, stream, k.sums, q);
+        ++launches;
+    }
+    if (e != cudaSuccess || cudaGetLastError() != cudaSuccess) {
+        cudaGetLastError();
+        return FLASHBEV_CUDA_ERROR;
+    }
+    t_last_launches = launches;
+    t_last_kernel = vec ? "block_norm_backward" : "block_norm_backward_scalar";
+    return FLASHBEV_OK;
+}
+
+}  // extern "C"

@@ -19,6 +19,7 @@
 //
 // Geometry (projection, validity, floor, fractions) is fp64, weights and accumulation fp32.
 #include "flashbev.h"
+#include "launch.cuh"
 
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -27,10 +28,11 @@
 #include <string.h>
 
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 #include <mutex>
 #include <type_traits>
+
+using namespace flashbev_host;
 
 namespace {
 
@@ -723,8 +725,6 @@ __global__ void __launch_bounds__(256) pad_channels_kernel(const T *__restrict__
 // ------------------------------------------------------------------------------------------
 // host side
 
-thread_local int t_last_launches = 0;
-thread_local const char *t_last_kernel = "none";
 
 // The optional device word of the bounds-checked build (absent in structs of callers built against an older header).
 unsigned *debug_word(const flashbev_vt_params *p)
@@ -837,26 +837,6 @@ flashbev_status launch_per_output(const flashbev_vt_params *p, cudaStream_t stre
     return FLASHBEV_OK;
 }
 
-// Number of SMs of the current device (cached per device; 148 on a B200).
-int sm_count()
-{
-    static std::atomic<int> cached[64];  // 0: not asked yet (concurrent callers may both ask: same answer)
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
-        cudaGetLastError();
-        return 148;
-    }
-    int n = cached[dev].load(std::memory_order_relaxed);
-    if (!n) {
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) {
-            cudaGetLastError();
-            n = 148;
-        }
-        cached[dev].store(n, std::memory_order_relaxed);
-    }
-    return n;
-}
-
 // Shapes the tiled kernel serves (whatever the layout): channel rows of whole 16-byte vectors, bounded Z and map size.
 bool tiled_shape_ok(const flashbev_vt_params *p)
 {
@@ -923,21 +903,6 @@ bool padded_tiled_applicable(const flashbev_vt_params *p)
     if (p->struct_size < sizeof(flashbev_vt_params) || !p->workspace) return false;
     const size_t need = pad_copy_bytes(p);
     return need && p->workspace_bytes >= need && (uintptr_t)p->workspace % 16 == 0;
-}
-
-int use_pdl() { return getenv("FLASHBEV_NO_PDL") ? 0 : 1; }
-
-// A kernel whose CTAs may be placed while the kernel before it in the stream drains; it waits for that one's end itself.
-template <typename... P, typename... A>
-cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const A &...args)
-{
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid, cfg.blockDim = block, cfg.dynamicSmemBytes = smem, cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    if (use_pdl()) cfg.attrs = attr, cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
 
 template <int V, bool BF16, int WARPS, bool BWD, bool WIDE = false, bool PLANAR = false, bool LEVEL = false>

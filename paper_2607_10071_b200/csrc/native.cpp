@@ -408,11 +408,327 @@ PyObject *py_sca(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- operators of a transformer layer ---------------------------------------------------------------------------------------
+
+int32_t row_dtype(const at::Tensor &t, const char *what)
+{
+    if (t.scalar_type() == at::kFloat) return FLASHBEV_F32;
+    if (t.scalar_type() == at::kBFloat16) return FLASHBEV_BF16;
+    PyErr_Format(PyExc_ValueError, "%s must be float32 or bfloat16", what);
+    throw Bad();
+}
+
+at::ScalarType scalar_type(int32_t dtype)
+{
+    if (dtype == FLASHBEV_F32) return at::kFloat;
+    if (dtype == FLASHBEV_BF16) return at::kBFloat16;
+    value_error("a number type is F32 or BF16");
+}
+
+// A tensor [..., width] as rows: their number and their distance in elements.
+struct Rows {
+    int64_t rows, width, ld;
+};
+
+Rows rows_of(const at::Tensor &t, const char *what)
+{
+    if (t.dim() < 1) {
+        PyErr_Format(PyExc_ValueError, "%s must have at least one dimension", what);
+        throw Bad();
+    }
+    Rows r = {1, t.size(-1), 0};
+    bool ok = r.width <= 1 || t.stride(-1) == 1;
+    for (int64_t d = t.dim() - 2; d >= 0; --d) {
+        const int64_t n = t.size(d);
+        if (n != 1 && t.numel()) {
+            if (r.rows == 1) r.ld = t.stride(d);
+            else ok = ok && t.stride(d) == r.rows * r.ld;
+        }
+        r.rows *= n;
+    }
+    if (r.rows <= 1 || !t.numel()) r.ld = r.width;
+    if (!ok || r.ld < r.width) {
+        PyErr_Format(PyExc_ValueError, "%s must have contiguous rows, all the same distance apart", what);
+        throw Bad();
+    }
+    return r;
+}
+
+// An argument that has to be a tensor of this number type on the device of `like`; None is allowed where `optional`.
+const at::Tensor *argument(PyObject *o, const at::Tensor &like, int32_t dtype, bool optional, const char *what)
+{
+    if (optional && o == Py_None) return nullptr;
+    const at::Tensor &t = tensor(o, what);
+    if (!t.is_cuda() || t.device() != like.device()) {
+        PyErr_Format(PyExc_ValueError, "%s must be a CUDA tensor on the device of the others", what);
+        throw Bad();
+    }
+    if (row_dtype(t, what) != dtype) {
+        PyErr_Format(PyExc_ValueError, "%s must be %s", what, dtype == FLASHBEV_F32 ? "float32" : "bfloat16");
+        throw Bad();
+    }
+    return &t;
+}
+
+// ... of `rows` rows of `width`; returns their distance
+int64_t matrix(const at::Tensor *t, int64_t rows, int64_t width, const char *what)
+{
+    if (!t) return 0;
+    const Rows r = rows_of(*t, what);
+    if (r.rows != rows || r.width != width) {
+        PyErr_Format(PyExc_ValueError, "%s must have %lld rows of %lld, not %lld of %lld", what, (long long)rows, (long long)width, (long long)r.rows,
+                     (long long)r.width);
+        throw Bad();
+    }
+    return r.ld;
+}
+
+void vector(const at::Tensor *t, int64_t width, const char *what)
+{
+    if (!t || (t->dim() == 1 && t->size(0) == width && t->is_contiguous())) return;
+    PyErr_Format(PyExc_ValueError, "%s must be a contiguous vector of %lld", what, (long long)width);
+    throw Bad();
+}
+
+const void *address(const at::Tensor *t) { return t ? t->data_ptr() : nullptr; }
+
+at::Tensor rows_like(const at::Tensor &t, int64_t width, int32_t dtype)
+{
+    std::vector<int64_t> shape(t.sizes().begin(), t.sizes().end());
+    shape.back() = width;
+    return at::empty(shape, at::TensorOptions().dtype(scalar_type(dtype)).device(t.device()));
+}
+
+bool truth(PyObject *o)
+{
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw Bad();
+    return v;
+}
+
+// Results of a call, None for the ones that were not asked for.
+PyObject *tuple(std::initializer_list<at::Tensor> ts)
+{
+    PyObject *t = PyTuple_New((Py_ssize_t)ts.size());
+    if (!t) throw Bad();
+    Py_ssize_t i = 0;
+    for (const at::Tensor &v : ts) {
+        PyObject *o = v.defined() ? THPVariable_Wrap(v) : (Py_INCREF(Py_None), Py_None);
+        if (!o) {
+            Py_DECREF(t);
+            throw Bad();
+        }
+        PyTuple_SET_ITEM(t, i++, o);
+    }
+    return t;
+}
+
+const at::Tensor &rows_argument(PyObject *o, const char *what)
+{
+    const at::Tensor &t = tensor(o, what);
+    if (!t.is_cuda()) {
+        PyErr_Format(PyExc_ValueError, "%s must be a CUDA tensor; there is no CPU path", what);
+        throw Bad();
+    }
+    return t;
+}
+
+// x, weight, bias, act, residual, out, out_dtype, preact, stream
+PyObject *py_linear(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        need_args(n, 9);
+        const at::Tensor &x = rows_argument(a[0], "x");
+        flashbev_linear_params p = {};
+        p.struct_size = sizeof(p);
+        p.dtype = row_dtype(x, "x");
+        const at::Tensor &w = *argument(a[1], x, p.dtype, false, "weight");
+        if (w.dim() != 2) value_error("weight must have two dimensions");
+        const Rows r = rows_of(x, "x");
+        p.rows = r.rows, p.ld_x = r.ld, p.in_features = narrow(r.width), p.out_features = narrow(w.size(0));
+        p.ld_weight = matrix(&w, w.size(0), r.width, "weight");
+        const at::Tensor *const bias = argument(a[2], x, p.dtype, true, "bias");
+        vector(bias, p.out_features, "bias");
+        p.act = integer32(a[3]);
+        at::Tensor out, scratch;
+        if (a[5] != Py_None) out = tensor(a[5], "out");
+        p.out_dtype = a[6] != Py_None ? integer32(a[6]) : (out.defined() ? row_dtype(out, "out") : p.dtype);
+        scalar_type(p.out_dtype);
+        if (out.defined()) p.ld_out = matrix(argument(a[5], x, p.out_dtype, false, "out"), p.rows, p.out_features, "out");
+        const at::Tensor *const residual = argument(a[4], x, p.out_dtype, true, "residual"), *const pre = argument(a[7], x, p.dtype, true, "preact");
+        p.ld_residual = matrix(residual, p.rows, p.out_features, "residual");
+        p.ld_preact = matrix(pre, p.rows, p.out_features, "preact");
+        const StreamArg stream(a[8]);
+        const flashbev_status st = unlocked([&] {
+            const Place place(x, stream);
+            if (!out.defined()) out = place.result(rows_like(x, p.out_features, p.out_dtype));
+            p.x = x.data_ptr(), p.weight = w.data_ptr(), p.bias = address(bias), p.residual = address(residual);
+            p.out = out.data_ptr(), p.preact_out = const_cast<void *>(address(pre));
+            if (const size_t need = flashbev_linear_workspace_bytes(&p)) {
+                scratch = empty({(int64_t)need}, at::kByte, x);
+                p.workspace = scratch.data_ptr(), p.workspace_bytes = need;
+            }
+            return flashbev_linear(&p, place.stream());
+        });
+        return st == FLASHBEV_OK ? THPVariable_Wrap(std::move(out)) : status(st);
+    });
+}
+
+// grad_out, x, weight, act, preact, grad_x, grad_weight, grad_bias (whether each is wanted), stream
+PyObject *py_linear_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        need_args(n, 9);
+        const at::Tensor &x = rows_argument(a[1], "x");
+        flashbev_linear_backward_params p = {};
+        p.struct_size = sizeof(p);
+        p.dtype = row_dtype(x, "x");
+        const at::Tensor &w = *argument(a[2], x, p.dtype, false, "weight");
+        if (w.dim() != 2) value_error("weight must have two dimensions");
+        const Rows r = rows_of(x, "x");
+        p.rows = r.rows, p.ld_x = r.ld, p.in_features = narrow(r.width), p.out_features = narrow(w.size(0));
+        p.ld_weight = matrix(&w, w.size(0), r.width, "weight");
+        p.grad_dtype = row_dtype(tensor(a[0], "grad_out"), "grad_out");
+        const at::Tensor &g = *argument(a[0], x, p.grad_dtype, false, "grad_out");
+        p.ld_grad_out = matrix(&g, p.rows, p.out_features, "grad_out");
+        p.act = integer32(a[3]);
+        const at::Tensor *const pre = argument(a[4], x, p.dtype, true, "preact");
+        p.ld_preact = matrix(pre, p.rows, p.out_features, "preact");
+        const bool want_x = truth(a[5]), want_w = truth(a[6]), want_b = truth(a[7]);
+        const StreamArg stream(a[8]);
+        at::Tensor gx, gw, gb, scratch;
+        const flashbev_status st = unlocked([&] {
+            const Place place(x, stream);
+            if (want_x) gx = place.result(rows_like(x, p.in_features, p.dtype)), p.grad_x = gx.data_ptr();
+            if (want_w) gw = place.result(rows_like(w, p.in_features, p.dtype)), p.grad_weight = gw.data_ptr();
+            if (want_b) gb = place.result(empty({p.out_features}, x.scalar_type(), x)), p.grad_bias = gb.data_ptr();
+            p.grad_out = g.data_ptr(), p.x = x.data_ptr(), p.weight = w.data_ptr(), p.preact = address(pre);
+            if (const size_t need = flashbev_linear_backward_workspace_bytes(&p)) {
+                scratch = empty({(int64_t)need}, at::kByte, x);
+                p.workspace = scratch.data_ptr(), p.workspace_bytes = need;
+            }
+            return flashbev_linear_backward(&p, place.stream());
+        });
+        return st == FLASHBEV_OK ? tuple({gx, gw, gb}) : status(st);
+    });
+}
+
+// What the forward and the backward call of the norms have in common: x, y, gate, scale, after and its parameters, before and its
+// parameters, eps.
+struct NormArguments {
+    const at::Tensor *x, *y, *gate, *after_weight, *after_bias, *before_weight, *before_bias;
+
+    template <typename P>
+    NormArguments(P &p, PyObject *const *a)
+    {
+        p.struct_size = sizeof(p);
+        x = &rows_argument(a[0], "x");
+        p.dtype = row_dtype(*x, "x");
+        const Rows r = rows_of(*x, "x");
+        p.rows = r.rows, p.C = narrow(r.width), p.ld_x = r.ld;
+        p.branch_dtype = a[1] != Py_None ? row_dtype(tensor(a[1], "y"), "y") : p.dtype;
+        y = argument(a[1], *x, p.branch_dtype, true, "y");
+        p.ld_y = matrix(y, p.rows, p.C, "y");
+        p.param_dtype = FLASHBEV_F32;
+        for (const int i : {2, 5, 6, 8, 9})
+            if (a[i] != Py_None) {
+                p.param_dtype = row_dtype(tensor(a[i], "a parameter"), "a parameter");
+                break;
+            }
+        gate = argument(a[2], *x, p.param_dtype, true, "gate");
+        if (gate) {
+            if (gate->dim() < 1 || gate->size(-1) != p.C || !gate->is_contiguous()) value_error("gate must be contiguous, [C] or [gates, C]");
+            p.gate_groups = p.C ? gate->numel() / p.C : 0;
+            if (!p.rows && !p.gate_groups) p.gate_groups = 1;
+        }
+        p.scale = real(a[3]);
+        p.after = integer32(a[4]), p.before = integer32(a[7]);
+        after_weight = argument(a[5], *x, p.param_dtype, true, "after_weight");
+        after_bias = argument(a[6], *x, p.param_dtype, true, "after_bias");
+        before_weight = argument(a[8], *x, p.param_dtype, true, "before_weight");
+        before_bias = argument(a[9], *x, p.param_dtype, true, "before_bias");
+        vector(after_weight, p.C, "after_weight"), vector(after_bias, p.C, "after_bias");
+        vector(before_weight, p.C, "before_weight"), vector(before_bias, p.C, "before_bias");
+        p.eps = real(a[10]);
+    }
+
+    template <typename P>
+    void addresses(P &p) const
+    {
+        p.x = x->data_ptr(), p.y = address(y), p.gate = address(gate);
+        p.after_weight = address(after_weight), p.after_bias = address(after_bias), p.before_weight = address(before_weight);
+    }
+};
+
+// x, y, gate, scale, after, after_weight, after_bias, before, before_weight, before_bias, eps, h, n, keep_h, stream
+PyObject *py_block_norm(PyObject *, PyObject *const *a, Py_ssize_t count)
+{
+    return guarded([&]() -> PyObject * {
+        need_args(count, 15);
+        flashbev_block_norm_params p = {};
+        const NormArguments in(p, a);
+        at::Tensor h, n;
+        if (a[12] != Py_None && !in.y) p.branch_dtype = row_dtype(tensor(a[12], "n"), "n");
+        if (a[11] != Py_None) h = *argument(a[11], *in.x, p.dtype, false, "h"), p.ld_h = matrix(&h, p.rows, p.C, "h");
+        if (a[12] != Py_None) n = *argument(a[12], *in.x, p.branch_dtype, false, "n"), p.ld_n = matrix(&n, p.rows, p.C, "n");
+        const bool keep = truth(a[13]) && in.y && !h.defined(), norm = p.before != FLASHBEV_NORM_NONE && !n.defined();
+        const StreamArg stream(a[14]);
+        const flashbev_status st = unlocked([&] {
+            const Place place(*in.x, stream);
+            if (keep) h = place.result(rows_like(*in.x, p.C, p.dtype));
+            if (norm) n = place.result(rows_like(*in.x, p.C, p.branch_dtype));
+            in.addresses(p);
+            p.before_bias = address(in.before_bias);
+            p.h = h.defined() ? h.data_ptr() : nullptr, p.n = n.defined() ? n.data_ptr() : nullptr;
+            return flashbev_block_norm(&p, place.stream());
+        });
+        return st == FLASHBEV_OK ? tuple({h, n}) : status(st);
+    });
+}
+
+// x, y, gate, scale, after, after_weight, after_bias, before, before_weight, before_bias, eps, grad_h, grad_n, stream
+PyObject *py_block_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t count)
+{
+    return guarded([&]() -> PyObject * {
+        need_args(count, 14);
+        flashbev_block_norm_backward_params p = {};
+        const NormArguments in(p, a);
+        if (a[12] != Py_None && !in.y) p.branch_dtype = row_dtype(tensor(a[12], "grad_n"), "grad_n");
+        const at::Tensor *const gh = argument(a[11], *in.x, p.dtype, true, "grad_h"), *const gn = argument(a[12], *in.x, p.branch_dtype, true, "grad_n");
+        p.ld_grad_h = matrix(gh, p.rows, p.C, "grad_h"), p.ld_grad_n = matrix(gn, p.rows, p.C, "grad_n");
+        const StreamArg stream(a[13]);
+        at::Tensor gx, gy, ggate, gaw, gab, gbw, gbb, scratch;
+        const flashbev_status st = unlocked([&] {
+            const Place place(*in.x, stream);
+            const auto like = [&](const at::Tensor *t, at::Tensor &g) -> void * {
+                if (!t) return nullptr;
+                g = place.result(at::empty(t->sizes(), at::TensorOptions().dtype(t->dtype()).device(t->device())));
+                return g.data_ptr();
+            };
+            p.grad_x = like(in.x, gx), p.grad_y = like(in.y, gy), p.grad_gate = like(in.gate, ggate);
+            p.grad_after_weight = like(in.after_weight, gaw), p.grad_after_bias = like(in.after_bias, gab);
+            p.grad_before_weight = like(in.before_weight, gbw), p.grad_before_bias = like(in.before_bias, gbb);
+            in.addresses(p);
+            p.grad_h = address(gh), p.grad_n = address(gn);
+            if (const size_t need = flashbev_block_norm_backward_workspace_bytes(&p)) {
+                scratch = empty({(int64_t)need}, at::kByte, *in.x);
+                p.workspace = scratch.data_ptr(), p.workspace_bytes = need;
+            }
+            return flashbev_block_norm_backward(&p, place.stream());
+        });
+        return st == FLASHBEV_OK ? tuple({gx, gy, ggate, gaw, gab, gbw, gbb}) : status(st);
+    });
+}
+
 PyMethodDef methods[] = {
     {"sampling_vt", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_sampling_vt)), METH_FASTCALL, nullptr},
     {"sampling_vt_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_sampling_vt_backward)), METH_FASTCALL, nullptr},
     {"sampling_vt_multires", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_sampling_vt_multires)), METH_FASTCALL, nullptr},
     {"sca", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_sca)), METH_FASTCALL, nullptr},
+    {"linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_linear)), METH_FASTCALL, nullptr},
+    {"linear_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_linear_backward)), METH_FASTCALL, nullptr},
+    {"block_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_block_norm)), METH_FASTCALL, nullptr},
+    {"block_norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(py_block_norm_backward)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

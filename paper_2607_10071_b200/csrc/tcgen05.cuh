@@ -1,0 +1,140 @@
+// The Blackwell instructions that the matrix products use: mbarriers with bounded waits, tiled TMA loads, tensor memory and
+// tcgen05.mma, and the descriptors of shared-memory tiles with 128-byte swizzle.
+#ifndef FLASHBEV_TCGEN05_CUH_
+#define FLASHBEV_TCGEN05_CUH_
+
+#include <cuda.h>
+#include <stdint.h>
+
+namespace flashbev_sm100 {
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+// ---- mbarriers ------------------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+
+__device__ __forceinline__ void mbar_arrive(uint32_t bar)
+{
+    asm volatile("{ .reg .b64 s; mbarrier.arrive.shared::cta.b64 s, [%0]; }" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("{ .reg .b64 s; mbarrier.arrive.expect_tx.shared::cta.b64 s, [%0], %1; }" ::"r"(bar), "r"(bytes) : "memory");
+}
+
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                 : "=r"(ok)
+                 : "r"(bar), "r"(parity)
+                 : "memory");
+    return ok != 0;
+}
+
+// Every wait ends: after about two seconds of clock it raises the CTA's failure flag and gives up, and so does every other wait
+// of the CTA that sees the flag.
+constexpr long long kWaitCycles = 4000000000LL;
+
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int *failed, long long limit = kWaitCycles)
+{
+    if (mbar_try(bar, parity)) return true;
+    const long long since = clock64();
+    while (!mbar_try(bar, parity)) {
+        if (*failed) return false;
+        if (clock64() - since > limit) {
+            *failed = 1;
+            return false;
+        }
+    }
+    return true;
+}
+
+// The wait of a CTA that has already failed, for what it still has in flight.
+__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity)
+{
+    const long long since = clock64();
+    while (!mbar_try(bar, parity) && clock64() - since < kWaitCycles / 8) {}
+}
+
+// ---- TMA ------------------------------------------------------------------------------------------------------------------
+
+// x: innermost coordinate, a multiple of 16 bytes' worth of elements.
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+}
+
+// ---- tensor memory and products -------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void tmem_alloc(uint32_t slot, uint32_t columns)  // by one whole warp
+{
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+
+__device__ __forceinline__ void tmem_free(uint32_t addr, uint32_t columns)  // by the same warp
+{
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(columns));
+}
+
+__device__ __forceinline__ void tcgen05_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tcgen05_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// D[128 x N] (+)= A[128 x 16] B[N x 16]^T, bf16 operands in shared memory, fp32 sums in tensor memory; by one thread.
+__device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate)
+{
+    asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a),
+                 "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+                 : "memory");
+}
+
+// The barrier completes when every product that this thread has issued is done.
+__device__ __forceinline__ void mma_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// Instruction descriptor: fp32 sums, bf16 operands, `a_mn` / `b_mn`: the operand's tile is contiguous along M / N instead of K.
+__host__ __device__ constexpr uint32_t mma_idesc(int n, bool a_mn, bool b_mn)
+{
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) |
+           ((128u >> 4) << 24);
+}
+
+// Shared-memory descriptor of a tile of 128-byte rows with 128-byte swizzle, its base a multiple of 1024 bytes.  K-major: a row of
+// the operand is 64 elements of K, eight rows are 1024 bytes apart.  MN-major: a row is 64 elements along M or N at one k, eight k
+// are 1024 bytes apart, the next 64 along M or N `block` bytes.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn, uint32_t block)
+{
+    const uint64_t lead = mn ? (uint64_t)(block >> 4) : 1;
+    return (uint64_t)((addr & 0x3ffff) >> 4) | (lead << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
+// 32 columns of the warp's 32 lanes of tensor memory (a warp reaches the lanes 32 (warp % 4) and up).
+__device__ __forceinline__ void tmem_load32(float (&v)[32], uint32_t addr)
+{
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, "
+        "%19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+}  // namespace flashbev_sm100
+
+#endif  // FLASHBEV_TCGEN05_CUH_
