@@ -28,16 +28,13 @@ namespace {
 using bf16 = __nv_bfloat16;
 
 constexpr int kBM = 128;            // rows of a tile: the 128 lanes of tensor memory
-constexpr int kBK = 64;             // K of a stage: one swizzled 128-byte row of bf16
-constexpr int kEpilogueWarps = 8;   // two per 32 lanes of tensor memory
-constexpr int kProducerWarps = 8;   // of the loaders without TMA
-constexpr int kRing = 192 * 1024;   // bytes of the operand stages
-constexpr int kSmem = 1024 + kRing + kEpilogueWarps * 4096 + 1024;  // alignment, stages, staging of the epilogue, barriers and bias
+constexpr int kProducerWarps = 8;   // of the loaders without TMA: two groups of them, for every other stage
+constexpr int kSmemLimit = 227 * 1024 - 512;
 
 // How a stage is filled.
 enum Loader {
     kTma = 0,     // bf16, 16-byte aligned rows: TMA
-    kCopy = 1,    // bf16 rows of any alignment: loads and shared-memory stores by eight warps
+    kCopy = 1,    // bf16 rows of any alignment: loads and shared-memory stores by 16 warps
     kSplit = 2    // float32: the same warps take every number apart into three bf16 pieces
 };
 
@@ -66,36 +63,90 @@ __device__ __forceinline__ T from_float(float v)
 
 // ---- activations ------------------------------------------------------------------------------------------------------------
 
-// Phi(z) = erfc(-z / sqrt 2) / 2.  Results that are rounded to bf16 take erfc from Abramowitz and Stegun, Handbook of Mathematical
-// Functions, 7.1.26 (within 1.5e-7; for z < 0 without a difference): 14 instructions instead of about 30, and the epilogue of a short sum is as long
-// as its memory traffic.
+__device__ __forceinline__ float exp2_approx(float v)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+__device__ __forceinline__ float rcp_approx(float v)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// Phi(z) = erfc(-z / sqrt 2) / 2 (the standard normal distribution).  Results that are rounded to bf16 take Phi(-|z|) from Abramowitz and
+// Stegun, Handbook of Mathematical Functions, 7.1.26 (erfc within 1.5e-7): s = Phi(-|z|) = t (a1 + t (a2 + ...)) exp(-z^2 / 2) / 2 with t = 1 / (1 +
+// p |z| / sqrt 2), nine instructions a number in pairs instead of about 30: the epilogue of a short sum is as long as its memory traffic.
+__device__ __forceinline__ float2 normal_tail(float2 a, float2 z)  // a = |z|
+{
+    float2 t = __ffma2_rn(a, both(0.3275911f * 0.70710678f), both(1.0f));
+    float2 e = __fmul2_rn(__fmul2_rn(z, z), both(-0.5f * 1.44269504f));
+    t.x = rcp_approx(t.x), t.y = rcp_approx(t.y);
+    e.x = exp2_approx(e.x), e.y = exp2_approx(e.y);
+    float2 s = __ffma2_rn(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
+    s = __ffma2_rn(s, t, both(0.5f * 1.421413741f));
+    s = __ffma2_rn(s, t, both(0.5f * -0.284496736f));
+    s = __ffma2_rn(s, t, both(0.5f * 0.254829592f));
+    return __fmul2_rn(__fmul2_rn(s, t), e);
+}
+
 template <bool FAST>
 __device__ __forceinline__ float normal_cdf(float z)
 {
     if constexpr (!FAST) return 0.5f * erfcf(-0.70710678f * z);
-    const float a = fabsf(z) * 0.70710678f;
-    const float t = __fdividef(1.0f, fmaf(0.3275911f, a, 1.0f));
-    float s = fmaf(1.061405429f, t, -1.453152027f);
-    s = fmaf(s, t, 1.421413741f);
-    s = fmaf(s, t, -0.284496736f);
-    s = fmaf(s, t, 0.254829592f);
-    s = 0.5f * s * t * __expf(-a * a);
+    const float s = normal_tail(both(fabsf(z)), both(z)).x;
     return z < 0.0f ? s : 1.0f - s;
 }
 
 template <bool FAST>
 __device__ __forceinline__ float sigmoid(float z)
 {
-    return FAST ? __fdividef(1.0f, 1.0f + __expf(-z)) : 1.0f / (1.0f + expf(-z));
+    return FAST ? rcp_approx(1.0f + exp2_approx(-1.44269504f * z)) : 1.0f / (1.0f + expf(-z));
 }
 
+// Two numbers at a time.  GELU as max(z, 0) - |z| Phi(-|z|): no difference of near numbers on either side, and no infinity times zero.
 template <bool FAST, int ACT>
-__device__ __forceinline__ float activate(float z)
+__device__ __forceinline__ float2 activate(float2 z)
 {
-    if (ACT == FLASHBEV_ACT_RELU) return z < 0.0f ? 0.0f : z;  // (NaN stays)
-    if (ACT == FLASHBEV_ACT_GELU) return z * normal_cdf<FAST>(z);
-    if (ACT == FLASHBEV_ACT_SILU) return z * sigmoid<FAST>(z);
+    if (ACT == FLASHBEV_ACT_RELU) return make_float2(max_nan(z.x, 0.0f), max_nan(z.y, 0.0f));
+    if (ACT == FLASHBEV_ACT_GELU) {
+        if constexpr (!FAST) return make_float2(z.x * normal_cdf<false>(z.x), z.y * normal_cdf<false>(z.y));
+        const float2 a = make_float2(fminf(fabsf(z.x), 3.0e38f), fminf(fabsf(z.y), 3.0e38f));
+        const float2 s = normal_tail(a, z), m = make_float2(max_nan(z.x, 0.0f), max_nan(z.y, 0.0f));
+        return __ffma2_rn(make_float2(-a.x, -a.y), s, m);
+    }
+    if (ACT == FLASHBEV_ACT_SILU) return __fmul2_rn(z, make_float2(sigmoid<FAST>(z.x), sigmoid<FAST>(z.y)));
     return z;
+}
+
+template <bool FAST, int ACT, int N>
+__device__ __forceinline__ void activate(float (&v)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+        const float2 q = activate<FAST, ACT>(make_float2(v[i], v[i + 1]));
+        v[i] = q.x, v[i + 1] = q.y;
+    }
+}
+
+template <bool FAST, int N>
+__device__ __forceinline__ void activate_all(float (&v)[N], int act)
+{
+    if (act == FLASHBEV_ACT_RELU) activate<FAST, FLASHBEV_ACT_RELU>(v);
+    else if (act == FLASHBEV_ACT_GELU) activate<FAST, FLASHBEV_ACT_GELU>(v);
+    else if (act == FLASHBEV_ACT_SILU) activate<FAST, FLASHBEV_ACT_SILU>(v);
 }
 
 // g act'(z)
@@ -116,15 +167,36 @@ __device__ __forceinline__ float slope_times(float g, float z, int act)
 
 // ---- the product ------------------------------------------------------------------------------------------------------------
 
+// K of a stage: a swizzled row of 64 bf16 numbers, of pieces 32 (three tiles per operand, and a stage's numbers fit a thread's registers).
+__host__ __device__ constexpr int block_k(int loader) { return loader == kSplit ? 32 : 64; }
+// Warps of the epilogue: with TMA loads 16, as it is their latency that a short sum waits for (64-column sums of 184950 rows, 64 columns:
+// 25 us with eight).  The other loaders leave four, and have 16 to bring the stages.  (Registers are those of a quarter of an SM: the last warps of
+// four, which do nothing, cost none.)
+__host__ __device__ constexpr int epilogue_warps(int loader) { return loader == kTma ? 16 : 4; }
+__host__ __device__ constexpr int gemm_threads(int loader) { return 32 * (loader == kTma ? 20 : 8 + 2 * kProducerWarps); }
+// Registers of the warps without TMA: 768 threads x 80 = 128 x 152 (epilogue) + 128 x 40 (products) + 512 x 72
+constexpr int kEpilogueRegs = 152, kProductRegs = 40, kProducerRegs = 72;
+static_assert(128 * kEpilogueRegs + 128 * kProductRegs + 64 * kProducerWarps * kProducerRegs <= 32 * (8 + 2 * kProducerWarps) * 80, "");
+// Bytes behind the ring: a buffer of 32 rows x 128 bytes and a bias of 64 columns per epilogue warp.
+__host__ __device__ constexpr int epilogue_bytes(int loader) { return epilogue_warps(loader) * (4096 + 256); }
+__host__ __device__ constexpr int ring_bytes(int loader) { return (kSmemLimit - 1024 - epilogue_bytes(loader)) / 1024 * 1024; }
+constexpr int kAccs = 4;            // most accumulators in tensor memory
+
 struct alignas(64) GemmParams {
     CUtensorMap ta, tb;         // kTma
+    CUtensorMap tout, tpre;     // store_tma
     const void *a, *b;          // the other loaders
     long long lda, ldb;
     int a_mn, b_mn;             // the operand's rows run along M / N, one per k
     int a_vec, b_vec;           // bytes that every row's start is a multiple of: 16, 4 or less
     int M, N, K;
     int bn, stages;             // columns of a tile; stages in the ring
-    int tiles_n, tiles, kblocks, kshare, splits;  // a tile's sum is cut into `splits` of `kshare` blocks of 64 (the last may have fewer)
+    int tiles_n, tiles, kblocks, kshare, splits;  // a tile's sum is cut into `splits` of `kshare` blocks of K (the last may have fewer)
+    int run;                    // blocks that are summed in tensor memory before the sum is taken on in registers; kshare or more: never
+    int columns;                // of tensor memory
+    int accs;                   // accumulators in it
+    int groups;                 // of epilogue warps, which take accumulators in turn
+    int store_tma;              // the results leave through TMA stores
     void *out, *pre;            // pre: z, or NULL
     const void *residual, *bias;
     long long ld_out, ld_pre, ld_res;
@@ -135,25 +207,27 @@ struct alignas(64) GemmParams {
     uint32_t *error_word;
 };
 
-// A chunk of 32 rows x 32 columns between tensor memory's layout (a lane has a row) and global memory's (16 bytes of a row per lane,
-// whole rows side by side), through 4 KB of the warp's own shared memory.  16-byte pieces are swizzled so that neither side has bank
+// A tile of the epilogue is 32 rows x 32 columns of a result: rows of eight (float32) or four pieces of 16 bytes, swizzled as TMA has
+// them.  In tensor memory's layout a lane has a row; in global memory's neighbouring lanes have a row's pieces.  Neither side has bank
 // conflicts.
 template <typename T>
-struct Chunk {
-    static constexpr int E = 16 / (int)sizeof(T);  // elements of 16 bytes
-    static constexpr int P = 32 / E;               // pieces of a row: 8 (float32) or 4
-    static constexpr int R = 32 / P;               // rows of one warp access
-    static __device__ __forceinline__ uint32_t at(int row, int piece)
-    {
-        return P == 8 ? row * 128 + ((piece ^ (row & 7)) << 4) : row * 64 + ((piece ^ ((row >> 1) & 3)) << 4);
-    }
-};
+constexpr int kPiece = 16 / (int)sizeof(T);  // elements of a piece
+template <typename T>
+constexpr int kPieces32 = 32 / kPiece<T>;    // pieces of a row; also the warp's accesses to the tile
+template <typename T>
+constexpr int kRows32 = 32 / kPieces32<T>;   // rows of an access
 
 template <typename T>
-__device__ __forceinline__ uint4 load_piece(const T *p, int have, bool vec)
+__device__ __forceinline__ int piece_at(int row, int piece)
 {
-    constexpr int E = Chunk<T>::E;
-    if (vec && have >= E) return *reinterpret_cast<const uint4 *>(p);
+    return kPieces32<T> == 8 ? row * 128 + ((piece ^ (row & 7)) << 4) : row * 64 + ((piece ^ (row >> 1 & 3)) << 4);
+}
+
+template <typename T>
+__device__ __forceinline__ uint4 load_piece(const T *p, int have)
+{
+    constexpr int E = kPiece<T>;
+    if (have >= E) return *reinterpret_cast<const uint4 *>(p);
     T v[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] = i < have ? p[i] : from_float<T>(0.0f);
@@ -163,10 +237,10 @@ __device__ __forceinline__ uint4 load_piece(const T *p, int have, bool vec)
 }
 
 template <typename T>
-__device__ __forceinline__ void store_piece(T *p, uint4 r, int have, bool vec)
+__device__ __forceinline__ void store_piece(T *p, uint4 r, int have)
 {
-    constexpr int E = Chunk<T>::E;
-    if (vec && have >= E) {
+    constexpr int E = kPiece<T>;
+    if (have >= E) {
         *reinterpret_cast<uint4 *>(p) = r;
         return;
     }
@@ -178,138 +252,184 @@ __device__ __forceinline__ void store_piece(T *p, uint4 r, int have, bool vec)
 }
 
 template <typename T>
-__device__ __forceinline__ void chunk_load(uint4 (&r)[Chunk<T>::P], const T *base, long long ld, int row0, int col0, int M, int N, bool vec,
-                                           int lane)
+__device__ __forceinline__ uint4 piece_of(const float *v)
 {
-    using C = Chunk<T>;
-    const int col = col0 + lane % C::P * C::E;
-#pragma unroll
-    for (int i = 0; i < C::P; ++i) {
-        const int row = row0 + i * C::R + lane / C::P;
-        if (row < M && col < N) r[i] = load_piece(base + row * ld + col, N - col, vec);
-    }
+    if constexpr (sizeof(T) == 4)
+        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    else
+        return make_uint4(pack(v[0], v[1]), pack(v[2], v[3]), pack(v[4], v[5]), pack(v[6], v[7]));
 }
 
-// Adds the chunk that `chunk_load` brought to the lane's row.
+// The lane's row into a tile
 template <typename T>
-__device__ __forceinline__ void chunk_add(float (&v)[32], const uint4 (&r)[Chunk<T>::P], unsigned char *stage, int lane)
+__device__ __forceinline__ void row_store(const float (&v)[32], unsigned char *tile, int lane)
 {
-    using C = Chunk<T>;
 #pragma unroll
-    for (int i = 0; i < C::P; ++i) *reinterpret_cast<uint4 *>(stage + C::at(i * C::R + lane / C::P, lane % C::P)) = r[i];
-    __syncwarp();
+    for (int c = 0; c < kPieces32<T>; ++c) *reinterpret_cast<uint4 *>(tile + piece_at<T>(lane, c)) = piece_of<T>(v + kPiece<T> * c);
+}
+
+// ... and added to from one
+template <typename T>
+__device__ __forceinline__ void row_add(float (&v)[32], const unsigned char *tile, int lane)
+{
 #pragma unroll
-    for (int c = 0; c < C::P; ++c) {
-        const uint4 q = *reinterpret_cast<const uint4 *>(stage + C::at(lane, c));
+    for (int c = 0; c < kPieces32<T>; ++c) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(tile + piece_at<T>(lane, c));
         const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if constexpr (C::E == 4) v[4 * c + j] += __uint_as_float(w[j]);
+            if constexpr (kPiece<T> == 4) v[4 * c + j] += __uint_as_float(w[j]);
             else v[8 * c + 2 * j] += low(w[j]), v[8 * c + 2 * j + 1] += high(w[j]);
         }
     }
-    __syncwarp();
+}
+
+// A tile from a matrix to registers, and from there to shared memory.  Rows of any alignment (`vec` false): a lane has a column, so that the warp
+// touches every sector of a row once; 16 rows in a register per 8 of them with 16-byte pieces.
+template <typename T>
+__device__ __forceinline__ void tile_load(uint4 (&r)[kPieces32<T>], const T *base, long long ld, bool vec, int row0, int col0, int M, int N, int lane)
+{
+    if (vec) {
+        const int row = row0 + lane / kPieces32<T>, col = col0 + lane % kPieces32<T> * kPiece<T>;
+        const T *p = base + row * ld + col;
+#pragma unroll
+        for (int i = 0; i < kPieces32<T>; ++i, p += kRows32<T> * ld)
+            if (row + kRows32<T> * i < M && col < N) r[i] = load_piece(p, N - col);
+    } else {
+        const T *p = base + row0 * ld + col0 + lane;
+        T v[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i, p += ld) v[i] = row0 + i < M && col0 + lane < N ? *p : from_float<T>(0.0f);
+        memcpy(r, v, sizeof(v));
+    }
 }
 
 template <typename T>
-__device__ __forceinline__ void chunk_store(const float (&v)[32], T *base, long long ld, int row0, int col0, int M, int N, bool vec,
-                                            unsigned char *stage, int lane)
+__device__ __forceinline__ void tile_stage(const uint4 (&r)[kPieces32<T>], bool vec, unsigned char *tile, int lane)
 {
-    using C = Chunk<T>;
+    if (vec) {
 #pragma unroll
-    for (int c = 0; c < C::P; ++c) {
-        uint4 q;
-        if constexpr (C::E == 4)
-            q = make_uint4(__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]), __float_as_uint(v[4 * c + 2]), __float_as_uint(v[4 * c + 3]));
-        else
-            q = make_uint4(pack(v[8 * c], v[8 * c + 1]), pack(v[8 * c + 2], v[8 * c + 3]), pack(v[8 * c + 4], v[8 * c + 5]),
-                           pack(v[8 * c + 6], v[8 * c + 7]));
-        *reinterpret_cast<uint4 *>(stage + C::at(lane, c)) = q;
-    }
-    __syncwarp();
-    const int col = col0 + lane % C::P * C::E;
+        for (int i = 0; i < kPieces32<T>; ++i)
+            *reinterpret_cast<uint4 *>(tile + piece_at<T>(kRows32<T> * i + lane / kPieces32<T>, lane % kPieces32<T>)) = r[i];
+    } else {
+        T v[32];
+        memcpy(v, r, sizeof(v));
 #pragma unroll
-    for (int i = 0; i < C::P; ++i) {
-        const int row = row0 + i * C::R + lane / C::P;
-        const uint4 q = *reinterpret_cast<const uint4 *>(stage + C::at(i * C::R + lane / C::P, lane % C::P));
-        if (row < M && col < N) store_piece(base + row * ld + col, q, N - col, vec);
+        for (int i = 0; i < 32; ++i) reinterpret_cast<T *>(tile + piece_at<T>(i, lane / kPiece<T>))[lane % kPiece<T>] = v[i];
     }
     __syncwarp();
 }
 
-// One row of 64 elements of an operand's tile, the eight that this lane brings.  `unit`: row of 128 bytes in the tile.  K-major: one
-// per m (or n); MN-major: 64 of them, one per k, for every 64 of M (or N).
-template <int LOADER>
-struct Eight {
-    uint32_t w[LOADER == kSplit ? 8 : 4];
+// A tile leaves: by one TMA store, which goes on while the warp does, or by ordinary ones.
+template <typename T>
+__device__ __forceinline__ void tile_leave(const unsigned char *tile, const CUtensorMap *map, T *base, long long ld, bool vec, int row0, int col0, int M,
+                                           int N, int layer, int lane)
+{
+    if (map) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) tma_store_3d(map, col0, row0, layer, smem_u32(tile));
+        return;
+    }
+    __syncwarp();
+    if (vec) {
+        const int row = row0 + lane / kPieces32<T>, col = col0 + lane % kPieces32<T> * kPiece<T>;
+        T *p = base + row * ld + col;
+#pragma unroll
+        for (int i = 0; i < kPieces32<T>; ++i, p += kRows32<T> * ld) {
+            const uint4 q = *reinterpret_cast<const uint4 *>(tile + piece_at<T>(kRows32<T> * i + lane / kPieces32<T>, lane % kPieces32<T>));
+            if (row + kRows32<T> * i < M && col < N) store_piece(p, q, N - col);
+        }
+    } else if (col0 + lane < N) {
+        T *p = base + row0 * ld + col0 + lane;
+#pragma unroll 8
+        for (int i = 0; i < min(32, M - row0); ++i, p += ld) *p = reinterpret_cast<const T *>(tile + piece_at<T>(i, lane / kPiece<T>))[lane % kPiece<T>];
+    }
+    __syncwarp();
+}
+
+// An operand's tile without TMA.  It is made of rows of contiguous elements, `slow` of them per k (MN-major) or per m or n; a thread brings
+// pieces of eight elements.  Q: the piece's place in the tile.
+struct Piece {
+    int slow, fast, at;  // first element, relative to the tile's; byte offset of its bf16 numbers in the tile
 };
 
-template <int LOADER>
-__device__ __forceinline__ Eight<LOADER> operand_load(const void *base, long long ld, bool mn, int vec, int mn0, int k0, int MN, int K, int unit,
-                                                      int piece)
+template <int BK>
+__device__ __forceinline__ Piece piece_of_tile(int q, bool mn)
 {
-    const int slow = mn ? k0 + unit % 64 : mn0 + unit, slows = mn ? K : MN;
-    const int fast = (mn ? mn0 + unit / 64 * 64 : k0) + piece * 8, fasts = mn ? MN : K;
-    Eight<LOADER> e;
-#pragma unroll
-    for (int i = 0; i < (LOADER == kSplit ? 8 : 4); ++i) e.w[i] = 0;
-    const int have = slow < slows ? fasts - fast : 0;
-    if (have <= 0) return e;
-    if constexpr (LOADER == kSplit) {
-        const float *p = static_cast<const float *>(base) + slow * ld + fast;
-        if (vec >= 16 && have >= 8) {
-            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p)), v = __ldg(reinterpret_cast<const uint4 *>(p) + 1);
-            e.w[0] = u.x, e.w[1] = u.y, e.w[2] = u.z, e.w[3] = u.w, e.w[4] = v.x, e.w[5] = v.y, e.w[6] = v.z, e.w[7] = v.w;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < have) e.w[i] = __float_as_uint(__ldg(p + i));
-        }
+    Piece e;
+    if (mn) {  // blocks of 64 along M or N: BK rows of 128 bytes
+        const int block = q / (8 * BK), k = q / 8 % BK, c = q % 8;
+        e.slow = k, e.fast = 64 * block + 8 * c, e.at = (block * BK + k) * 128 + ((c ^ (k & 7)) << 4);
+    } else if (BK == 64) {
+        const int row = q / 8, c = q % 8;
+        e.slow = row, e.fast = 8 * c, e.at = row * 128 + ((c ^ (row & 7)) << 4);
     } else {
-        const unsigned short *p = static_cast<const unsigned short *>(base) + slow * ld + fast;
-        if (vec >= 16 && have >= 8) {
-            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p));
-            e.w[0] = u.x, e.w[1] = u.y, e.w[2] = u.z, e.w[3] = u.w;
-        } else if (vec >= 4) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (2 * i + 2 <= have) e.w[i] = __ldg(reinterpret_cast<const uint32_t *>(p) + i);
-                else if (2 * i < have) e.w[i] = __ldg(p + 2 * i);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (2 * i < have) e.w[i] = __ldg(p + 2 * i);
-                if (2 * i + 1 < have) e.w[i] |= (uint32_t)__ldg(p + 2 * i + 1) << 16;
-            }
-        }
+        const int row = q / 4, c = q % 4;
+        e.slow = row, e.fast = 8 * c, e.at = row * 64 + ((c ^ (row >> 1 & 3)) << 4);
     }
     return e;
 }
 
-template <int LOADER>
-__device__ __forceinline__ void operand_store(const Eight<LOADER> &e, unsigned char *tile, int tile_bytes, int unit, int piece)
+// Where an operand's tile starts and what there is of it
+struct Source {
+    const void *base;
+    long long ld;
+    int slow0, fast0, slows, fasts, vec;
+};
+
+__device__ __forceinline__ Source source_of(const void *base, long long ld, bool mn, int vec, int mn0, int k0, int MN, int K)
 {
-    const int at = unit * 128 + ((piece ^ (unit & 7)) << 4);
-    if constexpr (LOADER != kSplit) {
-        *reinterpret_cast<uint4 *>(tile + at) = make_uint4(e.w[0], e.w[1], e.w[2], e.w[3]);
+    return {base, ld, mn ? k0 : mn0, mn ? mn0 : k0, mn ? K : MN, mn ? MN : K, vec};
+}
+
+__device__ __forceinline__ void piece_load(uint32_t (&w)[8], const Source &s, const Piece &e)  // float32
+{
+    const int slow = s.slow0 + e.slow, fast = s.fast0 + e.fast, have = slow < s.slows ? s.fasts - fast : 0;
+    const float *p = static_cast<const float *>(s.base) + slow * s.ld + fast;
+    if (s.vec >= 16 && have >= 8) {
+        const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p)), v = __ldg(reinterpret_cast<const uint4 *>(p) + 1);
+        w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w, w[4] = v.x, w[5] = v.y, w[6] = v.z, w[7] = v.w;
     } else {
-        uint32_t p0[4], p1[4], p2[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float u = __uint_as_float(e.w[2 * i]), v = __uint_as_float(e.w[2 * i + 1]);
-            p0[i] = pack(u, v);
-            u -= low(p0[i]), v -= high(p0[i]);
-            p1[i] = pack(u, v);
-            p2[i] = pack(u - low(p1[i]), v - high(p1[i]));
-        }
-        *reinterpret_cast<uint4 *>(tile + at) = make_uint4(p0[0], p0[1], p0[2], p0[3]);
-        *reinterpret_cast<uint4 *>(tile + tile_bytes + at) = make_uint4(p1[0], p1[1], p1[2], p1[3]);
-        *reinterpret_cast<uint4 *>(tile + 2 * tile_bytes + at) = make_uint4(p2[0], p2[1], p2[2], p2[3]);
+        for (int i = 0; i < 8; ++i) w[i] = i < have ? __float_as_uint(__ldg(p + i)) : 0;
     }
 }
 
-// A share of a tile's sum: tile (m0, n0) and the blocks [k, end) of 64.
+__device__ __forceinline__ void piece_store(const uint32_t (&w)[8], unsigned char *tile, int tile_bytes, int at)
+{
+    uint32_t p0[4], p1[4], p2[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float2 v = make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+        p0[i] = pack(v.x, v.y);
+        v = __fadd2_rn(v, make_float2(-low(p0[i]), -high(p0[i])));
+        p1[i] = pack(v.x, v.y);
+        v = __fadd2_rn(v, make_float2(-low(p1[i]), -high(p1[i])));
+        p2[i] = pack(v.x, v.y);
+    }
+    *reinterpret_cast<uint4 *>(tile + at) = make_uint4(p0[0], p0[1], p0[2], p0[3]);
+    *reinterpret_cast<uint4 *>(tile + tile_bytes + at) = make_uint4(p1[0], p1[1], p1[2], p1[3]);
+    *reinterpret_cast<uint4 *>(tile + 2 * tile_bytes + at) = make_uint4(p2[0], p2[1], p2[2], p2[3]);
+}
+
+// bf16 rows of any alignment: a warp brings a row of 64 elements at a time, a lane two neighbours, so that it touches every sector once.
+__device__ __forceinline__ uint32_t pair_load(const Source &s, int unit, bool mn, int lane)
+{
+    const int slow = s.slow0 + (mn ? unit % 64 : unit), fast = s.fast0 + (mn ? unit / 64 * 64 : 0) + 2 * lane;
+    const int have = slow < s.slows ? s.fasts - fast : 0;
+    const unsigned short *p = static_cast<const unsigned short *>(s.base) + slow * s.ld + fast;
+    if (have <= 0) return 0;
+    if (s.vec >= 4 && have >= 2) return __ldg(reinterpret_cast<const uint32_t *>(p));
+    return __ldg(p) | (have >= 2 ? (uint32_t)__ldg(p + 1) << 16 : 0);
+}
+
+__device__ __forceinline__ void pair_store(uint32_t w, unsigned char *tile, int unit, int lane)
+{
+    *reinterpret_cast<uint32_t *>(tile + unit * 128 + (((lane / 4) ^ (unit & 7)) << 4) + lane % 4 * 4) = w;
+}
+
+// A share of a tile's sum: tile (m0, n0) and the blocks [k, end) of K.
 struct Share {
     int m0, n0, k, end, split;
 };
@@ -326,44 +446,28 @@ __device__ __forceinline__ Share share_of(const GemmParams &p, int w)
     return s;
 }
 
-template <typename TIN, typename TOUT, int ACT>
-__device__ __forceinline__ void finish_chunk(const GemmParams &p, float (&v)[32], int row0, int col0, unsigned char *stage, const float *bias,
-                                             const uint4 (&res)[Chunk<TOUT>::P], int lane)
-{
-    constexpr bool kFast = std::is_same<TOUT, bf16>::value;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        const float4 b = reinterpret_cast<const float4 *>(bias)[c];
-        v[4 * c] += b.x, v[4 * c + 1] += b.y, v[4 * c + 2] += b.z, v[4 * c + 3] += b.w;
-    }
-    if (p.pre) chunk_store<TIN>(v, static_cast<TIN *>(p.pre), p.ld_pre, row0, col0, p.M, p.N, p.pre_vec, stage, lane);
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = activate<kFast, ACT>(v[i]);
-    if (p.residual) chunk_add<TOUT>(v, res, stage, lane);
-    chunk_store<TOUT>(v, static_cast<TOUT *>(p.out), p.ld_out, row0, col0, p.M, p.N, p.out_vec, stage, lane);
-}
-
 template <int LOADER, typename TOUT>
-__global__ void __launch_bounds__(LOADER == kTma ? 32 * (kEpilogueWarps + 2) : 32 * (kEpilogueWarps + 1 + kProducerWarps), 1)
-    gemm_kernel(const __grid_constant__ GemmParams p)
+__global__ void __launch_bounds__(gemm_threads(LOADER), 1) gemm_kernel(const __grid_constant__ GemmParams p)
 {
     using TIN = typename std::conditional<LOADER == kSplit, float, bf16>::type;
-    constexpr int kPieces = LOADER == kSplit ? 3 : 1;
+    constexpr int kPieces = LOADER == kSplit ? 3 : 1, kEpilogue = epilogue_warps(LOADER), BK = block_k(LOADER), kRing = ring_bytes(LOADER);
     extern __shared__ unsigned char raw[];
     unsigned char *const ring = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
     unsigned char *const staging = ring + kRing;
-    float *const bias_rows = reinterpret_cast<float *>(staging + kEpilogueWarps * 4096);  // 32 per warp
-    __shared__ __align__(8) uint64_t bars[2 * 8 + 4 + 1];
+    float *const bias_rows = reinterpret_cast<float *>(staging + kEpilogue * 4096);  // 64 per warp
+    __shared__ __align__(8) uint64_t bars[2 * 8 + 2 * kAccs + 1];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int failed;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const uint32_t full = smem_u32(bars), empty = full + 64, acc_full = full + 128, acc_empty = full + 144, last = full + 160;
-    // Tensor memory: two accumulators, so that one is taken out while the other is filled.  With pieces each has a second one behind it
-    // for all products but p0 p0: the tensor cores cut the sum off, not round it, at every instruction, and the five small products
-    // would do so to the whole sum five times as often as the large one does (float32, K = 4096, 16 rows: relative error 3.2e-6
-    // with one accumulator).
+    const uint32_t full = smem_u32(bars), empty = full + 64, acc_full = full + 128, acc_empty = acc_full + 8 * kAccs, last = acc_empty + 8 * kAccs;
+    // Tensor memory.  Two to four accumulators, so that some are taken out while another is filled.  The tensor cores cut a sum off, not round it, at
+    // every instruction, by 3e-8 of the sum on the average.  So (1) pieces have a second accumulator for all products but p0 p0, which keeps the five
+    // small products of each step from cutting at the large sum; (2) after `run` blocks the sum is added to a running one that stays in tensor
+    // memory too, behind the accumulators, and so does the small products' then.
     constexpr int kParts = kPieces == 3 ? 2 : 1;
-    const uint32_t columns = 2 * kParts * p.bn;
+    const bool runs = p.run < p.kshare;
+    const int acc_step = runs ? p.bn : kParts * p.bn, sum_at = 2 * p.bn;  // (with runs there are two accumulators)
+    const unsigned acc_mask = p.accs - 1, acc_shift = p.accs == 4 ? 2 : 1;
 
     if (threadIdx.x == 0) {
         failed = 0;
@@ -371,12 +475,12 @@ __global__ void __launch_bounds__(LOADER == kTma ? 32 * (kEpilogueWarps + 2) : 3
             mbar_init(full + 8 * s, LOADER == kTma ? 1 : kProducerWarps);
             mbar_init(empty + 8 * s, 1);
         }
-        for (int b = 0; b < 2; ++b) mbar_init(acc_full + 8 * b, 1), mbar_init(acc_empty + 8 * b, kEpilogueWarps);
+        for (int b = 0; b < p.accs; ++b) mbar_init(acc_full + 8 * b, 1), mbar_init(acc_empty + 8 * b, kEpilogue / p.groups);
         mbar_init(last, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (warp == kEpilogueWarps) tmem_alloc(smem_u32(&tmem_slot), columns);
+    if (warp == kEpilogue) tmem_alloc(smem_u32(&tmem_slot), p.columns);
     tcgen05_fence_before();
     __syncthreads();
     tcgen05_fence_after();
@@ -385,95 +489,161 @@ __global__ void __launch_bounds__(LOADER == kTma ? 32 * (kEpilogueWarps + 2) : 3
     asm volatile("griddepcontrol.launch_dependents;");
 
     const int total = p.tiles * p.splits;
-    const int a_bytes = kBM * 128, b_bytes = p.bn * 128, stage_bytes = kPieces * (a_bytes + b_bytes);
+    const int a_bytes = kBM * 2 * BK, b_bytes = p.bn * 2 * BK, stage_bytes = kPieces * (a_bytes + b_bytes);
 
-    if (warp < kEpilogueWarps) {
-        // ---- epilogue: warps w and w + 4 share the 32 lanes 32 (w % 4) and up, every other chunk of 32 columns each
-        unsigned char *const stage = staging + warp * 4096;
-        float *const bias = bias_rows + warp * 32;
+    if (warp < kEpilogue) {
+        if constexpr (LOADER != kTma) more_registers<kEpilogueRegs>();
+        // ---- epilogue: the 32 lanes 32 (warp % 4) and up, parts of 64 columns in two tiles of 32.  16 warps are as many as the widest product
+        // has such parts; for narrower ones they form groups that take the accumulators in turn.
+        const int in_group = kEpilogue / 4 / p.groups, group = warp / 4 / in_group, part = warp / 4 % in_group;
+        unsigned char *const buffer = staging + warp * 4096;  // a float32 tile, or two bf16 ones: for the part's two, or for the result and z
+        float *const bias = bias_rows + warp * 64;
         const uint32_t lanes = tmem + ((uint32_t)(warp % 4 * 32) << 16);
-        int buf = 0, phase = 0;
-        for (int w = blockIdx.x; w < total; w += gridDim.x) {
-            const Share s = share_of(p, w);
-            const int row0 = s.m0 + warp % 4 * 32;
-            bool waited = false, ok = true;
-            for (int c = warp / 4; c < p.bn / 32; c += 2) {
-                const int col0 = s.n0 + 32 * c;
-                if (col0 >= p.N || row0 >= p.M) break;
-                uint4 res[Chunk<TOUT>::P];
-                if (!p.partial) {
-                    if (p.residual) chunk_load<TOUT>(res, static_cast<const TOUT *>(p.residual), p.ld_res, row0, col0, p.M, p.N, p.res_vec, lane);
-                    const int col = col0 + lane;
-                    bias[lane] = p.bias && col < p.N ? to_float(static_cast<const TIN *>(p.bias)[col]) : 0.0f;
-                    __syncwarp();
-                }
-                if (!waited) {
-                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * buf, phase, &failed)))) break;
-                    tcgen05_fence_after();
-                    waited = true;
-                }
-                float v[32];
-                tmem_load32(v, lanes + buf * kParts * p.bn + 32 * c);
-                if constexpr (kParts == 2) {
-                    float small[32];
-                    tmem_load32(small, lanes + (2 * buf + 1) * p.bn + 32 * c);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] += small[i];
-                }
-                if (p.partial) {
-                    float *const out = p.partial + (long long)s.split * p.M * p.ld_partial;
-                    chunk_store<float>(v, out, p.ld_partial, row0, col0, p.M, p.N, true, stage, lane);
-                } else if (p.act == FLASHBEV_ACT_NONE) {
-                    finish_chunk<TIN, TOUT, FLASHBEV_ACT_NONE>(p, v, row0, col0, stage, bias, res, lane);
-                } else if (p.act == FLASHBEV_ACT_RELU) {
-                    finish_chunk<TIN, TOUT, FLASHBEV_ACT_RELU>(p, v, row0, col0, stage, bias, res, lane);
-                } else if (p.act == FLASHBEV_ACT_GELU) {
-                    finish_chunk<TIN, TOUT, FLASHBEV_ACT_GELU>(p, v, row0, col0, stage, bias, res, lane);
-                } else {
-                    finish_chunk<TIN, TOUT, FLASHBEV_ACT_SILU>(p, v, row0, col0, stage, bias, res, lane);
-                }
-            }
-            if (ok && !waited) ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * buf, phase, &failed));
-            if (!ok) break;
-            tcgen05_fence_before();
+        const CUtensorMap *const tout = p.store_tma ? &p.tout : nullptr, *const tpre = p.store_tma ? &p.tpre : nullptr;
+        unsigned u = 0;          // accumulators of the CTA so far
+        int bias_at = -1;        // the column that the bias in shared memory starts at
+        const auto stores_done = [&] {  // (with the buffer)
+            if (lane == 0) tma_store_wait<0>();
             __syncwarp();
-            if (lane == 0) mbar_arrive(acc_empty + 8 * buf);
-            phase ^= buf, buf ^= 1;
+        };
+        bool ok = true;
+        for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
+            const Share s = share_of(p, w);
+            const int row0 = s.m0 + warp % 4 * 32, tiles = row0 < p.M ? (min(p.bn, p.N - s.n0) + 31) / 32 : 0;
+            for (int k0 = s.k; k0 < s.end; k0 += p.run, ++u) {
+                if (u % p.groups != group) continue;
+                const bool first = k0 == s.k, ends = k0 + p.run >= s.end;
+                const unsigned a = u & acc_mask;
+                bool waited = false;
+                for (int h0 = 2 * part; h0 < tiles; h0 += 2 * in_group) {
+                    const int c0 = s.n0 + 32 * h0;
+                    uint4 res[kPieces32<TOUT>];
+                    const auto bring = [&](int col0) {
+                        tile_load<TOUT>(res, static_cast<const TOUT *>(p.residual), p.ld_res, p.res_vec, row0, col0, p.M, p.N, lane);
+                    };
+                    if (ends && !p.partial) {  // what does not need the sums
+                        if (p.residual) bring(c0);
+                        if (bias_at != c0) {
+                            bias_at = c0;
+#pragma unroll
+                            for (int j = 0; j < 64; j += 32)
+                                bias[j + lane] = p.bias && c0 + j + lane < p.N ? to_float(static_cast<const TIN *>(p.bias)[c0 + j + lane]) : 0.0f;
+                        }
+                        stores_done();
+                    }
+                    if (!waited) {
+                        if (!(ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * a, u >> acc_shift & 1, &failed)))) break;
+                        tcgen05_fence_after();
+                        waited = true;
+                    }
+#pragma unroll
+                    for (int odd = 0; odd < 2; ++odd) {
+                        const int h = h0 + odd, col0 = c0 + 32 * odd;
+                        if (h >= tiles) break;
+                        const uint32_t acc = lanes + a * acc_step + 32 * h, sum = lanes + sum_at + 32 * h;
+                        uint32_t r[32];
+                        float v[32];
+                        tmem_load32(r, acc);
+                        tmem_wait(r);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+                        const auto add = [&](uint32_t at) {
+                            tmem_load32(r, at);
+                            tmem_wait(r);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) v[i] += __uint_as_float(r[i]);
+                        };
+                        if (runs && !first) add(sum);
+                        if (!ends) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(v[i]);
+                            tmem_store32(sum, r);
+                            continue;
+                        }
+                        if (kParts == 2) add(runs ? sum + p.bn : acc + p.bn);
+                        if (p.partial) {
+                            stores_done();
+                            row_store<float>(v, buffer, lane);
+                            tile_leave<float>(buffer, &p.tout, nullptr, 0, true, row0, col0, p.M, p.N, s.split, lane);
+                            continue;
+                        }
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            const float4 q = reinterpret_cast<const float4 *>(bias + 32 * odd)[c];
+                            const float2 x = __fadd2_rn(make_float2(v[4 * c], v[4 * c + 1]), make_float2(q.x, q.y));
+                            const float2 y = __fadd2_rn(make_float2(v[4 * c + 2], v[4 * c + 3]), make_float2(q.z, q.w));
+                            v[4 * c] = x.x, v[4 * c + 1] = x.y, v[4 * c + 2] = y.x, v[4 * c + 3] = y.y;
+                        }
+                        // z leaves from the buffer's second half, or from the whole of it before the result comes
+                        if (p.pre) {
+                            unsigned char *const tile = buffer + (sizeof(TIN) == 2 && sizeof(TOUT) == 2 ? 2048 : 0);
+                            if (odd) stores_done();
+                            row_store<TIN>(v, tile, lane);
+                            tile_leave<TIN>(tile, tpre, static_cast<TIN *>(p.pre), p.ld_pre, p.pre_vec, row0, col0, p.M, p.N, 0, lane);
+                        }
+                        activate_all<std::is_same<TOUT, bf16>::value>(v, p.act);
+                        unsigned char *const tile = buffer + (sizeof(TOUT) == 2 && odd && !p.pre ? 2048 : 0);
+                        if (p.pre ? sizeof(TIN) == 4 || sizeof(TOUT) == 4 : odd && sizeof(TOUT) == 4) stores_done();
+                        if (p.residual) {
+                            tile_stage<TOUT>(res, p.res_vec, tile, lane);
+                            if (!odd && h + 1 < tiles) bring(col0 + 32);
+                            row_add<TOUT>(v, tile, lane);
+                        }
+                        row_store<TOUT>(v, tile, lane);
+                        tile_leave<TOUT>(tile, tout, static_cast<TOUT *>(p.out), p.ld_out, p.out_vec, row0, col0, p.M, p.N, 0, lane);
+                    }
+                }
+                if (ok && !waited) ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * a, u >> acc_shift & 1, &failed));
+                if (!ok) break;
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(acc_empty + 8 * a);
+            }
         }
-    } else if (warp == kEpilogueWarps) {
+        if (lane == 0) tma_store_wait<0>();
+        __syncwarp();
+    } else if (LOADER == kTma ? warp == kEpilogue : warp < 2 * kEpilogue) {
         // ---- products, by one thread
-        if (lane == 0) {
+        if constexpr (LOADER != kTma) fewer_registers<kProductRegs>();
+        if (warp == kEpilogue && lane == 0) {
             const uint32_t idesc = mma_idesc(p.bn, p.a_mn, p.b_mn);
             const int a_step = p.a_mn ? 2048 >> 4 : 32 >> 4, b_step = p.b_mn ? 2048 >> 4 : 32 >> 4;  // 16 of K further
-            int stage = 0, phase = 0, buf = 0, acc_phase = 0;
+            int stage = 0, phase = 0;
+            unsigned u = 0;  // accumulators filled so far
             bool ok = true;
             for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
                 const Share s = share_of(p, w);
-                if (!(ok = mbar_wait(acc_empty + 8 * buf, acc_phase ^ 1, &failed))) break;
-                tcgen05_fence_after();
-                const uint32_t d = tmem + buf * kParts * p.bn;
-                for (int k = s.k; k < s.end; ++k) {
-                    if (!(ok = mbar_wait(full + 8 * stage, phase, &failed))) break;
+                for (int k0 = s.k; k0 < s.end && ok; k0 += p.run, ++u) {
+                    const unsigned acc = u & acc_mask;
+                    ok = mbar_wait(acc_empty + 8 * acc, (u >> acc_shift & 1) ^ 1, &failed);
+                    // (the one accumulator of the small products: the tile before has been taken out)
+                    if (ok && kParts == 2 && runs && k0 == s.k) ok = mbar_wait(acc_empty + 8 * ((u + 1) & 1), ((u + 1) >> 1 & 1) ^ 1, &failed);
+                    if (!ok) break;
                     tcgen05_fence_after();
-                    const uint32_t at = smem_u32(ring) + stage * stage_bytes;
-                    const uint64_t a = smem_desc(at, p.a_mn, 8192), b = smem_desc(at + kPieces * a_bytes, p.b_mn, 8192);
-                    if constexpr (kPieces == 1) {
+                    const uint32_t d = tmem + acc * acc_step, small = runs ? tmem + 3 * p.bn : d + p.bn;
+                    const int k1 = min(k0 + p.run, s.end);
+                    for (int k = k0; k < k1; ++k) {
+                        if (!(ok = mbar_wait(full + 8 * stage, phase, &failed))) break;
+                        tcgen05_fence_after();
+                        const uint32_t at = smem_u32(ring) + stage * stage_bytes;
+                        const uint64_t a = smem_desc(at, p.a_mn, 2 * BK, 128 * BK), b = smem_desc(at + kPieces * a_bytes, p.b_mn, 2 * BK, 128 * BK);
+                        if constexpr (kPieces == 1) {
 #pragma unroll
-                        for (int i = 0; i < kBK / 16; ++i) mma_bf16(d, a + i * a_step, b + i * b_step, idesc, k > s.k || i > 0);
-                    } else {
-                        constexpr int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
+                            for (int i = 0; i < BK / 16; ++i) mma_bf16(d, a + i * a_step, b + i * b_step, idesc, k > k0 || i > 0);
+                        } else {
+                            constexpr int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
 #pragma unroll
-                        for (int j = 0; j < 6; ++j)
+                            for (int j = 0; j < 6; ++j)
 #pragma unroll
-                            for (int i = 0; i < kBK / 16; ++i)
-                                mma_bf16(j < 5 ? d + p.bn : d, a + pa[j] * (a_bytes >> 4) + i * a_step, b + pb[j] * (b_bytes >> 4) + i * b_step,
-                                         idesc, k > s.k || i > 0 || (j > 0 && j < 5));
+                                for (int i = 0; i < BK / 16; ++i)
+                                    mma_bf16(j < 5 ? small : d, a + pa[j] * (a_bytes >> 4) + i * a_step, b + pb[j] * (b_bytes >> 4) + i * b_step, idesc,
+                                             i > 0 || (j < 5 ? k > s.k || j > 0 : k > k0));
+                        }
+                        mma_commit(empty + 8 * stage);
+                        if (++stage == p.stages) stage = 0, phase ^= 1;
                     }
-                    mma_commit(empty + 8 * stage);
-                    if (++stage == p.stages) stage = 0, phase ^= 1;
+                    if (ok) mma_commit(acc_full + 8 * acc);
                 }
-                if (ok) mma_commit(acc_full + 8 * buf);
-                acc_phase ^= buf, buf ^= 1;
             }
             if (!ok) {  // nothing of this CTA may be in flight when it gives its memory back
                 mma_commit(last);
@@ -482,7 +652,7 @@ __global__ void __launch_bounds__(LOADER == kTma ? 32 * (kEpilogueWarps + 2) : 3
         }
         __syncwarp();
     } else if constexpr (LOADER == kTma) {
-        if (lane == 0) {
+        if (warp == kEpilogue + 1 && lane == 0) {
             int stage = 0, phase = 0;
             bool ok = true;
             for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
@@ -492,14 +662,14 @@ __global__ void __launch_bounds__(LOADER == kTma ? 32 * (kEpilogueWarps + 2) : 3
                     const uint32_t at = smem_u32(ring) + stage * stage_bytes, bar = full + 8 * stage;
                     mbar_expect(bar, stage_bytes);
                     if (p.a_mn) {
-                        for (int i = 0; i < kBM / 64; ++i) tma_load_2d(at + 8192 * i, &p.ta, s.m0 + 64 * i, k * kBK, bar);
+                        for (int i = 0; i < kBM / 64; ++i) tma_load_2d(at + 8192 * i, &p.ta, s.m0 + 64 * i, k * BK, bar);
                     } else {
-                        tma_load_2d(at, &p.ta, k * kBK, s.m0, bar);
+                        tma_load_2d(at, &p.ta, k * BK, s.m0, bar);
                     }
                     if (p.b_mn) {
-                        for (int i = 0; i < p.bn / 64; ++i) tma_load_2d(at + a_bytes + 8192 * i, &p.tb, s.n0 + 64 * i, k * kBK, bar);
+                        for (int i = 0; i < p.bn / 64; ++i) tma_load_2d(at + a_bytes + 8192 * i, &p.tb, s.n0 + 64 * i, k * BK, bar);
                     } else {
-                        tma_load_2d(at + a_bytes, &p.tb, k * kBK, s.n0, bar);
+                        tma_load_2d(at + a_bytes, &p.tb, k * BK, s.n0, bar);
                     }
                     if (++stage == p.stages) stage = 0, phase ^= 1;
                 }
@@ -509,51 +679,85 @@ __global__ void __launch_bounds__(LOADER == kTma ? 32 * (kEpilogueWarps + 2) : 3
         }
         __syncwarp();
     } else {
-        // ---- loads without TMA: a warp brings four rows of 128 bytes (64 elements) at a time; the loads of the next stage are under
-        // way while this one is written and the products of the ones before run
-        constexpr int kPasses = (kBM + 128) / (4 * kProducerWarps);  // tiles are at most 128 columns wide here
-        const int first = (warp - kEpilogueWarps - 1) * 4 + lane / 8, piece = lane % 8;
-        const int passes = (kBM + p.bn) / (4 * kProducerWarps);
+        // ---- loads without TMA, two groups of warps for every other stage: a group's loads for its next stage are under way while the
+        // other one's are written and the products of the stages before run
+        fewer_registers<kProducerRegs>();
+        constexpr int kThreads = 32 * kProducerWarps;
+        constexpr int kPiecesA = kBM * BK / 8 / kThreads, kPiecesB = 128 * BK / 8 / kThreads;  // of a thread, at most
+        constexpr int kRowsA = kBM / kProducerWarps, kRowsB = 256 / kProducerWarps;                                        // of a warp
+        const int group = (warp - 2 * kEpilogue) / kProducerWarps, member = warp % kProducerWarps, t = threadIdx.x % kThreads;
+        const int pieces_b = p.bn * BK / 8;
         int w = blockIdx.x, stage = 0, phase = 0;
         Share s = share_of(p, min(w, total - 1));
-        Eight<LOADER> r[kPasses];
-        const auto fetch = [&] {
-#pragma unroll
-            for (int i = 0; i < kPasses; ++i) {
-                const int unit = first + 4 * kProducerWarps * i;
-                if (i < kBM / (4 * kProducerWarps))
-                    r[i] = operand_load<LOADER>(p.a, p.lda, p.a_mn, p.a_vec, s.m0, s.k * kBK, p.M, p.K, unit, piece);
-                else if (i < passes)
-                    r[i] = operand_load<LOADER>(p.b, p.ldb, p.b_mn, p.b_vec, s.n0, s.k * kBK, p.N, p.K, unit - kBM, piece);
-            }
+        const auto next = [&] {  // the block of K after this one; false behind the last
+            if (++stage == p.stages) stage = 0, phase ^= 1;
+            if (++s.k < s.end) return true;
+            w += gridDim.x;
+            if (w >= total) return false;
+            s = share_of(p, w);
+            return true;
         };
-        if (w < total) fetch();
-        while (w < total) {
-            if (!__all_sync(0xffffffffu, mbar_wait(empty + 8 * stage, phase ^ 1, &failed))) break;
-            unsigned char *const at = ring + stage * stage_bytes;
-#pragma unroll
-            for (int i = 0; i < kPasses; ++i) {
-                const int unit = first + 4 * kProducerWarps * i;
-                if (i < kBM / (4 * kProducerWarps)) operand_store<LOADER>(r[i], at, a_bytes, unit, piece);
-                else if (i < passes) operand_store<LOADER>(r[i], at + kPieces * a_bytes, b_bytes, unit - kBM, piece);
-            }
+        const auto source_a = [&] { return source_of(p.a, p.lda, p.a_mn, p.a_vec, s.m0, s.k * BK, p.M, p.K); };
+        const auto source_b = [&] { return source_of(p.b, p.ldb, p.b_mn, p.b_vec, s.n0, s.k * BK, p.N, p.K); };
+        bool more = w < total && (group == 0 || next());
+        const auto ready = [&] {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(full + 8 * stage);
-            if (++stage == p.stages) stage = 0, phase ^= 1;
-            if (++s.k == s.end) {
-                w += gridDim.x;
-                if (w >= total) break;
-                s = share_of(p, w);
+        };
+        const auto free_stage = [&] { return __all_sync(0xffffffffu, mbar_wait(empty + 8 * stage, phase ^ 1, &failed)); };
+        if constexpr (LOADER == kSplit) {
+            uint32_t a[kPiecesA][8], b[kPiecesB][8];
+            const auto fetch = [&] {
+                const Source sa = source_a(), sb = source_b();
+#pragma unroll
+                for (int i = 0; i < kPiecesA; ++i) piece_load(a[i], sa, piece_of_tile<BK>(t + kThreads * i, p.a_mn));
+#pragma unroll
+                for (int i = 0; i < kPiecesB; ++i)
+                    if (t + kThreads * i < pieces_b) piece_load(b[i], sb, piece_of_tile<BK>(t + kThreads * i, p.b_mn));
+            };
+            if (more) fetch();
+            while (more && free_stage()) {
+                unsigned char *const at = ring + stage * stage_bytes;
+#pragma unroll
+                for (int i = 0; i < kPiecesA; ++i) piece_store(a[i], at, a_bytes, piece_of_tile<BK>(t + kThreads * i, p.a_mn).at);
+#pragma unroll
+                for (int i = 0; i < kPiecesB; ++i)
+                    if (t + kThreads * i < pieces_b)
+                        piece_store(b[i], at + kPieces * a_bytes, b_bytes, piece_of_tile<BK>(t + kThreads * i, p.b_mn).at);
+                ready();
+                more = next() && next();
+                if (more) fetch();
             }
-            fetch();
+        } else {
+            uint32_t a[kRowsA], b[kRowsB];
+            const auto fetch = [&] {
+                const Source sa = source_a(), sb = source_b();
+#pragma unroll
+                for (int i = 0; i < kRowsA; ++i) a[i] = pair_load(sa, member + kProducerWarps * i, p.a_mn, lane);
+#pragma unroll
+                for (int i = 0; i < kRowsB; ++i)
+                    if (member + kProducerWarps * i < p.bn) b[i] = pair_load(sb, member + kProducerWarps * i, p.b_mn, lane);
+            };
+            if (more) fetch();
+            while (more && free_stage()) {
+                unsigned char *const at = ring + stage * stage_bytes;
+#pragma unroll
+                for (int i = 0; i < kRowsA; ++i) pair_store(a[i], at, member + kProducerWarps * i, lane);
+#pragma unroll
+                for (int i = 0; i < kRowsB; ++i)
+                    if (member + kProducerWarps * i < p.bn) pair_store(b[i], at + a_bytes, member + kProducerWarps * i, lane);
+                ready();
+                more = next() && next();
+                if (more) fetch();
+            }
         }
     }
     tcgen05_fence_before();
     __syncthreads();
-    if (warp == kEpilogueWarps) {
+    if (warp == kEpilogue) {
         tcgen05_fence_after();
-        tmem_free(tmem, columns);
+        tmem_free(tmem, p.columns);
     }
     if (threadIdx.x == 0 && failed && p.error_word) atomicAdd(p.error_word, 1u);
 }
@@ -585,13 +789,15 @@ __global__ void __launch_bounds__(256) join_kernel(const float *__restrict__ par
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (col + j >= N) break;
-            float z = v[j] + (bias ? to_float(bias[col + j]) : 0.0f);
-            if (pre) pre[row * ld_pre + col + j] = from_float<TIN>(z);
-            if (act == FLASHBEV_ACT_RELU) z = activate<kFast, FLASHBEV_ACT_RELU>(z);
-            else if (act == FLASHBEV_ACT_GELU) z = activate<kFast, FLASHBEV_ACT_GELU>(z);
-            else if (act == FLASHBEV_ACT_SILU) z = activate<kFast, FLASHBEV_ACT_SILU>(z);
-            if (residual) z += to_float(residual[row * ld_res + col + j]);
-            out[row * ld_out + col + j] = from_float<TOUT>(z);
+            if (bias) v[j] += to_float(bias[col + j]);
+            if (pre) pre[row * ld_pre + col + j] = from_float<TIN>(v[j]);
+        }
+        activate_all<kFast>(v, act);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (col + j >= N) break;
+            if (residual) v[j] += to_float(residual[row * ld_res + col + j]);
+            out[row * ld_out + col + j] = from_float<TOUT>(v[j]);
         }
     }
 }
@@ -753,13 +959,11 @@ __global__ void __launch_bounds__(256) rows_kernel(const TIN *__restrict__ x, lo
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             if (lane != r * NC + c || r >= M || n0 + c >= N) continue;
-            float z = acc[r][c] + (bias ? to_float(bias[n0 + c]) : 0.0f);
-            if (pre) pre[r * ld_pre + n0 + c] = from_float<TIN>(z);
-            if (act == FLASHBEV_ACT_RELU) z = activate<kFast, FLASHBEV_ACT_RELU>(z);
-            else if (act == FLASHBEV_ACT_GELU) z = activate<kFast, FLASHBEV_ACT_GELU>(z);
-            else if (act == FLASHBEV_ACT_SILU) z = activate<kFast, FLASHBEV_ACT_SILU>(z);
-            if (residual) z += to_float(residual[r * ld_res + n0 + c]);
-            out[r * ld_out + n0 + c] = from_float<TOUT>(z);
+            float z[2] = {acc[r][c] + (bias ? to_float(bias[n0 + c]) : 0.0f), 0.0f};
+            if (pre) pre[r * ld_pre + n0 + c] = from_float<TIN>(z[0]);
+            activate_all<kFast>(z, act);
+            if (residual) z[0] += to_float(residual[r * ld_res + n0 + c]);
+            out[r * ld_out + n0 + c] = from_float<TOUT>(z[0]);
         }
 }
 
@@ -775,7 +979,8 @@ struct Operand {
     bool mn;  // a row per k
 };
 
-bool tma_ok(const Operand &o) { return (uintptr_t)o.p % 16 == 0 && o.ld % 8 == 0; }
+// (a tensor map's strides end at 2^40 bytes)
+bool tma_ok(const Operand &o) { return (uintptr_t)o.p % 16 == 0 && o.ld % 8 == 0 && o.ld < (1LL << 38); }
 
 int row_vec(const Operand &o, int elem)
 {
@@ -808,48 +1013,79 @@ bool make_map(CUtensorMap &map, const Operand &o, int across, int K, int rows)
     const EncodeTiled encode = encode_tiled();
     if (!encode) return false;
     const cuuint64_t size[2] = {(cuuint64_t)(o.mn ? across : K), (cuuint64_t)(o.mn ? K : across)}, pitch[1] = {(cuuint64_t)o.ld * 2};
-    const cuuint32_t box[2] = {kBK, (cuuint32_t)(o.mn ? kBK : rows)}, step[2] = {1, 1};
+    constexpr int BK = block_k(kTma);
+    const cuuint32_t box[2] = {BK, (cuuint32_t)(o.mn ? BK : rows)}, step[2] = {1, 1};
     return encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(o.p), size, pitch, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Results: `layers` matrices of M rows, stored in tiles of 32 x 32
+bool make_store_map(CUtensorMap &map, void *p, bool f32, int M, int N, long long ld, int layers)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const int elem = f32 ? 4 : 2;
+    const cuuint64_t size[3] = {(cuuint64_t)N, (cuuint64_t)M, (cuuint64_t)layers};
+    const cuuint64_t pitch[2] = {(cuuint64_t)ld * elem, (cuuint64_t)ld * elem * (cuuint64_t)(layers > 1 ? M : 1)};
+    const cuuint32_t box[3] = {32, 32, 1}, step[3] = {1, 1, 1};
+    return encode(&map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, p, size, pitch, box, step,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// K after which a float32 result's sum is taken out of the tensor cores: 24 instructions that cut it off, 8e-7 of it.
+constexpr int kRun = 384;
+
 // Tiles and shares of a product.
 struct Plan {
-    int loader, bn, stages, tiles_m, tiles_n, kblocks, kshare, splits;
+    int loader, bn, stages, tiles_m, tiles_n, kblocks, kshare, splits, run, columns, accs, groups;
     long long ld_partial;
     size_t partial_bytes;  // 0: every tile's sum belongs to one CTA
 };
 
-Plan plan_product(const Operand &a, const Operand &b, bool f32, int M, int N, int K, bool may_split)
+Plan plan_product(const Operand &a, const Operand &b, bool f32, bool out_f32, int M, int N, int K, bool may_split)
 {
     Plan q = {};
     q.loader = f32 ? kSplit : (tma_ok(a) && tma_ok(b) ? kTma : kCopy);
     const int sms = sm_count();
     q.tiles_m = (M + kBM - 1) / kBM;
-    q.kblocks = (K + kBK - 1) / kBK;
-    // The widest tile that does not leave more than a tenth of the SMs' time idle (a wide tile reads A fewer times and feeds the
-    // tensor cores better).
-    const int widest = q.loader == kTma ? 256 : 128;
-    double best = 0.0;
-    for (int bn = widest; bn >= 64; bn /= 2) {
-        const long long tiles = (long long)q.tiles_m * ((N + bn - 1) / bn);
-        const long long waves = (tiles + sms - 1) / sms;
-        const double use = (double)M * N / ((double)waves * sms * kBM * bn);
-        if (use > 1.1 * best) best = use, q.bn = bn;
+    const int bk = block_k(q.loader);
+    q.kblocks = (K + bk - 1) / bk;
+    const bool runs = out_f32 && K > kRun;
+    // Widths: the columns in equal parts, at most 256 (128 where accumulators for pieces or a running sum take tensor memory).  A tile
+    // costs its columns and about 32 more; the last wave may be nearly empty.
+    const int widest = f32 || runs ? 128 : 256;
+    long long best = 0;
+    for (int t = (N + widest - 1) / widest; t <= (N + 63) / 64; ++t) {
+        const int grain = b.mn ? 64 : 32;
+        const int bn = ((N + t - 1) / t + grain - 1) / grain * grain;
+        const long long tiles = (long long)q.tiles_m * ((N + bn - 1) / bn), cost = (tiles + sms - 1) / sms * (bn + 32);
+        if (!best || cost < best) best = cost, q.bn = bn;
+        if (t > 64) break;  // (wide results: the widest tiles)
     }
     q.tiles_n = (N + q.bn - 1) / q.bn;
-    const int stage = (q.loader == kSplit ? 3 : 1) * (kBM + q.bn) * 128;
-    q.stages = std::min(8, kRing / stage);
+    const int stage = (q.loader == kSplit ? 3 : 1) * (kBM + q.bn) * 2 * bk;
+    q.stages = std::min(8, ring_bytes(q.loader) / stage);
     const long long tiles = (long long)q.tiles_m * q.tiles_n;
     q.splits = 1, q.kshare = q.kblocks;
     if (may_split && tiles * 2 <= sms) {
-        const int least = 2;  // blocks of 64 for a share to be worth its partial sums
-        int splits = (int)std::min<long long>(sms / tiles, q.kblocks / least);
+        const int least = 128 / bk;  // blocks for a share to be worth its partial sums
+        const int splits = (int)std::min<long long>(sms / tiles, q.kblocks / least);
         if (splits > 1) {
             q.kshare = (q.kblocks + splits - 1) / splits;
             q.splits = (q.kblocks + q.kshare - 1) / q.kshare;
         }
     }
+    q.run = runs && q.kshare > kRun / bk ? kRun / bk : q.kshare;
+    // Accumulators: with runs two, the running sum and, of float32 operands, that of the small products; else four where they fit (float32
+    // operands: pairs).  Groups of epilogue warps: as many 64-column parts as the tile has in each, and no more of them than accumulators.
+    const int parts = f32 ? 2 : 1, warps = epilogue_warps(q.loader) / 4, wide = (q.bn + 63) / 64;
+    const bool in_runs = q.run < q.kshare;
+    q.accs = !in_runs && 4 * parts * q.bn <= 512 ? 4 : 2;
+    const int used = in_runs ? (2 + parts) * q.bn : q.accs * parts * q.bn;
+    for (q.columns = 32; q.columns < used;) q.columns *= 2;
+    q.groups = 1;
+    while (!in_runs && q.groups < q.accs && q.groups * 2 * wide <= warps) q.groups *= 2;
     if (q.splits > 1) {
         q.ld_partial = (N + 3) / 4 * 4;
         q.partial_bytes = (size_t)q.splits * M * q.ld_partial * sizeof(float);
@@ -868,18 +1104,18 @@ struct Epilogue {
 
 bool vec_ok(const void *p, long long ld, bool f32)
 {
-    return ((uintptr_t)p | (uintptr_t)(ld * (f32 ? 4 : 2))) % 16 == 0;
+    return ((uintptr_t)p | (uintptr_t)(ld * (f32 ? 4 : 2))) % 16 == 0 && ld < (1LL << 37);
 }
 
 template <int LOADER, typename TOUT>
 cudaError_t launch_gemm(const GemmParams &g, cudaStream_t stream)
 {
     const auto kernel = gemm_kernel<LOADER, TOUT>;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    constexpr int smem = 1024 + ring_bytes(LOADER) + epilogue_bytes(LOADER);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    const int threads = LOADER == kTma ? 32 * (kEpilogueWarps + 2) : 32 * (kEpilogueWarps + 1 + kProducerWarps);
     const int grid = std::min(g.tiles * g.splits, sm_count());
-    return launch_dependent(kernel, dim3((unsigned)grid), dim3((unsigned)threads), kSmem, stream, g);
+    return launch_dependent(kernel, dim3((unsigned)grid), dim3((unsigned)gemm_threads(LOADER)), smem, stream, g);
 }
 
 template <typename TIN, typename TOUT>
@@ -902,12 +1138,21 @@ flashbev_status run_product(const Plan &q, const Operand &a, const Operand &b, b
     g.a = a.p, g.b = b.p, g.lda = a.ld, g.ldb = b.ld, g.a_mn = a.mn, g.b_mn = b.mn;
     g.a_vec = row_vec(a, elem), g.b_vec = row_vec(b, elem);
     g.M = M, g.N = N, g.K = K, g.bn = q.bn, g.stages = q.stages;
+    g.run = q.run, g.columns = q.columns, g.accs = q.accs, g.groups = q.groups;
     g.tiles_n = q.tiles_n, g.tiles = q.tiles_m * q.tiles_n, g.kblocks = q.kblocks, g.kshare = q.kshare, g.splits = q.splits;
     g.out = e.out, g.pre = e.pre, g.residual = e.residual, g.bias = e.bias, g.act = e.act;
     g.ld_out = e.ld_out, g.ld_pre = e.ld_pre, g.ld_res = e.ld_res;
     g.out_vec = vec_ok(e.out, e.ld_out, e.out_f32), g.pre_vec = vec_ok(e.pre, e.ld_pre, f32), g.res_vec = vec_ok(e.residual, e.ld_res, e.out_f32);
     g.error_word = error_word;
-    if (q.splits > 1) g.partial = partial, g.ld_partial = q.ld_partial;
+    if (q.splits > 1) {
+        g.partial = partial, g.ld_partial = q.ld_partial;
+        // (partial sums have no other results)
+        if (!make_store_map(g.tout, partial, true, M, N, q.ld_partial, q.splits)) return FLASHBEV_CUDA_ERROR;
+    } else if (g.out_vec && (!e.pre || g.pre_vec)) {
+        g.store_tma = 1;
+        if (!make_store_map(g.tout, e.out, e.out_f32, M, N, e.ld_out, 1)) return FLASHBEV_CUDA_ERROR;
+        if (e.pre && !make_store_map(g.tpre, e.pre, f32, M, N, e.ld_pre, 1)) return FLASHBEV_CUDA_ERROR;
+    }
     cudaError_t err;
     if (q.loader == kSplit) err = e.out_f32 ? launch_gemm<kSplit, float>(g, stream) : launch_gemm<kSplit, bf16>(g, stream);
     else if (q.loader == kCopy) err = e.out_f32 ? launch_gemm<kCopy, float>(g, stream) : launch_gemm<kCopy, bf16>(g, stream);
@@ -1033,8 +1278,8 @@ BackwardPlan plan_backward(const flashbev_linear_backward_params *p)
     const Operand w = {p->weight, dense(p->ld_weight, K), true}, x = {p->x, dense(p->ld_x, K), true};
     Operand dzt = q.dz;
     dzt.mn = true;
-    if (q.need_x) q.gx = plan_product(q.dz, w, f32, M, K, N, true);
-    if (q.need_w) q.gw = plan_product(dzt, x, f32, N, K, M, true);
+    if (q.need_x) q.gx = plan_product(q.dz, w, f32, f32, M, K, N, true);
+    if (q.need_w) q.gw = plan_product(dzt, x, f32, f32, N, K, M, true);
     q.partial_at = at;  // (the products run one after the other)
     at += up(std::max(q.gx.partial_bytes, q.gw.partial_bytes));
     q.total = at;
@@ -1086,8 +1331,8 @@ flashbev_status flashbev_linear(const flashbev_linear_params *p, void *stream_)
             launches = 1;
             t_last_kernel = "linear_rows";
         } else {
-            Plan q = plan_product(x, w, f32, M, N, K, true);
-            if (q.partial_bytes && (!p->workspace || p->workspace_bytes < q.partial_bytes)) q = plan_product(x, w, f32, M, N, K, false);
+            Plan q = plan_product(x, w, f32, e.out_f32, M, N, K, true);
+            if (q.partial_bytes && (!p->workspace || p->workspace_bytes < q.partial_bytes)) q = plan_product(x, w, f32, e.out_f32, M, N, K, false);
             const flashbev_status run =
                 run_product(q, x, w, f32, M, N, K, e, static_cast<float *>(p->workspace), p->error_word, stream, launches);
             if (run != FLASHBEV_OK) return run;
@@ -1101,7 +1346,9 @@ flashbev_status flashbev_linear(const flashbev_linear_params *p, void *stream_)
 size_t flashbev_linear_workspace_bytes(const flashbev_linear_params *p)
 {
     if (check_linear(p) != FLASHBEV_OK || p->rows <= kFewRows) return 0;
-    return plan_product(operand_x(p), operand_w(p), p->dtype == FLASHBEV_F32, (int)p->rows, p->out_features, p->in_features, true).partial_bytes;
+    return plan_product(operand_x(p), operand_w(p), p->dtype == FLASHBEV_F32, p->out_dtype == FLASHBEV_F32, (int)p->rows, p->out_features,
+                        p->in_features, true)
+        .partial_bytes;
 }
 
 flashbev_status flashbev_linear_backward(const flashbev_linear_backward_params *p, void *stream_)

@@ -72,6 +72,21 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map
                  : "memory");
 }
 
+// The box of the map at (x, y, z) from shared memory; what lies outside the tensor is not written.
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, int x, int y, int z, uint32_t src)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(src)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+
+// All but the last N stores of this thread have read their shared memory.
+template <int N>
+__device__ __forceinline__ void tma_store_wait()
+{
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+}
+
 // ---- tensor memory and products -------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ void tmem_alloc(uint32_t slot, uint32_t columns)  // by one whole warp
@@ -109,30 +124,66 @@ __host__ __device__ constexpr uint32_t mma_idesc(int n, bool a_mn, bool b_mn)
            ((128u >> 4) << 24);
 }
 
-// Shared-memory descriptor of a tile of 128-byte rows with 128-byte swizzle, its base a multiple of 1024 bytes.  K-major: a row of
-// the operand is 64 elements of K, eight rows are 1024 bytes apart.  MN-major: a row is 64 elements along M or N at one k, eight k
-// are 1024 bytes apart, the next 64 along M or N `block` bytes.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn, uint32_t block)
+// Shared-memory descriptor of a tile, its base a multiple of 1024 bytes.  K-major: a row of the operand is `row` bytes of K, 128 or 64,
+// swizzled over 128 or 64 bytes, eight rows are 8 `row` apart.  MN-major: a row is 64 elements along M or N at one k (128 bytes, swizzled
+// so), eight k are 1024 bytes apart, the next 64 along M or N `block` bytes.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn, uint32_t row, uint32_t block)
 {
-    const uint64_t lead = mn ? (uint64_t)(block >> 4) : 1;
-    return (uint64_t)((addr & 0x3ffff) >> 4) | (lead << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+    const uint64_t lead = mn ? (uint64_t)(block >> 4) : 1, step = mn ? 1024 : 8 * row, swizzle = mn || row == 128 ? 2 : 4;
+    return (uint64_t)((addr & 0x3ffff) >> 4) | (lead << 16) | ((step >> 4) << 32) | (1ull << 46) | (swizzle << 61);
 }
 
-// 32 columns of the warp's 32 lanes of tensor memory (a warp reaches the lanes 32 (warp % 4) and up).
-__device__ __forceinline__ void tmem_load32(float (&v)[32], uint32_t addr)
+template <int N>
+__device__ __forceinline__ void more_registers()
 {
-    uint32_t r[32];
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+template <int N>
+__device__ __forceinline__ void fewer_registers()
+{
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+// 32 columns of the warp's 32 lanes of tensor memory (a warp reaches the lanes 32 (warp % 4) and up).  The registers hold them after
+// tmem_wait only; that they pass through it keeps their uses behind it.
+__device__ __forceinline__ void tmem_load32(uint32_t (&r)[32], uint32_t addr)
+{
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, "
         "%19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        :
+          "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
           "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
           "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
           "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(addr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+__device__ __forceinline__ void tmem_wait(uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 :
+          "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+          "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]),
+          "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]),
+          "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+                 :
+                 : "memory");
+}
+
+__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
+        "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::
+          "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+          "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+          "r"(r[30]), "r"(r[31]),
+          "r"(addr)
+        : "memory");
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 
 }  // namespace flashbev_sm100
