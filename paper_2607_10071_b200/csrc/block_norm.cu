@@ -48,102 +48,195 @@ struct NormParams {
     float scale, eps, inv_c;
 };
 
-// The eight elements of a thread: neighbours (VEC: 16-byte accesses; C a multiple of 8) or every team-th.
+// A thread's eight elements of a row, as four pairs for the two-wide instructions.  VEC 8: eight neighbours, 16-byte accesses; 2:
+// every team-th pair of neighbours; 1: every team-th element.
+struct Eight {
+    float2 p[4];
+};
+
 template <typename T>
 struct Raw {
     T v[kE];
 };
 
-template <typename T, bool VEC>
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ Eight eight(float v) { return {{both(v), both(v), both(v), both(v)}}; }
+
+// Column of element i
+template <int VEC>
+__device__ __forceinline__ int column(int i, int t, int team)
+{
+    return VEC == 8 ? t * 8 + i : (VEC == 2 ? 2 * (t + i / 2 * team) + i % 2 : t + i * team);
+}
+
+// Whether it is one of the row's
+template <int VEC>
+__device__ __forceinline__ bool has(int i, int t, int team, int C)
+{
+    return VEC == 8 ? t * 8 < C : column<VEC>(VEC == 2 ? i & ~1 : i, t, team) < C;
+}
+
+template <typename T, int VEC>
 __device__ __forceinline__ void read(Raw<T> &r, const T *row, int t, int team, int C)
 {
-    if constexpr (VEC) {
+    if constexpr (VEC == 8) {
         constexpr int Q = kE * (int)sizeof(T) / 16;
-        if (t * kE < C) {
+        if (t * 8 < C) {
             uint4 q[Q];
 #pragma unroll
-            for (int i = 0; i < Q; ++i) q[i] = reinterpret_cast<const uint4 *>(row + t * kE)[i];
+            for (int i = 0; i < Q; ++i) q[i] = reinterpret_cast<const uint4 *>(row + t * 8)[i];
             memcpy(r.v, q, sizeof(q));
         }
+    } else if constexpr (VEC == 2) {
+        using Pair = typename std::conditional<sizeof(T) == 4, uint2, uint32_t>::type;
+#pragma unroll
+        for (int i = 0; i < kE; i += 2)
+            if (has<2>(i, t, team, C)) {
+                const Pair q = *reinterpret_cast<const Pair *>(row + column<2>(i, t, team));
+                memcpy(r.v + i, &q, sizeof(q));
+            }
     } else {
 #pragma unroll
         for (int i = 0; i < kE; ++i)
-            if (t + i * team < C) r.v[i] = row[t + i * team];
+            if (has<1>(i, t, team, C)) r.v[i] = row[column<1>(i, t, team)];
     }
 }
 
-template <typename T, bool VEC>
-__device__ __forceinline__ void write(T *row, const float (&f)[kE], int t, int team, int C)
+template <typename T, int VEC>
+__device__ __forceinline__ void write(T *row, const Eight &f, int t, int team, int C)
 {
-    if constexpr (VEC) {
-        constexpr int Q = kE * (int)sizeof(T) / 16;
-        if (t * kE < C) {
-            Raw<T> r;
+    Raw<T> r;
 #pragma unroll
-            for (int i = 0; i < kE; ++i) r.v[i] = from_float<T>(f[i]);
+    for (int i = 0; i < 4; ++i) r.v[2 * i] = from_float<T>(f.p[i].x), r.v[2 * i + 1] = from_float<T>(f.p[i].y);
+    if constexpr (VEC == 8) {
+        constexpr int Q = kE * (int)sizeof(T) / 16;
+        if (t * 8 < C) {
             uint4 q[Q];
             memcpy(q, r.v, sizeof(q));
 #pragma unroll
-            for (int i = 0; i < Q; ++i) reinterpret_cast<uint4 *>(row + t * kE)[i] = q[i];
+            for (int i = 0; i < Q; ++i) reinterpret_cast<uint4 *>(row + t * 8)[i] = q[i];
         }
+    } else if constexpr (VEC == 2) {
+        using Pair = typename std::conditional<sizeof(T) == 4, uint2, uint32_t>::type;
+#pragma unroll
+        for (int i = 0; i < kE; i += 2)
+            if (has<2>(i, t, team, C)) {
+                Pair q;
+                memcpy(&q, r.v + i, sizeof(q));
+                *reinterpret_cast<Pair *>(row + column<2>(i, t, team)) = q;
+            }
     } else {
 #pragma unroll
         for (int i = 0; i < kE; ++i)
-            if (t + i * team < C) row[t + i * team] = from_float<T>(f[i]);
+            if (has<1>(i, t, team, C)) row[column<1>(i, t, team)] = r.v[i];
     }
 }
 
-// Whether element i of this thread is one of the row's
-template <bool VEC>
-__device__ __forceinline__ bool has(int i, int t, int team, int C)
+// To float; with VEC 2 and 1 elements behind the row's end are 0 (with 8 a thread has all of its elements or none, and its sums are masked)
+template <typename T, int VEC>
+__device__ __forceinline__ void widen(Eight &f, const Raw<T> &r, int t, int team, int C)
 {
-    return VEC ? t * kE < C : t + i * team < C;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f.p[i] = make_float2(to_float(r.v[2 * i]), to_float(r.v[2 * i + 1]));
+        if (VEC != 8 && !has<VEC>(2 * i, t, team, C)) f.p[i].x = 0.0f;
+        if (VEC != 8 && !has<VEC>(2 * i + 1, t, team, C)) f.p[i].y = 0.0f;
+    }
+}
+
+__device__ __forceinline__ Eight operator+(const Eight &a, const Eight &b)
+{
+    Eight r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.p[i] = __fadd2_rn(a.p[i], b.p[i]);
+    return r;
+}
+
+__device__ __forceinline__ Eight operator*(const Eight &a, const Eight &b)
+{
+    Eight r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.p[i] = __fmul2_rn(a.p[i], b.p[i]);
+    return r;
+}
+
+__device__ __forceinline__ Eight fma(const Eight &a, const Eight &b, const Eight &c)
+{
+    Eight r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.p[i] = __ffma2_rn(a.p[i], b.p[i], c.p[i]);
+    return r;
+}
+
+__device__ __forceinline__ float total(const Eight &a)
+{
+    const float2 s = __fadd2_rn(__fadd2_rn(a.p[0], a.p[1]), __fadd2_rn(a.p[2], a.p[3]));
+    return s.x + s.y;
 }
 
 // The norms' parameters lie in shared memory as floats, `count` vectors one after another, 1 or 0 where there is none: in registers
 // they would be 32 of a thread, and of the gradients' kernel 72 with their sums.
-template <typename P>
+// (VEC 8: the first four of every eight, then the others, so that neighbouring threads read neighbouring 16 bytes)
+template <int VEC>
+__device__ __forceinline__ int param_at(int c, int C)
+{
+    return VEC == 8 ? (c / 4 % 2) * (C / 2) + c / 8 * 4 + c % 4 : c;
+}
+
+template <typename P, int VEC>
 __device__ __forceinline__ void stage_params(float *to, const void *const (&from)[4], int count, int C)
 {
     for (int j = 0; j < count; ++j)
         for (int c = threadIdx.x; c < C; c += blockDim.x)
-            to[j * C + c] = from[j] ? to_float(static_cast<const P *>(from[j])[c]) : (j % 2 ? 0.0f : 1.0f);
+            to[j * C + param_at<VEC>(c, C)] = from[j] ? to_float(static_cast<const P *>(from[j])[c]) : (j % 2 ? 0.0f : 1.0f);
     __syncthreads();
 }
 
-template <bool VEC>
-__device__ __forceinline__ void read_param(float (&f)[kE], const float *p, int t, int team, int C)
+template <int VEC>
+__device__ __forceinline__ Eight read_param(const float *p, int t, int team, int C)
 {
-    if constexpr (VEC) {
-        const float4 *const q = reinterpret_cast<const float4 *>(p + (t * kE < C ? t * kE : 0));
-        const float4 a = q[0], b = q[1];
-        f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+    Eight r;
+    if constexpr (VEC == 8) {
+        const float *const q = p + (t * 8 < C ? t * 4 : 0);
+        const float4 a = *reinterpret_cast<const float4 *>(q), b = *reinterpret_cast<const float4 *>(q + C / 2);
+        r.p[0] = make_float2(a.x, a.y), r.p[1] = make_float2(a.z, a.w), r.p[2] = make_float2(b.x, b.y), r.p[3] = make_float2(b.z, b.w);
     } else {
 #pragma unroll
-        for (int i = 0; i < kE; ++i) f[i] = p[t + i * team < C ? t + i * team : 0];
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (VEC == 2)  // (C is even, and with it every vector's start)
+                r.p[i] = *reinterpret_cast<const float2 *>(p + (has<2>(2 * i, t, team, C) ? column<2>(2 * i, t, team) : 0));
+            else
+                r.p[i] = make_float2(p[has<1>(2 * i, t, team, C) ? column<1>(2 * i, t, team) : 0],
+                                     p[has<1>(2 * i + 1, t, team, C) ? column<1>(2 * i + 1, t, team) : 0]);
+        }
     }
+    return r;
 }
 
-// The gate of row `g`, times the scale.  It is read for every row (from L1, where rows share it).
-template <typename P, bool VEC>
-__device__ __forceinline__ void read_gate(float (&f)[kE], const void *gate, long long g, float scale, int t, int team, int C)
+// The gate of row `g` of them, times the scale
+template <typename P, int VEC>
+__device__ __forceinline__ Eight read_gate(const void *gate, long long g, float scale, int t, int team, int C)
 {
+    if (!gate) return eight(scale);
     Raw<P> r;
-    if (gate) read<P, VEC>(r, static_cast<const P *>(gate) + g * C, t, team, C);
-#pragma unroll
-    for (int i = 0; i < kE; ++i) f[i] = gate ? (has<VEC>(i, t, team, C) ? scale * to_float(r.v[i]) : 0.0f) : scale;
+    read<P, VEC>(r, static_cast<const P *>(gate) + g * C, t, team, C);
+    Eight f;
+    widen<P, VEC>(f, r, t, team, C);
+    return f * eight(scale);
 }
 
 // Sums over a team.  WIDE: teams of several warps.
 template <bool WIDE>
 struct Team {
     int threads, t, slot;       // threads of a team; this one's place in it; the team's place in the block
+    bool mine;                  // VEC 8: this thread has a part of the row
     float2 *shared;             // WIDE: [2][32] of this team
     int turn;
 
     __device__ __forceinline__ float2 sum(float a, float b)
     {
         const int most = WIDE ? 16 : threads / 2;
+        if (!mine) a = b = 0.0f;
 #pragma unroll
         for (int d = 16; d; d /= 2)
             if (d <= most) a += __shfl_xor_sync(0xffffffffu, a, d), b += __shfl_xor_sync(0xffffffffu, b, d);
@@ -154,16 +247,17 @@ struct Team {
             const int warps = threads / 32;
             if (t % 32 == 0) buf[t / 32] = make_float2(a, b);
             asm volatile("bar.sync %0, %1;" ::"r"(1 + slot), "r"(threads) : "memory");
-            const float2 v = t % 32 < warps ? buf[t % 32] : make_float2(0.0f, 0.0f);
+            const float2 v = t % 16 < warps ? buf[t % 16] : make_float2(0.0f, 0.0f);  // (both halves of a warp alike)
             a = v.x, b = v.y;
 #pragma unroll
-            for (int d = 16; d; d /= 2) a += __shfl_xor_sync(0xffffffffu, a, d), b += __shfl_xor_sync(0xffffffffu, b, d);
+            for (int d = 8; d; d /= 2) a += __shfl_xor_sync(0xffffffffu, a, d), b += __shfl_xor_sync(0xffffffffu, b, d);
         }
         return make_float2(a, b);
     }
     __device__ __forceinline__ float sum(float a)
     {
         const int most = WIDE ? 16 : threads / 2;
+        if (!mine) a = 0.0f;
 #pragma unroll
         for (int d = 16; d; d /= 2)
             if (d <= most) a += __shfl_xor_sync(0xffffffffu, a, d);
@@ -172,77 +266,77 @@ struct Team {
             turn ^= 1;
             if (t % 32 == 0) buf[t / 32].x = a;
             asm volatile("bar.sync %0, %1;" ::"r"(1 + slot), "r"(threads) : "memory");
-            a = t % 32 < threads / 32 ? buf[t % 32].x : 0.0f;
+            a = t % 16 < threads / 32 ? buf[t % 16].x : 0.0f;
 #pragma unroll
-            for (int d = 16; d; d /= 2) a += __shfl_xor_sync(0xffffffffu, a, d);
+            for (int d = 8; d; d /= 2) a += __shfl_xor_sync(0xffffffffu, a, d);
         }
         return a;
     }
 };
 
-// v becomes (v - mean) / deviation (or v / root mean square); returns 1 / deviation.  Elements behind the row's end are 0 before and after.
-template <bool VEC, bool WIDE>
-__device__ __forceinline__ float whiten(float (&v)[kE], int kind, const NormParams &p, Team<WIDE> &team)
+// Elements behind the row's end, of VEC 2 and 1, back to 0
+template <int VEC, bool WIDE>
+__device__ __forceinline__ void trim(Eight &v, const Team<WIDE> &team, int C)
 {
-    float s = 0.0f;
-    if (kind == FLASHBEV_NORM_LAYER) {
+    if (VEC == 8) return;
 #pragma unroll
-        for (int i = 0; i < kE; ++i) s += v[i];
-        const float mean = team.sum(s) * p.inv_c;
-#pragma unroll
-        for (int i = 0; i < kE; ++i) v[i] = has<VEC>(i, team.t, team.threads, p.C) ? v[i] - mean : 0.0f;
+    for (int i = 0; i < 4; ++i) {
+        if (!has<VEC>(2 * i, team.t, team.threads, C)) v.p[i].x = 0.0f;
+        if (!has<VEC>(2 * i + 1, team.t, team.threads, C)) v.p[i].y = 0.0f;
     }
-    s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kE; ++i) s = fmaf(v[i], v[i], s);
-    const float r = 1.0f / sqrtf(team.sum(s) * p.inv_c + p.eps);
-#pragma unroll
-    for (int i = 0; i < kE; ++i) v[i] *= r;
+}
+
+// v becomes (v - mean) / deviation (or v / root mean square); returns 1 / deviation.
+template <int VEC, bool WIDE>
+__device__ __forceinline__ float whiten(Eight &v, int kind, const NormParams &p, Team<WIDE> &team)
+{
+    if (kind == FLASHBEV_NORM_LAYER) {
+        v = v + eight(-team.sum(total(v)) * p.inv_c);
+        trim<VEC>(v, team, p.C);
+    }
+    const float r = rsqrtf(fmaf(team.sum(total(v * v)), p.inv_c, p.eps));
+    v = v * eight(r);
     return r;
 }
 
 // Gradient at the input of `whiten` from that at its result t: r (g - mean(g) - t mean(g t)), without mean(g) for root mean squares.
-template <bool VEC, bool WIDE>
-__device__ __forceinline__ void whiten_back(float (&g)[kE], const float (&t)[kE], float r, int kind, const NormParams &p, Team<WIDE> &team)
+template <int VEC, bool WIDE>
+__device__ __forceinline__ void whiten_back(Eight &g, const Eight &t, float r, int kind, const NormParams &p, Team<WIDE> &team)
 {
-    float a = 0.0f, b = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kE; ++i) a += g[i], b = fmaf(g[i], t[i], b);
-    const float2 s = team.sum(a, b);
-    const float mean = kind == FLASHBEV_NORM_LAYER ? s.x * p.inv_c : 0.0f, along = s.y * p.inv_c;
-#pragma unroll
-    for (int i = 0; i < kE; ++i) g[i] = has<VEC>(i, team.t, team.threads, p.C) ? r * (g[i] - mean - t[i] * along) : 0.0f;
+    if (kind == FLASHBEV_NORM_LAYER) {
+        const float2 s = team.sum(total(g), total(g * t));
+        g = fma(t, eight(-s.y * p.inv_c), g + eight(-s.x * p.inv_c));
+        trim<VEC>(g, team, p.C);
+    } else {
+        g = fma(t, eight(-team.sum(total(g * t)) * p.inv_c), g);
+    }
+    g = g * eight(r);
 }
 
-template <bool WIDE>
+template <int VEC, bool WIDE>
 __device__ __forceinline__ Team<WIDE> make_team(const NormParams &p, float2 *shared)
 {
     Team<WIDE> team;
     team.threads = p.team, team.slot = threadIdx.x / p.team, team.t = threadIdx.x % p.team, team.turn = 0;
+    team.mine = VEC != 8 || team.t * 8 < p.C;
     team.shared = shared + (WIDE ? 64 * team.slot : 0);
     return team;
 }
 
-template <typename T, bool VEC>
-__device__ __forceinline__ void widen(float (&f)[kE], const Raw<T> &r, int t, int team, int C)
-{
-#pragma unroll
-    for (int i = 0; i < kE; ++i) f[i] = has<VEC>(i, t, team, C) ? to_float(r.v[i]) : 0.0f;
-}
-
 constexpr int kMostThreads = FLASHBEV_NORM_MAX_CHANNELS / kE;
+static_assert(kMostThreads <= 512, "the sums of a team's warps are added up by half a warp");
 
 // S, T, P: types of x and h, of y and n, of the parameters.
-template <typename S, typename T, typename P, bool VEC, bool WIDE>
+template <typename S, typename T, typename P, int VEC, bool WIDE>
 __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 3) norm_kernel(const __grid_constant__ NormParams p)
 {
     __shared__ float2 shared[WIDE ? 64 * 4 : 1];  // (at most four teams of 64 threads in a block)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
-    Team<WIDE> team = make_team<WIDE>(p, shared);
+    Team<WIDE> team = make_team<VEC, WIDE>(p, shared);
     const int t = team.t, threads = p.team, C = p.C, teams = blockDim.x / threads;
     extern __shared__ __align__(16) float params[];  // before weight, before bias, after weight, after bias
-    stage_params<P>(params, {p.wb, p.bb, p.wa, p.ba}, p.after != FLASHBEV_NORM_NONE ? 4 : 2, C);
+    stage_params<P, VEC>(params, {p.wb, p.bb, p.wa, p.ba}, p.after != FLASHBEV_NORM_NONE ? 4 : 2, C);
     const long long step = (long long)gridDim.x * teams, first = (long long)blockIdx.x * teams + team.slot;
     // (narrow teams share a warp's shuffles: all of them go as long as one has a row)
     const long long lead = WIDE ? first : first - (threadIdx.x % 32) / threads;
@@ -254,41 +348,31 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 3) norm_
         if (p.y) read<T, VEC>(yr, static_cast<const T *>(p.y) + row * p.ld_y, t, threads, C);
     };
     bring(first);
+    Eight gate = eight(p.scale);
+    long long gate_end = 0;  // the row behind the last one with this gate
     for (long long row = first, at = lead; at < p.rows; row += step, at += step) {
         const bool live = row < p.rows;
-        float h[kE], m[kE];
-        widen<S, VEC>(h, xr, t, threads, live ? C : 0);
-        if (p.y) widen<T, VEC>(m, yr, t, threads, live ? C : 0);
+        Eight h, m;
+        widen<S, VEC>(h, xr, t, threads, C);
+        if (p.y) widen<T, VEC>(m, yr, t, threads, C);
         bring(row + step);
         if (p.y) {
             if (p.after != FLASHBEV_NORM_NONE) {
                 whiten<VEC, WIDE>(m, p.after, p, team);
-                float w[kE], b[kE];
-                read_param<VEC>(w, params + 2 * C, t, threads, C);
-                read_param<VEC>(b, params + 3 * C, t, threads, C);
-#pragma unroll
-                for (int i = 0; i < kE; ++i) m[i] = fmaf(m[i], w[i], b[i]);
+                m = fma(m, read_param<VEC>(params + 2 * C, t, threads, C), read_param<VEC>(params + 3 * C, t, threads, C));
             }
-            if (p.gate) {
-                float gate[kE];
-                read_gate<P, VEC>(gate, p.gate, live ? (int)row / (int)p.per_gate : 0, p.scale, t, threads, C);
-#pragma unroll
-                for (int i = 0; i < kE; ++i) m[i] *= gate[i];
-            } else {
-#pragma unroll
-                for (int i = 0; i < kE; ++i) m[i] *= p.scale;
+            if (p.gate && live && row >= gate_end) {
+                const long long g = (int)row / (int)p.per_gate;
+                gate = read_gate<P, VEC>(p.gate, g, p.scale, t, threads, C);
+                gate_end = (g + 1) * p.per_gate;
             }
-#pragma unroll
-            for (int i = 0; i < kE; ++i) h[i] = has<VEC>(i, t, threads, C) ? h[i] + m[i] : 0.0f;
+            h = fma(m, gate, h);
             if (p.h && live) write<S, VEC>(static_cast<S *>(p.h) + row * p.ld_h, h, t, threads, C);
         }
         if (p.before != FLASHBEV_NORM_NONE) {
+            trim<VEC>(h, team, C);  // (of the norm's bias)
             whiten<VEC, WIDE>(h, p.before, p, team);
-            float w[kE], b[kE];
-            read_param<VEC>(w, params, t, threads, C);
-            read_param<VEC>(b, params + C, t, threads, C);
-#pragma unroll
-            for (int i = 0; i < kE; ++i) h[i] = fmaf(h[i], w[i], b[i]);
+            h = fma(h, read_param<VEC>(params, t, threads, C), read_param<VEC>(params + C, t, threads, C));
             if (live) write<T, VEC>(static_cast<T *>(p.n) + row * p.ld_n, h, t, threads, C);
         }
     }
@@ -297,20 +381,19 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 3) norm_
 // Gradients.  The rows of a gate are shared by `chunks` blocks, whose teams take every so manieth row; sums over rows stay in
 // registers until the block's end, when they are added up over its teams in a fixed order.  `direct`: there are many gates with few rows, and a
 // team takes the rows of one gate after another and writes the gate's gradient itself.
-template <typename S, typename T, typename P, bool VEC, bool WIDE>
+template <typename S, typename T, typename P, int VEC, bool WIDE>
 __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 2) norm_backward_kernel(const __grid_constant__ NormParams p)
 {
     __shared__ float2 shared[WIDE ? 64 * 4 : 1];
     __shared__ float joined[2048];  // [teams (warps, where a warp has several)][C]
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
-    Team<WIDE> team = make_team<WIDE>(p, shared);
+    Team<WIDE> team = make_team<VEC, WIDE>(p, shared);
     const int t = team.t, threads = p.team, C = p.C, teams = blockDim.x / threads;
     extern __shared__ __align__(16) float params[];  // before weight, after bias, after weight
-    stage_params<P>(params, {p.wb, p.ba, p.wa, nullptr}, p.after != FLASHBEV_NORM_NONE ? 3 : 1, C);
-    float dwa[kE], dba[kE], dwb[kE], dbb[kE], dg[kE];
-#pragma unroll
-    for (int i = 0; i < kE; ++i) dwa[i] = dba[i] = dwb[i] = dbb[i] = dg[i] = 0.0f;
+    const int vectors = p.after != FLASHBEV_NORM_NONE ? 3 : 1;
+    stage_params<P, VEC>(params, {p.wb, p.ba, p.wa, nullptr}, vectors, C);
+    Eight dwa = eight(0.0f), dba = dwa, dwb = dwa, dbb = dwa, dg = dwa;
 
     const int inside = WIDE ? 0 : (threadIdx.x % 32) / threads;  // place of the team in its warp
     long long g, g_step, g_lead;
@@ -321,20 +404,19 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 2) norm_
         g = g_lead = blockIdx.x / p.chunks, g_step = p.gates;
     }
     for (; g_lead < p.gates; g += g_step, g_lead += g_step) {
-        long long row, end, step, lead;
+        long long row, end, step;
         const bool mine = g < p.gates;
         if (p.direct) {
             row = g * p.per_gate, end = mine ? row + p.per_gate : 0, step = 1;
-            lead = 0;
         } else {
             const int chunk = (int)(blockIdx.x - g * p.chunks);
             const long long base = g * p.per_gate, share = (p.per_gate + p.chunks - 1) / p.chunks;
             end = base + min(p.per_gate, (chunk + 1) * share);
             row = base + chunk * share + team.slot, step = teams;
-            lead = 0;
         }
         // every team of a warp goes around as often
         const long long rounds = p.direct ? p.per_gate : (end - (row - inside) + step - 1) / step;
+        const Eight gate = read_gate<P, VEC>(p.gate, mine ? g : 0, p.scale, t, threads, C);
         Raw<S> xr, ghr;
         Raw<T> yr, gnr;
         const auto bring = [&](long long at) {
@@ -345,92 +427,52 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 2) norm_
             if (p.gh) read<S, VEC>(ghr, static_cast<const S *>(p.gh) + at * p.ld_gh, t, threads, C);
         };
         bring(row);
-        for (; lead < rounds; ++lead, row += step) {
+        for (long long round = 0; round < rounds; ++round, row += step) {
             const bool live = row < end;
-            const int have = live ? C : 0;
-            float u[kE], v[kE], gn[kE], gh[kE];
-            widen<S, VEC>(u, xr, t, threads, have);
-            if (p.y) widen<T, VEC>(v, yr, t, threads, have);
-            if (p.gn) widen<T, VEC>(gn, gnr, t, threads, have);
-            if (p.gh) {
-                widen<S, VEC>(gh, ghr, t, threads, have);
-            } else {
-#pragma unroll
-                for (int i = 0; i < kE; ++i) gh[i] = 0.0f;
-            }
+            Eight u, v, gn, gh = eight(0.0f);
+            widen<S, VEC>(u, xr, t, threads, C);
+            if (p.y) widen<T, VEC>(v, yr, t, threads, C);
+            if (p.gn) widen<T, VEC>(gn, gnr, t, threads, C);
+            if (p.gh) widen<S, VEC>(gh, ghr, t, threads, C);
             bring(row + step);
             // after(y), of which v keeps the part without the parameters
-            const auto branch = [&](float (&m)[kE]) {
-                if (p.after != FLASHBEV_NORM_NONE) {
-                    float w[kE], b[kE];
-                    read_param<VEC>(w, params + 2 * C, t, threads, C);
-                    read_param<VEC>(b, params + C, t, threads, C);
-#pragma unroll
-                    for (int i = 0; i < kE; ++i) m[i] = fmaf(v[i], w[i], b[i]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < kE; ++i) m[i] = v[i];
-                }
+            const auto branch = [&]() -> Eight {
+                if (p.after == FLASHBEV_NORM_NONE) return v;
+                return fma(v, read_param<VEC>(params + 2 * C, t, threads, C), read_param<VEC>(params + C, t, threads, C));
             };
             float ra = 0.0f;
             if (p.after != FLASHBEV_NORM_NONE) ra = whiten<VEC, WIDE>(v, p.after, p, team);
             if (p.before != FLASHBEV_NORM_NONE) {
                 if (p.y) {
-                    float m[kE], gate[kE];
-                    branch(m);
-                    read_gate<P, VEC>(gate, p.gate, mine ? g : 0, p.scale, t, threads, C);
-#pragma unroll
-                    for (int i = 0; i < kE; ++i) u[i] = has<VEC>(i, t, threads, have) ? fmaf(m[i], gate[i], u[i]) : 0.0f;
+                    u = fma(branch(), gate, u);
+                    trim<VEC>(u, team, C);
                 }
                 const float rb = whiten<VEC, WIDE>(u, p.before, p, team);
-                float w[kE];
-                read_param<VEC>(w, params, t, threads, C);
-#pragma unroll
-                for (int i = 0; i < kE; ++i) {
-                    dwb[i] = fmaf(gn[i], u[i], dwb[i]), dbb[i] += gn[i];
-                    gn[i] *= w[i];
-                }
+                if (live) dwb = fma(gn, u, dwb), dbb = dbb + gn;
+                gn = gn * read_param<VEC>(params, t, threads, C);
                 whiten_back<VEC, WIDE>(gn, u, rb, p.before, p, team);
-                if (live)
-#pragma unroll
-                    for (int i = 0; i < kE; ++i) gh[i] += gn[i];
+                gh = gh + gn;
             }
             if (p.gx && live) write<S, VEC>(static_cast<S *>(p.gx) + row * p.ld_gx, gh, t, threads, C);
             if (!p.y) continue;
-            if (live && p.ggate) {
-                float m[kE];
-                branch(m);
-#pragma unroll
-                for (int i = 0; i < kE; ++i) dg[i] = fmaf(gh[i] * p.scale, m[i], dg[i]);
-            }
-            {
-                float gate[kE];
-                read_gate<P, VEC>(gate, p.gate, mine ? g : 0, p.scale, t, threads, C);
-#pragma unroll
-                for (int i = 0; i < kE; ++i) gh[i] *= gate[i];
-            }
+            if (live && p.ggate) dg = fma(gh * eight(p.scale), branch(), dg);
+            gh = gh * gate;
             if (p.after != FLASHBEV_NORM_NONE) {
-                float w[kE];
-                read_param<VEC>(w, params + 2 * C, t, threads, C);
-#pragma unroll
-                for (int i = 0; i < kE; ++i) {
-                    if (live) dwa[i] = fmaf(gh[i], v[i], dwa[i]), dba[i] += gh[i];
-                    gh[i] *= w[i];
-                }
+                if (live) dwa = fma(gh, v, dwa), dba = dba + gh;
+                gh = gh * read_param<VEC>(params + 2 * C, t, threads, C);
                 whiten_back<VEC, WIDE>(gh, v, ra, p.after, p, team);
             }
             if (p.gy && live) write<T, VEC>(static_cast<T *>(p.gy) + row * p.ld_gy, gh, t, threads, C);
         }
         if (p.direct) {
             if (p.ggate && mine) write<P, VEC>(static_cast<P *>(p.ggate) + g * C, dg, t, threads, C);
-#pragma unroll
-            for (int i = 0; i < kE; ++i) dg[i] = 0.0f;
+            dg = eight(0.0f);
         }
     }
     // sums over the block's teams, one array after another
     long long array = 0;
     const int slots = WIDE ? teams : blockDim.x / 32, slot = WIDE ? team.slot : threadIdx.x / 32;
-    const auto put = [&](float (&d)[kE], int bit) {
+    const auto put = [&](Eight &d, int bit) {
         if (!(p.want >> bit & 1)) return;
         float *const out = p.sums + (array++ * gridDim.x + blockIdx.x) * (long long)C;
         if (!WIDE) {
@@ -438,14 +480,20 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 2) norm_
             for (int s = 16; s; s /= 2)
                 if (s >= threads)
 #pragma unroll
-                    for (int i = 0; i < kE; ++i) d[i] += __shfl_xor_sync(0xffffffffu, d[i], s);
+                    for (int i = 0; i < 4; ++i)
+                        d.p[i].x += __shfl_xor_sync(0xffffffffu, d.p[i].x, s), d.p[i].y += __shfl_xor_sync(0xffffffffu, d.p[i].y, s);
         }
+        const auto scatter = [&](float *to) {  // (any alignment)
+#pragma unroll
+            for (int i = 0; i < kE; ++i)
+                if (has<VEC>(i, t, threads, C)) to[column<VEC>(i, t, threads)] = i % 2 ? d.p[i / 2].y : d.p[i / 2].x;
+        };
         if (slots == 1) {
-            write<float, false>(out, d, VEC ? t * kE : t, VEC ? 1 : threads, C);
+            scatter(out);
             return;
         }
         __syncthreads();  // (the array before has been read)
-        if (WIDE || inside == 0) write<float, false>(joined + slot * C, d, VEC ? t * kE : t, VEC ? 1 : threads, C);
+        if (WIDE || inside == 0) scatter(joined + slot * C);
         __syncthreads();
         for (int c = threadIdx.x; c < C; c += blockDim.x) {
             float s = 0.0f;
@@ -493,7 +541,6 @@ __global__ void __launch_bounds__(512) norm_sum_kernel(const float *__restrict__
 bool dtype_ok(int d) { return d == FLASHBEV_F32 || d == FLASHBEV_BF16; }
 size_t elem_size(int d) { return d == FLASHBEV_F32 ? 4 : 2; }
 bool aligned(const void *p, int dtype) { return (uintptr_t)p % elem_size(dtype) == 0; }
-bool whole(const void *p, long long ld, int dtype) { return ((uintptr_t)p | (uintptr_t)(ld * (long long)elem_size(dtype))) % 16 == 0; }
 long long dense(long long ld, int C) { return ld ? ld : C; }
 
 int team_threads(int C)
@@ -565,20 +612,21 @@ flashbev_status check_backward(const flashbev_block_norm_backward_params *p)
 }
 
 // The instance for the call's types, alignment and width.
-template <bool BACKWARD, typename S, typename T, typename P>
-auto pick(bool vec, bool wide)
+template <bool BACKWARD, typename S, typename T, typename P, int VEC>
+auto pick(bool wide)
 {
-    if constexpr (BACKWARD) {
-        if (vec) return wide ? norm_backward_kernel<S, T, P, true, true> : norm_backward_kernel<S, T, P, true, false>;
-        return wide ? norm_backward_kernel<S, T, P, false, true> : norm_backward_kernel<S, T, P, false, false>;
-    } else {
-        if (vec) return wide ? norm_kernel<S, T, P, true, true> : norm_kernel<S, T, P, true, false>;
-        return wide ? norm_kernel<S, T, P, false, true> : norm_kernel<S, T, P, false, false>;
-    }
+    if constexpr (BACKWARD) return wide ? norm_backward_kernel<S, T, P, VEC, true> : norm_backward_kernel<S, T, P, VEC, false>;
+    else return wide ? norm_kernel<S, T, P, VEC, true> : norm_kernel<S, T, P, VEC, false>;
+}
+
+template <bool BACKWARD, typename S, typename T, typename P>
+auto pick(int vec, bool wide)
+{
+    return vec == 8 ? pick<BACKWARD, S, T, P, 8>(wide) : (vec == 2 ? pick<BACKWARD, S, T, P, 2>(wide) : pick<BACKWARD, S, T, P, 1>(wide));
 }
 
 template <bool BACKWARD>
-cudaError_t launch_norm(const NormParams &k, int dtype, int branch, int param, bool vec, unsigned blocks, int threads, cudaStream_t stream)
+cudaError_t launch_norm(const NormParams &k, int dtype, int branch, int param, int vec, unsigned blocks, int threads, cudaStream_t stream)
 {
     const bool wide = k.team > 32;
     void (*kernel)(NormParams);
@@ -595,6 +643,19 @@ cudaError_t launch_norm(const NormParams &k, int dtype, int branch, int param, b
     }
     return launch_dependent(kernel, dim3(blocks), dim3((unsigned)threads), smem, stream, k);
 }
+
+// Elements that a thread can take at once: 8 or 2 neighbours where every row starts on their boundary, else one.
+struct Alignment {
+    int vec;
+    explicit Alignment(int C) : vec(C % 8 == 0 ? 8 : (C % 2 == 0 ? 2 : 1)) {}
+    void rows(const void *p, long long ld, int dtype)
+    {
+        if (!p) return;
+        const uintptr_t bits = (uintptr_t)p | (uintptr_t)(ld * (long long)elem_size(dtype));
+        if (vec == 8 && bits % 16) vec = 2;
+        if (vec == 2 && bits % (2 * elem_size(dtype))) vec = 1;
+    }
+};
 
 // Blocks and rows of a backward call.
 struct BackwardShape {
@@ -647,18 +708,18 @@ flashbev_status flashbev_block_norm(const flashbev_block_norm_params *p, void *s
     k.ld_x = dense(p->ld_x, p->C), k.ld_y = dense(p->ld_y, p->C), k.ld_h = dense(p->ld_h, p->C), k.ld_n = dense(p->ld_n, p->C);
     k.C = p->C, k.after = p->after, k.before = p->before, k.scale = (float)p->scale, k.eps = (float)p->eps, k.inv_c = 1.0f / (float)p->C;
     k.team = team_threads(p->C);
-    bool vec = p->C % kE == 0 && whole(p->x, k.ld_x, p->dtype) && (!p->y || whole(p->y, k.ld_y, p->branch_dtype)) &&
-               (!p->h || whole(p->h, k.ld_h, p->dtype)) && (!p->n || whole(p->n, k.ld_n, p->branch_dtype));
-    vec = vec && (uintptr_t)p->gate % 16 == 0;
+    Alignment al(p->C);
+    al.rows(p->x, k.ld_x, p->dtype), al.rows(p->h, k.ld_h, p->dtype), al.rows(p->y, k.ld_y, p->branch_dtype), al.rows(p->n, k.ld_n, p->branch_dtype);
+    al.rows(p->gate, p->C, p->param_dtype);
     const int threads = std::max(256, k.team), teams = threads / k.team;
     const long long blocks = std::min<long long>((p->rows + teams - 1) / teams, (long long)sm_count() * (threads > 512 ? 2 : 6));
-    const cudaError_t e = launch_norm<false>(k, p->dtype, p->branch_dtype, p->param_dtype, vec, (unsigned)blocks, threads, static_cast<cudaStream_t>(stream));
+    const cudaError_t e = launch_norm<false>(k, p->dtype, p->branch_dtype, p->param_dtype, al.vec, (unsigned)blocks, threads, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess || cudaGetLastError() != cudaSuccess) {
         cudaGetLastError();
         return FLASHBEV_CUDA_ERROR;
     }
     t_last_launches = 1;
-    t_last_kernel = vec ? "block_norm" : "block_norm_scalar";
+    t_last_kernel = al.vec == 8 ? "block_norm" : (al.vec == 2 ? "block_norm_pairs" : "block_norm_scalar");
     return FLASHBEV_OK;
 }
 
@@ -694,11 +755,11 @@ flashbev_status flashbev_block_norm_backward(const flashbev_block_norm_backward_
     k.ld_gx = dense(p->ld_grad_x, p->C), k.ld_gy = dense(p->ld_grad_y, p->C);
     k.C = p->C, k.after = p->after, k.before = p->before, k.scale = (float)p->scale, k.eps = (float)p->eps, k.inv_c = 1.0f / (float)p->C;
     k.team = s.team;
-    bool vec = p->C % kE == 0 && whole(p->x, k.ld_x, p->dtype) && (!p->y || whole(p->y, k.ld_y, p->branch_dtype)) &&
-               (!p->grad_h || whole(p->grad_h, k.ld_gh, p->dtype)) && (!p->grad_n || whole(p->grad_n, k.ld_gn, p->branch_dtype)) &&
-               (!p->grad_x || whole(p->grad_x, k.ld_gx, p->dtype)) && (!p->grad_y || whole(p->grad_y, k.ld_gy, p->branch_dtype));
-    vec = vec && (uintptr_t)p->gate % 16 == 0 && (uintptr_t)p->grad_gate % 16 == 0;
-    cudaError_t e = launch_norm<true>(k, p->dtype, p->branch_dtype, p->param_dtype, vec, (unsigned)s.blocks, s.threads, stream);
+    Alignment al(p->C);
+    al.rows(p->x, k.ld_x, p->dtype), al.rows(p->grad_h, k.ld_gh, p->dtype), al.rows(p->grad_x, k.ld_gx, p->dtype);
+    al.rows(p->y, k.ld_y, p->branch_dtype), al.rows(p->grad_n, k.ld_gn, p->branch_dtype), al.rows(p->grad_y, k.ld_gy, p->branch_dtype);
+    al.rows(p->gate, p->C, p->param_dtype), al.rows(p->grad_gate, p->C, p->param_dtype);
+    cudaError_t e = launch_norm<true>(k, p->dtype, p->branch_dtype, p->param_dtype, al.vec, (unsigned)s.blocks, s.threads, stream);
     int launches = 1;
     if (e == cudaSuccess && s.arrays) {
         SumJobs q = {};
@@ -718,7 +779,7 @@ flashbev_status flashbev_block_norm_backward(const flashbev_block_norm_backward_
         return FLASHBEV_CUDA_ERROR;
     }
     t_last_launches = launches;
-    t_last_kernel = vec ? "block_norm_backward" : "block_norm_backward_scalar";
+    t_last_kernel = al.vec == 8 ? "block_norm_backward" : (al.vec == 2 ? "block_norm_backward_pairs" : "block_norm_backward_scalar");
     return FLASHBEV_OK;
 }
 

@@ -6,9 +6,13 @@
 //     grad_x      = dz      weight       A = dz (K-major),      B = weight^T (contiguous along N: MN-major)
 //     grad_weight = dz^T    x            A = dz^T (MN-major),   B = x^T      (MN-major)
 //
-// persistent CTAs, one per SM: a producer fills a ring of shared-memory stages (64 of K each), one thread issues the products into
-// one half of tensor memory, eight warps take the other half through bias, activation and residual to global memory.  In every
-// tile, operands are 128-byte rows of 64 bf16 numbers with 128-byte swizzle, whether a row runs along K or along M or N.
+// persistent CTAs, one per SM: one thread fills a ring of shared-memory stages by TMA, one issues the products into
+// tensor memory, and 8 or 16 warps take finished sums from there through bias, activation and residual to global memory.  In every tile,
+// operands are rows of bf16 numbers with the swizzle of TMA, whether a row runs along K or along M or N.
+//
+// Operands that TMA cannot read so -- float32 ones, which become three bf16 pieces, and bf16 ones whose rows are no whole 16-byte vectors
+// -- are laid out in the caller's scratch by a kernel ahead of the product.  (Sixteen warps that load, split and store the stages in the product itself
+// were bound by the latency of what they can have in flight: 40000 x 1024 x 256, float32: 172 us, tensor cores busy for 39 %.)
 #include "flashbev.h"
 #include "launch.cuh"
 #include "tcgen05.cuh"
@@ -28,15 +32,8 @@ namespace {
 using bf16 = __nv_bfloat16;
 
 constexpr int kBM = 128;            // rows of a tile: the 128 lanes of tensor memory
-constexpr int kProducerWarps = 8;   // of the loaders without TMA: two groups of them, for every other stage
-constexpr int kSmemLimit = 227 * 1024 - 512;
-
-// How a stage is filled.
-enum Loader {
-    kTma = 0,     // bf16, 16-byte aligned rows: TMA
-    kCopy = 1,    // bf16 rows of any alignment: loads and shared-memory stores by 16 warps
-    kSplit = 2    // float32: the same warps take every number apart into three bf16 pieces
-};
+constexpr int kSmemLimit = 227 * 1024;
+constexpr int kControlBytes = 512;  // barriers and the like
 
 // Elements of float32 operands: x = p0 + p1 + p2, each piece the bf16 number nearest to what is left.  Every difference is exact and
 // 8 + 8 + 8 bits hold the 24 of x.  Of the nine products the three left out, p1 p2, p2 p1 and p2 p2, are below 2^-25 |a| |b|.  Two tf32
@@ -149,46 +146,49 @@ __device__ __forceinline__ void activate_all(float (&v)[N], int act)
     else if (act == FLASHBEV_ACT_SILU) activate<FAST, FLASHBEV_ACT_SILU>(v);
 }
 
-// g act'(z)
+// g act'(z).  Where the slope is 0 the product is, whatever g.
 template <bool FAST>
-__device__ __forceinline__ float slope_times(float g, float z, int act)
+__device__ __forceinline__ float2 slope_times(float2 g, float2 z, int act)
 {
-    if (act == FLASHBEV_ACT_RELU) return z > 0.0f ? g : 0.0f;
-    if (act == FLASHBEV_ACT_GELU) {
-        const float e = FAST ? __expf(-0.5f * z * z) : expf(-0.5f * z * z);
-        return g * fmaf(z * 0.39894228f, e, normal_cdf<FAST>(z));
+    if (act == FLASHBEV_ACT_RELU) return make_float2(z.x > 0.0f ? g.x : 0.0f, z.y > 0.0f ? g.y : 0.0f);
+    if (act == FLASHBEV_ACT_GELU) {  // Phi(z) + z phi(z)
+        float2 cdf, e = __fmul2_rn(__fmul2_rn(z, z), both(FAST ? -0.5f * 1.44269504f : -0.5f));
+        if constexpr (FAST) {
+            const float2 s = normal_tail(make_float2(fabsf(z.x), fabsf(z.y)), z);
+            cdf = make_float2(z.x < 0.0f ? s.x : 1.0f - s.x, z.y < 0.0f ? s.y : 1.0f - s.y);
+            e.x = exp2_approx(e.x), e.y = exp2_approx(e.y);
+        } else {
+            cdf = make_float2(normal_cdf<false>(z.x), normal_cdf<false>(z.y));
+            e.x = expf(e.x), e.y = expf(e.y);
+        }
+        return __fmul2_rn(g, __ffma2_rn(__fmul2_rn(z, both(0.39894228f)), e, cdf));
     }
     if (act == FLASHBEV_ACT_SILU) {
-        const float s = sigmoid<FAST>(z);
-        return g * s * fmaf(z, 1.0f - s, 1.0f);
+        const float2 s = make_float2(sigmoid<FAST>(z.x), sigmoid<FAST>(z.y));
+        return __fmul2_rn(__fmul2_rn(g, s), __ffma2_rn(z, __fadd2_rn(both(1.0f), make_float2(-s.x, -s.y)), both(1.0f)));
     }
     return g;
 }
 
 // ---- the product ------------------------------------------------------------------------------------------------------------
 
-// K of a stage: a swizzled row of 64 bf16 numbers, of pieces 32 (three tiles per operand, and a stage's numbers fit a thread's registers).
-__host__ __device__ constexpr int block_k(int loader) { return loader == kSplit ? 32 : 64; }
-// Warps of the epilogue: with TMA loads 16, as it is their latency that a short sum waits for (64-column sums of 184950 rows, 64 columns:
-// 25 us with eight).  The other loaders leave four, and have 16 to bring the stages.  (Registers are those of a quarter of an SM: the last warps of
-// four, which do nothing, cost none.)
-__host__ __device__ constexpr int epilogue_warps(int loader) { return loader == kTma ? 16 : 4; }
-__host__ __device__ constexpr int gemm_threads(int loader) { return 32 * (loader == kTma ? 20 : 8 + 2 * kProducerWarps); }
-// Registers of the warps without TMA: 768 threads x 80 = 128 x 152 (epilogue) + 128 x 40 (products) + 512 x 72
-constexpr int kEpilogueRegs = 152, kProductRegs = 40, kProducerRegs = 72;
-static_assert(128 * kEpilogueRegs + 128 * kProductRegs + 64 * kProducerWarps * kProducerRegs <= 32 * (8 + 2 * kProducerWarps) * 80, "");
+// pieces: 1 (bf16) or 3 (float32).  K of a stage: a swizzled row of 64 numbers, or of 32 where an operand has three tiles: three stages of 48 KB
+// (two of 96 KB: 59 us against 45 for 40000 x 256 x 256).
+__host__ __device__ constexpr int block_k(int pieces) { return pieces == 3 ? 32 : 64; }
+// Warps of the epilogue: 16, as it is their latency that a short sum waits for (64-column sums of 184950 rows, 64 columns: 25 us with eight,
+// 20 us with 16).  Three pieces are six times the products; they leave eight, and shared memory for a third stage.  (Registers are those of a
+// quarter of an SM: the last warps of four, which do nothing, cost none.)
+__host__ __device__ constexpr int epilogue_warps(int pieces) { return pieces == 3 ? 8 : 16; }
+__host__ __device__ constexpr int gemm_threads(int pieces) { return 32 * (epilogue_warps(pieces) + 4); }
 // Bytes behind the ring: a buffer of 32 rows x 128 bytes and a bias of 64 columns per epilogue warp.
-__host__ __device__ constexpr int epilogue_bytes(int loader) { return epilogue_warps(loader) * (4096 + 256); }
-__host__ __device__ constexpr int ring_bytes(int loader) { return (kSmemLimit - 1024 - epilogue_bytes(loader)) / 1024 * 1024; }
+__host__ __device__ constexpr int epilogue_bytes(int pieces) { return epilogue_warps(pieces) * (4096 + 256); }
+__host__ __device__ constexpr int ring_bytes(int pieces) { return (kSmemLimit - kControlBytes - epilogue_bytes(pieces)) / 1024 * 1024; }
 constexpr int kAccs = 4;            // most accumulators in tensor memory
 
 struct alignas(64) GemmParams {
-    CUtensorMap ta, tb;         // kTma
-    CUtensorMap tout, tpre;     // store_tma
-    const void *a, *b;          // the other loaders
-    long long lda, ldb;
+    CUtensorMap ta, tb;         // operands
+    CUtensorMap tout, tpre;     // results, with store_tma
     int a_mn, b_mn;             // the operand's rows run along M / N, one per k
-    int a_vec, b_vec;           // bytes that every row's start is a multiple of: 16, 4 or less
     int M, N, K;
     int bn, stages;             // columns of a tile; stages in the ring
     int tiles_n, tiles, kblocks, kshare, splits;  // a tile's sum is cut into `splits` of `kshare` blocks of K (the last may have fewer)
@@ -348,87 +348,6 @@ __device__ __forceinline__ void tile_leave(const unsigned char *tile, const CUte
     __syncwarp();
 }
 
-// An operand's tile without TMA.  It is made of rows of contiguous elements, `slow` of them per k (MN-major) or per m or n; a thread brings
-// pieces of eight elements.  Q: the piece's place in the tile.
-struct Piece {
-    int slow, fast, at;  // first element, relative to the tile's; byte offset of its bf16 numbers in the tile
-};
-
-template <int BK>
-__device__ __forceinline__ Piece piece_of_tile(int q, bool mn)
-{
-    Piece e;
-    if (mn) {  // blocks of 64 along M or N: BK rows of 128 bytes
-        const int block = q / (8 * BK), k = q / 8 % BK, c = q % 8;
-        e.slow = k, e.fast = 64 * block + 8 * c, e.at = (block * BK + k) * 128 + ((c ^ (k & 7)) << 4);
-    } else if (BK == 64) {
-        const int row = q / 8, c = q % 8;
-        e.slow = row, e.fast = 8 * c, e.at = row * 128 + ((c ^ (row & 7)) << 4);
-    } else {
-        const int row = q / 4, c = q % 4;
-        e.slow = row, e.fast = 8 * c, e.at = row * 64 + ((c ^ (row >> 1 & 3)) << 4);
-    }
-    return e;
-}
-
-// Where an operand's tile starts and what there is of it
-struct Source {
-    const void *base;
-    long long ld;
-    int slow0, fast0, slows, fasts, vec;
-};
-
-__device__ __forceinline__ Source source_of(const void *base, long long ld, bool mn, int vec, int mn0, int k0, int MN, int K)
-{
-    return {base, ld, mn ? k0 : mn0, mn ? mn0 : k0, mn ? K : MN, mn ? MN : K, vec};
-}
-
-__device__ __forceinline__ void piece_load(uint32_t (&w)[8], const Source &s, const Piece &e)  // float32
-{
-    const int slow = s.slow0 + e.slow, fast = s.fast0 + e.fast, have = slow < s.slows ? s.fasts - fast : 0;
-    const float *p = static_cast<const float *>(s.base) + slow * s.ld + fast;
-    if (s.vec >= 16 && have >= 8) {
-        const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p)), v = __ldg(reinterpret_cast<const uint4 *>(p) + 1);
-        w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w, w[4] = v.x, w[5] = v.y, w[6] = v.z, w[7] = v.w;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = i < have ? __float_as_uint(__ldg(p + i)) : 0;
-    }
-}
-
-__device__ __forceinline__ void piece_store(const uint32_t (&w)[8], unsigned char *tile, int tile_bytes, int at)
-{
-    uint32_t p0[4], p1[4], p2[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float2 v = make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
-        p0[i] = pack(v.x, v.y);
-        v = __fadd2_rn(v, make_float2(-low(p0[i]), -high(p0[i])));
-        p1[i] = pack(v.x, v.y);
-        v = __fadd2_rn(v, make_float2(-low(p1[i]), -high(p1[i])));
-        p2[i] = pack(v.x, v.y);
-    }
-    *reinterpret_cast<uint4 *>(tile + at) = make_uint4(p0[0], p0[1], p0[2], p0[3]);
-    *reinterpret_cast<uint4 *>(tile + tile_bytes + at) = make_uint4(p1[0], p1[1], p1[2], p1[3]);
-    *reinterpret_cast<uint4 *>(tile + 2 * tile_bytes + at) = make_uint4(p2[0], p2[1], p2[2], p2[3]);
-}
-
-// bf16 rows of any alignment: a warp brings a row of 64 elements at a time, a lane two neighbours, so that it touches every sector once.
-__device__ __forceinline__ uint32_t pair_load(const Source &s, int unit, bool mn, int lane)
-{
-    const int slow = s.slow0 + (mn ? unit % 64 : unit), fast = s.fast0 + (mn ? unit / 64 * 64 : 0) + 2 * lane;
-    const int have = slow < s.slows ? s.fasts - fast : 0;
-    const unsigned short *p = static_cast<const unsigned short *>(s.base) + slow * s.ld + fast;
-    if (have <= 0) return 0;
-    if (s.vec >= 4 && have >= 2) return __ldg(reinterpret_cast<const uint32_t *>(p));
-    return __ldg(p) | (have >= 2 ? (uint32_t)__ldg(p + 1) << 16 : 0);
-}
-
-__device__ __forceinline__ void pair_store(uint32_t w, unsigned char *tile, int unit, int lane)
-{
-    *reinterpret_cast<uint32_t *>(tile + unit * 128 + (((lane / 4) ^ (unit & 7)) << 4) + lane % 4 * 4) = w;
-}
-
 // A share of a tile's sum: tile (m0, n0) and the blocks [k, end) of K.
 struct Share {
     int m0, n0, k, end, split;
@@ -446,18 +365,17 @@ __device__ __forceinline__ Share share_of(const GemmParams &p, int w)
     return s;
 }
 
-template <int LOADER, typename TOUT>
-__global__ void __launch_bounds__(gemm_threads(LOADER), 1) gemm_kernel(const __grid_constant__ GemmParams p)
+template <int kPieces, typename TOUT>
+__global__ void __launch_bounds__(gemm_threads(kPieces), 1) gemm_kernel(const __grid_constant__ GemmParams p)
 {
-    using TIN = typename std::conditional<LOADER == kSplit, float, bf16>::type;
-    constexpr int kPieces = LOADER == kSplit ? 3 : 1, kEpilogue = epilogue_warps(LOADER), BK = block_k(LOADER), kRing = ring_bytes(LOADER);
-    extern __shared__ unsigned char raw[];
-    unsigned char *const ring = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
+    using TIN = typename std::conditional<kPieces == 3, float, bf16>::type;
+    constexpr int kEpilogue = epilogue_warps(kPieces), BK = block_k(kPieces), kRing = ring_bytes(kPieces);
+    extern __shared__ __align__(1024) unsigned char ring[];  // (the kernel declares no other: it starts on a swizzle's boundary)
     unsigned char *const staging = ring + kRing;
     float *const bias_rows = reinterpret_cast<float *>(staging + kEpilogue * 4096);  // 64 per warp
-    __shared__ __align__(8) uint64_t bars[2 * 8 + 2 * kAccs + 1];
-    __shared__ uint32_t tmem_slot;
-    __shared__ volatile int failed;
+    uint64_t *const bars = reinterpret_cast<uint64_t *>(staging + epilogue_bytes(kPieces));  // 2 * 8 + 2 * kAccs + 1
+    uint32_t &tmem_slot = *reinterpret_cast<uint32_t *>(bars + 2 * 8 + 2 * kAccs + 1);
+    volatile int &failed = *reinterpret_cast<volatile int *>(&tmem_slot + 1);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t full = smem_u32(bars), empty = full + 64, acc_full = full + 128, acc_empty = acc_full + 8 * kAccs, last = acc_empty + 8 * kAccs;
     // Tensor memory.  Two to four accumulators, so that some are taken out while another is filled.  The tensor cores cut a sum off, not round it, at
@@ -472,7 +390,7 @@ __global__ void __launch_bounds__(gemm_threads(LOADER), 1) gemm_kernel(const __g
     if (threadIdx.x == 0) {
         failed = 0;
         for (int s = 0; s < p.stages; ++s) {
-            mbar_init(full + 8 * s, LOADER == kTma ? 1 : kProducerWarps);
+            mbar_init(full + 8 * s, 1);
             mbar_init(empty + 8 * s, 1);
         }
         for (int b = 0; b < p.accs; ++b) mbar_init(acc_full + 8 * b, 1), mbar_init(acc_empty + 8 * b, kEpilogue / p.groups);
@@ -492,7 +410,6 @@ __global__ void __launch_bounds__(gemm_threads(LOADER), 1) gemm_kernel(const __g
     const int a_bytes = kBM * 2 * BK, b_bytes = p.bn * 2 * BK, stage_bytes = kPieces * (a_bytes + b_bytes);
 
     if (warp < kEpilogue) {
-        if constexpr (LOADER != kTma) more_registers<kEpilogueRegs>();
         // ---- epilogue: the 32 lanes 32 (warp % 4) and up, parts of 64 columns in two tiles of 32.  16 warps are as many as the widest product
         // has such parts; for narrower ones they form groups that take the accumulators in turn.
         const int in_group = kEpilogue / 4 / p.groups, group = warp / 4 / in_group, part = warp / 4 % in_group;
@@ -602,10 +519,9 @@ __global__ void __launch_bounds__(gemm_threads(LOADER), 1) gemm_kernel(const __g
         }
         if (lane == 0) tma_store_wait<0>();
         __syncwarp();
-    } else if (LOADER == kTma ? warp == kEpilogue : warp < 2 * kEpilogue) {
+    } else if (warp == kEpilogue) {
         // ---- products, by one thread
-        if constexpr (LOADER != kTma) fewer_registers<kProductRegs>();
-        if (warp == kEpilogue && lane == 0) {
+        if (lane == 0) {
             const uint32_t idesc = mma_idesc(p.bn, p.a_mn, p.b_mn);
             const int a_step = p.a_mn ? 2048 >> 4 : 32 >> 4, b_step = p.b_mn ? 2048 >> 4 : 32 >> 4;  // 16 of K further
             int stage = 0, phase = 0;
@@ -651,26 +567,27 @@ __global__ void __launch_bounds__(gemm_threads(LOADER), 1) gemm_kernel(const __g
             }
         }
         __syncwarp();
-    } else if constexpr (LOADER == kTma) {
-        if (warp == kEpilogue + 1 && lane == 0) {
+    } else if (warp == kEpilogue + 1) {
+        // ---- loads, by one thread
+        if (lane == 0) {
             int stage = 0, phase = 0;
             bool ok = true;
             for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
                 const Share s = share_of(p, w);
                 for (int k = s.k; k < s.end; ++k) {
                     if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, &failed))) break;
-                    const uint32_t at = smem_u32(ring) + stage * stage_bytes, bar = full + 8 * stage;
+                    const uint32_t bar = full + 8 * stage;
+                    uint32_t at = smem_u32(ring) + stage * stage_bytes;
                     mbar_expect(bar, stage_bytes);
-                    if (p.a_mn) {
-                        for (int i = 0; i < kBM / 64; ++i) tma_load_2d(at + 8192 * i, &p.ta, s.m0 + 64 * i, k * BK, bar);
-                    } else {
-                        tma_load_2d(at, &p.ta, k * BK, s.m0, bar);
-                    }
-                    if (p.b_mn) {
-                        for (int i = 0; i < p.bn / 64; ++i) tma_load_2d(at + a_bytes + 8192 * i, &p.tb, s.n0 + 64 * i, k * BK, bar);
-                    } else {
-                        tma_load_2d(at + a_bytes, &p.tb, k * BK, s.n0, bar);
-                    }
+                    // (an operand whose rows run along M or N: 64 of it at a time)
+                    for (int piece = 0; piece < kPieces; ++piece, at += a_bytes)
+                        if (!p.a_mn) tma_load_3d(at, &p.ta, k * BK, s.m0, piece, bar);
+                        else
+                            for (int i = 0; i < kBM / 64; ++i) tma_load_3d(at + 128 * BK * i, &p.ta, s.m0 + 64 * i, k * BK, piece, bar);
+                    for (int piece = 0; piece < kPieces; ++piece, at += b_bytes)
+                        if (!p.b_mn) tma_load_3d(at, &p.tb, k * BK, s.n0, piece, bar);
+                        else
+                            for (int i = 0; i < p.bn / 64; ++i) tma_load_3d(at + 128 * BK * i, &p.tb, s.n0 + 64 * i, k * BK, piece, bar);
                     if (++stage == p.stages) stage = 0, phase ^= 1;
                 }
             }
@@ -678,80 +595,6 @@ __global__ void __launch_bounds__(gemm_threads(LOADER), 1) gemm_kernel(const __g
                 for (int i = 0; i < p.stages; ++i) mbar_drain(full + 8 * i, i < stage ? phase : phase ^ 1);
         }
         __syncwarp();
-    } else {
-        // ---- loads without TMA, two groups of warps for every other stage: a group's loads for its next stage are under way while the
-        // other one's are written and the products of the stages before run
-        fewer_registers<kProducerRegs>();
-        constexpr int kThreads = 32 * kProducerWarps;
-        constexpr int kPiecesA = kBM * BK / 8 / kThreads, kPiecesB = 128 * BK / 8 / kThreads;  // of a thread, at most
-        constexpr int kRowsA = kBM / kProducerWarps, kRowsB = 256 / kProducerWarps;                                        // of a warp
-        const int group = (warp - 2 * kEpilogue) / kProducerWarps, member = warp % kProducerWarps, t = threadIdx.x % kThreads;
-        const int pieces_b = p.bn * BK / 8;
-        int w = blockIdx.x, stage = 0, phase = 0;
-        Share s = share_of(p, min(w, total - 1));
-        const auto next = [&] {  // the block of K after this one; false behind the last
-            if (++stage == p.stages) stage = 0, phase ^= 1;
-            if (++s.k < s.end) return true;
-            w += gridDim.x;
-            if (w >= total) return false;
-            s = share_of(p, w);
-            return true;
-        };
-        const auto source_a = [&] { return source_of(p.a, p.lda, p.a_mn, p.a_vec, s.m0, s.k * BK, p.M, p.K); };
-        const auto source_b = [&] { return source_of(p.b, p.ldb, p.b_mn, p.b_vec, s.n0, s.k * BK, p.N, p.K); };
-        bool more = w < total && (group == 0 || next());
-        const auto ready = [&] {
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(full + 8 * stage);
-        };
-        const auto free_stage = [&] { return __all_sync(0xffffffffu, mbar_wait(empty + 8 * stage, phase ^ 1, &failed)); };
-        if constexpr (LOADER == kSplit) {
-            uint32_t a[kPiecesA][8], b[kPiecesB][8];
-            const auto fetch = [&] {
-                const Source sa = source_a(), sb = source_b();
-#pragma unroll
-                for (int i = 0; i < kPiecesA; ++i) piece_load(a[i], sa, piece_of_tile<BK>(t + kThreads * i, p.a_mn));
-#pragma unroll
-                for (int i = 0; i < kPiecesB; ++i)
-                    if (t + kThreads * i < pieces_b) piece_load(b[i], sb, piece_of_tile<BK>(t + kThreads * i, p.b_mn));
-            };
-            if (more) fetch();
-            while (more && free_stage()) {
-                unsigned char *const at = ring + stage * stage_bytes;
-#pragma unroll
-                for (int i = 0; i < kPiecesA; ++i) piece_store(a[i], at, a_bytes, piece_of_tile<BK>(t + kThreads * i, p.a_mn).at);
-#pragma unroll
-                for (int i = 0; i < kPiecesB; ++i)
-                    if (t + kThreads * i < pieces_b)
-                        piece_store(b[i], at + kPieces * a_bytes, b_bytes, piece_of_tile<BK>(t + kThreads * i, p.b_mn).at);
-                ready();
-                more = next() && next();
-                if (more) fetch();
-            }
-        } else {
-            uint32_t a[kRowsA], b[kRowsB];
-            const auto fetch = [&] {
-                const Source sa = source_a(), sb = source_b();
-#pragma unroll
-                for (int i = 0; i < kRowsA; ++i) a[i] = pair_load(sa, member + kProducerWarps * i, p.a_mn, lane);
-#pragma unroll
-                for (int i = 0; i < kRowsB; ++i)
-                    if (member + kProducerWarps * i < p.bn) b[i] = pair_load(sb, member + kProducerWarps * i, p.b_mn, lane);
-            };
-            if (more) fetch();
-            while (more && free_stage()) {
-                unsigned char *const at = ring + stage * stage_bytes;
-#pragma unroll
-                for (int i = 0; i < kRowsA; ++i) pair_store(a[i], at, member + kProducerWarps * i, lane);
-#pragma unroll
-                for (int i = 0; i < kRowsB; ++i)
-                    if (member + kProducerWarps * i < p.bn) pair_store(b[i], at + a_bytes, member + kProducerWarps * i, lane);
-                ready();
-                more = next() && next();
-                if (more) fetch();
-            }
-        }
     }
     tcgen05_fence_before();
     __syncthreads();
@@ -802,15 +645,92 @@ __global__ void __launch_bounds__(256) join_kernel(const float *__restrict__ par
     }
 }
 
+// ---- operands laid out for TMA --------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void split(float2 v, uint32_t (&p)[3])
+{
+    p[0] = pack(v.x, v.y);
+    v = __fadd2_rn(v, make_float2(-low(p[0]), -high(p[0])));
+    p[1] = pack(v.x, v.y);
+    v = __fadd2_rn(v, make_float2(-low(p[1]), -high(p[1])));
+    p[2] = pack(v.x, v.y);
+}
+
+// Eight neighbours as bf16 pieces, 16 bytes of each of the operand's matrices (`layer` apart)
+__device__ __forceinline__ void store_pieces(const float (&v)[8], bf16 *to, long long layer)
+{
+    uint32_t p[3][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t q[3];
+        split(make_float2(v[2 * i], v[2 * i + 1]), q);
+        p[0][i] = q[0], p[1][i] = q[1], p[2][i] = q[2];
+    }
+#pragma unroll
+    for (int j = 0; j < 3; ++j) *reinterpret_cast<uint4 *>(to + j * layer) = make_uint4(p[j][0], p[j][1], p[j][2], p[j][3]);
+}
+
+struct LayoutJob {
+    const void *from;
+    bf16 *to;               // [pieces][rows][ld_to]
+    long long ld, ld_to, layer;
+    int rows, width;        // width 0: no job
+    int vec;                // 16-byte loads are allowed
+    unsigned lanes;         // threads of a row: one for eight elements, or for two
+};
+
+// Two jobs, x and the weights: whole blocks of either.  Rows of whole vectors: a thread has eight elements; others: two, so that a warp touches
+// each sector once.
+template <typename T>
+__global__ void __launch_bounds__(256) layout_kernel(const LayoutJob first, const LayoutJob second, unsigned first_blocks)
+{
+    constexpr int kP = sizeof(T) == 4 ? 3 : 1;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+    const bool is_first = blockIdx.x < first_blocks;
+    const LayoutJob &q = is_first ? first : second;
+    const unsigned block = is_first ? blockIdx.x : blockIdx.x - first_blocks, blocks = is_first ? first_blocks : gridDim.x - first_blocks;
+    const unsigned long long all = (unsigned long long)q.rows * q.lanes;
+    for (unsigned long long i = block * 256ull + threadIdx.x; i < all; i += blocks * 256ull) {
+        const unsigned long long row = i / q.lanes;
+        const int lane = (int)(i - row * q.lanes);
+        const T *src = static_cast<const T *>(q.from) + row * q.ld;
+        bf16 *dst = q.to + row * q.ld_to;
+        if (q.vec) {
+            src += 8 * lane, dst += 8 * lane;
+            if constexpr (kP == 3) {
+                const uint4 a = __ldcs(reinterpret_cast<const uint4 *>(src)), b = __ldcs(reinterpret_cast<const uint4 *>(src) + 1);
+                const float v[8] = {__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
+                                    __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)};
+                store_pieces(v, dst, q.layer);
+            } else {
+                *reinterpret_cast<uint4 *>(dst) = __ldcs(reinterpret_cast<const uint4 *>(src));
+            }
+        } else {
+            const int col = 2 * lane;
+            const T a = src[col], b = col + 1 < q.width ? src[col + 1] : from_float<T>(0.0f);
+            if constexpr (kP == 3) {
+                uint32_t p[3];
+                split(make_float2(a, b), p);
+#pragma unroll
+                for (int j = 0; j < 3; ++j) *reinterpret_cast<uint32_t *>(dst + j * q.layer + col) = p[j];
+            } else {
+                *reinterpret_cast<__nv_bfloat162 *>(dst + col) = __nv_bfloat162(a, b);
+            }
+        }
+    }
+}
+
 // ---- dz = grad_out act'(z), and its column sums ---------------------------------------------------------------------------
 
 constexpr int kSlopeRows = 8;  // warps of a block: each takes every eighth row of the block's
 
-// A lane has VEC neighbouring columns, a warp a stretch of a row, the block `per` rows.  dz may be NULL (column sums only), sums too.
+// A lane has VEC neighbouring columns, a warp a stretch of a row, the block `per` rows.  dz, in bf16 numbers or three pieces `layer` apart, may be NULL
+// (column sums only), sums too.
 template <typename TG, typename TZ, int VEC>
 __global__ void __launch_bounds__(32 * kSlopeRows) slope_kernel(const TG *__restrict__ g, long long ld_g, const TZ *__restrict__ z, long long ld_z,
-                                                                TZ *__restrict__ dz, long long ld_dz, float *__restrict__ sums, int M, int N, int per,
-                                                                int act)
+                                                                bf16 *__restrict__ dz, long long ld_dz, long long layer, float *__restrict__ sums, int M,
+                                                                int N, int per, int act)
 {
     constexpr bool kFast = std::is_same<TZ, bf16>::value;
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -842,23 +762,32 @@ __global__ void __launch_bounds__(32 * kSlopeRows) slope_kernel(const TG *__rest
                 if (z) zv[0] = z[row * ld_z + col];
             }
             float d[VEC];
+            if constexpr (VEC == 1) {
+                d[0] = z ? slope_times<kFast>(both(to_float(gv[0])), both(to_float(zv[0])), act).x : to_float(gv[0]);
+                acc[0] += d[0];
+            } else {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                d[j] = z ? slope_times<kFast>(to_float(gv[j]), to_float(zv[j]), act) : to_float(gv[j]);
-                acc[j] += d[j];
+                for (int j = 0; j < VEC; j += 2) {
+                    float2 v = make_float2(to_float(gv[j]), to_float(gv[j + 1]));
+                    if (z) v = slope_times<kFast>(v, make_float2(to_float(zv[j]), to_float(zv[j + 1])), act);
+                    d[j] = v.x, d[j + 1] = v.y;
+                    v = __fadd2_rn(v, make_float2(acc[j], acc[j + 1]));
+                    acc[j] = v.x, acc[j + 1] = v.y;
+                }
             }
             if (dz) {
-                if constexpr (VEC > 1) {
-                    constexpr int ZQ = VEC * (int)sizeof(TZ) / 16;
-                    TZ o[VEC];
+                bf16 *const to = dz + row * ld_dz + col;
+                if constexpr (VEC == 8 && sizeof(TZ) == 4) {
+                    store_pieces(d, to, layer);
+                } else if constexpr (VEC == 8) {
+                    *reinterpret_cast<uint4 *>(to) = make_uint4(pack(d[0], d[1]), pack(d[2], d[3]), pack(d[4], d[5]), pack(d[6], d[7]));
+                } else if constexpr (sizeof(TZ) == 4) {
+                    uint32_t p[3];
+                    split(make_float2(d[0], 0.0f), p);
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) o[j] = from_float<TZ>(d[j]);
-                    uint4 q[ZQ];
-                    memcpy(q, o, sizeof(o));
-#pragma unroll
-                    for (int i = 0; i < ZQ; ++i) reinterpret_cast<uint4 *>(dz + row * ld_dz + col)[i] = q[i];
+                    for (int j = 0; j < 3; ++j) to[j * layer] = __ushort_as_bfloat16((unsigned short)p[j]);
                 } else {
-                    dz[row * ld_dz + col] = from_float<TZ>(d[0]);
+                    *to = from_float<bf16>(d[0]);
                 }
             }
         }
@@ -877,26 +806,25 @@ __global__ void __launch_bounds__(32 * kSlopeRows) slope_kernel(const TG *__rest
     }
 }
 
-// Column sums of `rows` rows of partial sums: 32 columns per block, its eight warps take every eighth row.
+// Column sums of `rows` rows of partial sums: 32 columns per block, its 32 warps take every 32nd row.
 template <typename T>
-__global__ void __launch_bounds__(256) column_sum_kernel(const float *__restrict__ sums, int rows, int N, T *__restrict__ out)
+__global__ void __launch_bounds__(1024) column_sum_kernel(const float *__restrict__ sums, int rows, int N, T *__restrict__ out)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
-    __shared__ float part[8][33];
+    __shared__ float part[32][33];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, col = blockIdx.x * 32 + lane;
     float v = 0.0f;
     if (col < N)
 #pragma unroll 8
-        for (int r = warp; r < rows; r += 8) v += sums[(long long)r * N + col];
+        for (int r = warp; r < rows; r += 32) v += sums[(long long)r * N + col];
     part[warp][lane] = v;
     __syncthreads();
-    if (warp == 0 && col < N) {
-        v = 0.0f;
+    // a column's 32 numbers by a warp of their own
+    v = part[lane][warp];
 #pragma unroll
-        for (int w = 0; w < 8; ++w) v += part[w][lane];
-        out[col] = from_float<T>(v);
-    }
+    for (int d = 16; d; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
+    if (lane == 0 && blockIdx.x * 32 + warp < N) out[blockIdx.x * 32 + warp] = from_float<T>(v);
 }
 
 // ---- few rows ---------------------------------------------------------------------------------------------------------------
@@ -972,21 +900,22 @@ __global__ void __launch_bounds__(256) rows_kernel(const TIN *__restrict__ x, lo
 constexpr int kMaxFeatures = 1 << 24;
 constexpr int kFewRows = 8;
 
-// One of the kernel's operands: rows of `fast` contiguous elements, `slow` of them, ld apart.
+// One of the kernel's operands: rows of contiguous bf16 numbers, ld apart; of pieces three such matrices, `layer` apart.
 struct Operand {
     const void *p;
     long long ld;
     bool mn;  // a row per k
+    long long layer = 0;
 };
 
 // (a tensor map's strides end at 2^40 bytes)
-bool tma_ok(const Operand &o) { return (uintptr_t)o.p % 16 == 0 && o.ld % 8 == 0 && o.ld < (1LL << 38); }
+bool tma_ok(const void *p, long long ld) { return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && ld < (1LL << 38); }
 
-int row_vec(const Operand &o, int elem)
-{
-    const uintptr_t bits = (uintptr_t)o.p | (uintptr_t)(o.ld * elem);
-    return bits % 16 == 0 ? 16 : (bits % 4 == 0 ? 4 : 1);
-}
+size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
+
+// Distance of the rows, and bytes, of an operand that has to be laid out in the scratch
+long long laid_out_ld(int width) { return (width + 7LL) / 8 * 8; }
+size_t laid_out_bytes(long long rows, int width, bool f32) { return round_up((size_t)rows * laid_out_ld(width) * (f32 ? 6 : 2)); }
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -1008,15 +937,17 @@ EncodeTiled encode_tiled()
 }
 
 // `across`: extent along M or N; box: rows of the tile
-bool make_map(CUtensorMap &map, const Operand &o, int across, int K, int rows)
+bool make_map(CUtensorMap &map, const Operand &o, int pieces, int across, int K, int rows)
 {
     const EncodeTiled encode = encode_tiled();
     if (!encode) return false;
-    const cuuint64_t size[2] = {(cuuint64_t)(o.mn ? across : K), (cuuint64_t)(o.mn ? K : across)}, pitch[1] = {(cuuint64_t)o.ld * 2};
-    constexpr int BK = block_k(kTma);
-    const cuuint32_t box[2] = {BK, (cuuint32_t)(o.mn ? BK : rows)}, step[2] = {1, 1};
-    return encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(o.p), size, pitch, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const int bk = block_k(pieces);
+    const cuuint64_t size[3] = {(cuuint64_t)(o.mn ? across : K), (cuuint64_t)(o.mn ? K : across), (cuuint64_t)pieces};
+    const cuuint64_t pitch[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)(pieces == 1 ? o.ld : o.layer) * 2};
+    const cuuint32_t box[3] = {(cuuint32_t)(o.mn ? 64 : bk), (cuuint32_t)(o.mn ? bk : rows), 1}, step[3] = {1, 1, 1};
+    return encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(o.p), size, pitch, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  o.mn || bk == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Results: `layers` matrices of M rows, stored in tiles of 32 x 32
@@ -1038,48 +969,42 @@ constexpr int kRun = 384;
 
 // Tiles and shares of a product.
 struct Plan {
-    int loader, bn, stages, tiles_m, tiles_n, kblocks, kshare, splits, run, columns, accs, groups;
+    int bn, stages, tiles_m, tiles_n, kblocks, kshare, splits, run, columns, accs, groups;
     long long ld_partial;
     size_t partial_bytes;  // 0: every tile's sum belongs to one CTA
 };
 
-Plan plan_product(const Operand &a, const Operand &b, bool f32, bool out_f32, int M, int N, int K, bool may_split)
+Plan plan_product(bool b_mn, bool f32, bool out_f32, int M, int N, int K, bool may_split)
 {
     Plan q = {};
-    q.loader = f32 ? kSplit : (tma_ok(a) && tma_ok(b) ? kTma : kCopy);
-    const int sms = sm_count();
+    const int sms = sm_count(), pieces = f32 ? 3 : 1;
     q.tiles_m = (M + kBM - 1) / kBM;
-    const int bk = block_k(q.loader);
+    const int bk = block_k(pieces);
     q.kblocks = (K + bk - 1) / bk;
     const bool runs = out_f32 && K > kRun;
-    // Widths: the columns in equal parts, at most 256 (128 where accumulators for pieces or a running sum take tensor memory).  A tile
-    // costs its columns and about 32 more; the last wave may be nearly empty.
+    // Widths: the columns in equal parts, at most 256 (128 where accumulators for pieces or a running sum take tensor memory); and shares of
+    // long sums where there are few tiles.  By estimated cycles of the CTA with the most to do: a block of K as measured (8192 x 4096 x 4096 with 256
+    // columns, 40000 x 1024 x 256 with 128; pieces 40000 x 256 x 256), a tile's epilogue 12 cycles a column and 800 more, beside the products of the next
+    // tile if there is one; partial sums are written and read again by another kernel, all CTAs together at 2000 bytes a cycle.
     const int widest = f32 || runs ? 128 : 256;
-    long long best = 0;
+    double best = 0.0;
     for (int t = (N + widest - 1) / widest; t <= (N + 63) / 64; ++t) {
-        const int grain = b.mn ? 64 : 32;
-        const int bn = ((N + t - 1) / t + grain - 1) / grain * grain;
-        const long long tiles = (long long)q.tiles_m * ((N + bn - 1) / bn), cost = (tiles + sms - 1) / sms * (bn + 32);
-        if (!best || cost < best) best = cost, q.bn = bn;
+        const int grain = b_mn ? 64 : 32, bn = ((N + t - 1) / t + grain - 1) / grain * grain;
+        const long long tiles = (long long)q.tiles_m * ((N + bn - 1) / bn);
+        const int most = may_split && tiles * 2 <= sms ? (int)std::min<long long>(sms / tiles, (long long)q.kblocks * bk / 128) : 1;
+        const int share = (q.kblocks + std::max(1, most) - 1) / std::max(1, most), splits = (q.kblocks + share - 1) / share;
+        const double items = (double)((tiles * splits + sms - 1) / sms), main = share * (f32 ? 8.0 : 2.15) * std::max(kBM + bn, f32 ? 0 : 360);
+        const double rest = 12.0 * bn + 800.0, join = splits > 1 ? 4000.0 + splits * 8.0 * M * N / 2000.0 : 0.0;
+        const double cost = items * std::max(main, rest) + std::min(main, rest) + join;
+        if (q.bn == 0 || cost < best) best = cost, q.bn = bn, q.kshare = share, q.splits = splits;
         if (t > 64) break;  // (wide results: the widest tiles)
     }
     q.tiles_n = (N + q.bn - 1) / q.bn;
-    const int stage = (q.loader == kSplit ? 3 : 1) * (kBM + q.bn) * 2 * bk;
-    q.stages = std::min(8, ring_bytes(q.loader) / stage);
-    const long long tiles = (long long)q.tiles_m * q.tiles_n;
-    q.splits = 1, q.kshare = q.kblocks;
-    if (may_split && tiles * 2 <= sms) {
-        const int least = 128 / bk;  // blocks for a share to be worth its partial sums
-        const int splits = (int)std::min<long long>(sms / tiles, q.kblocks / least);
-        if (splits > 1) {
-            q.kshare = (q.kblocks + splits - 1) / splits;
-            q.splits = (q.kblocks + q.kshare - 1) / q.kshare;
-        }
-    }
+    q.stages = std::min(8, ring_bytes(pieces) / (pieces * (kBM + q.bn) * 2 * bk));
     q.run = runs && q.kshare > kRun / bk ? kRun / bk : q.kshare;
     // Accumulators: with runs two, the running sum and, of float32 operands, that of the small products; else four where they fit (float32
     // operands: pairs).  Groups of epilogue warps: as many 64-column parts as the tile has in each, and no more of them than accumulators.
-    const int parts = f32 ? 2 : 1, warps = epilogue_warps(q.loader) / 4, wide = (q.bn + 63) / 64;
+    const int parts = f32 ? 2 : 1, warps = epilogue_warps(pieces) / 4, wide = (q.bn + 63) / 64;
     const bool in_runs = q.run < q.kshare;
     q.accs = !in_runs && 4 * parts * q.bn <= 512 ? 4 : 2;
     const int used = in_runs ? (2 + parts) * q.bn : q.accs * parts * q.bn;
@@ -1107,15 +1032,31 @@ bool vec_ok(const void *p, long long ld, bool f32)
     return ((uintptr_t)p | (uintptr_t)(ld * (f32 ? 4 : 2))) % 16 == 0 && ld < (1LL << 37);
 }
 
-template <int LOADER, typename TOUT>
+template <int PIECES, typename TOUT>
 cudaError_t launch_gemm(const GemmParams &g, cudaStream_t stream)
 {
-    const auto kernel = gemm_kernel<LOADER, TOUT>;
-    constexpr int smem = 1024 + ring_bytes(LOADER) + epilogue_bytes(LOADER);
+    const auto kernel = gemm_kernel<PIECES, TOUT>;
+    constexpr int smem = ring_bytes(PIECES) + epilogue_bytes(PIECES) + kControlBytes;
+    static_assert(smem <= kSmemLimit && ring_bytes(3) >= 3 * 3 * (kBM + 128) * 2 * block_k(3), "");
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     const int grid = std::min(g.tiles * g.splits, sm_count());
-    return launch_dependent(kernel, dim3((unsigned)grid), dim3((unsigned)gemm_threads(LOADER)), smem, stream, g);
+    return launch_dependent(kernel, dim3((unsigned)grid), dim3((unsigned)gemm_threads(PIECES)), smem, stream, g);
+}
+
+// Lays one or two operands out in the scratch
+template <typename T>
+cudaError_t launch_layout(LayoutJob *jobs, int count, cudaStream_t stream)
+{
+    unsigned blocks[2] = {0, 0};
+    for (int i = 0; i < count; ++i) {
+        LayoutJob &q = jobs[i];
+        q.ld_to = laid_out_ld(q.width), q.layer = q.rows * q.ld_to;
+        q.vec = q.width % 8 == 0 && ((uintptr_t)q.from | (uintptr_t)(q.ld * (long long)sizeof(T))) % 16 == 0;
+        q.lanes = (unsigned)(q.vec ? q.width / 8 : (q.width + 1) / 2);
+        blocks[i] = (unsigned)std::min<long long>(((long long)q.rows * q.lanes + 255) / 256, 8LL * sm_count());
+    }
+    return launch_dependent(layout_kernel<T>, dim3(blocks[0] + blocks[1]), dim3(256), 0, stream, jobs[0], jobs[count - 1], blocks[0]);
 }
 
 template <typename TIN, typename TOUT>
@@ -1133,10 +1074,9 @@ flashbev_status run_product(const Plan &q, const Operand &a, const Operand &b, b
                             uint32_t *error_word, cudaStream_t stream, int &launches)
 {
     GemmParams g = {};
-    if (q.loader == kTma && !(make_map(g.ta, a, M, K, kBM) && make_map(g.tb, b, N, K, q.bn))) return FLASHBEV_CUDA_ERROR;
-    const int elem = f32 ? 4 : 2;
-    g.a = a.p, g.b = b.p, g.lda = a.ld, g.ldb = b.ld, g.a_mn = a.mn, g.b_mn = b.mn;
-    g.a_vec = row_vec(a, elem), g.b_vec = row_vec(b, elem);
+    const int pieces = f32 ? 3 : 1;
+    if (!make_map(g.ta, a, pieces, M, K, kBM) || !make_map(g.tb, b, pieces, N, K, q.bn)) return FLASHBEV_CUDA_ERROR;
+    g.a_mn = a.mn, g.b_mn = b.mn;
     g.M = M, g.N = N, g.K = K, g.bn = q.bn, g.stages = q.stages;
     g.run = q.run, g.columns = q.columns, g.accs = q.accs, g.groups = q.groups;
     g.tiles_n = q.tiles_n, g.tiles = q.tiles_m * q.tiles_n, g.kblocks = q.kblocks, g.kshare = q.kshare, g.splits = q.splits;
@@ -1154,9 +1094,8 @@ flashbev_status run_product(const Plan &q, const Operand &a, const Operand &b, b
         if (e.pre && !make_store_map(g.tpre, e.pre, f32, M, N, e.ld_pre, 1)) return FLASHBEV_CUDA_ERROR;
     }
     cudaError_t err;
-    if (q.loader == kSplit) err = e.out_f32 ? launch_gemm<kSplit, float>(g, stream) : launch_gemm<kSplit, bf16>(g, stream);
-    else if (q.loader == kCopy) err = e.out_f32 ? launch_gemm<kCopy, float>(g, stream) : launch_gemm<kCopy, bf16>(g, stream);
-    else err = e.out_f32 ? launch_gemm<kTma, float>(g, stream) : launch_gemm<kTma, bf16>(g, stream);
+    if (f32) err = e.out_f32 ? launch_gemm<3, float>(g, stream) : launch_gemm<3, bf16>(g, stream);
+    else err = e.out_f32 ? launch_gemm<1, float>(g, stream) : launch_gemm<1, bf16>(g, stream);
     ++launches;
     if (err == cudaSuccess && q.splits > 1) {
         if (f32) err = e.out_f32 ? launch_join<float, float>(q, partial, M, N, e, stream) : launch_join<float, bf16>(q, partial, M, N, e, stream);
@@ -1171,12 +1110,12 @@ flashbev_status run_product(const Plan &q, const Operand &a, const Operand &b, b
 }
 
 template <typename TIN, typename TOUT>
-cudaError_t launch_rows(const Operand &x, const Operand &w, int M, int N, int K, const Epilogue &e, cudaStream_t stream)
+cudaError_t launch_rows(const void *x, long long ld_x, const void *weight, long long ld_w, int M, int N, int K, const Epilogue &e, cudaStream_t stream)
 {
-    const bool vec = row_vec(x, sizeof(TIN)) == 16 && row_vec(w, sizeof(TIN)) == 16;
+    const bool vec = (((uintptr_t)x | (uintptr_t)weight) | (uintptr_t)((ld_x | ld_w) * (long long)sizeof(TIN))) % 16 == 0;
     const auto go = [&](auto kernel, int nc) {
-        return launch_dependent(kernel, dim3((unsigned)((N + 8 * nc - 1) / (8 * nc))), dim3(256), 0, stream, static_cast<const TIN *>(x.p), x.ld,
-                                static_cast<const TIN *>(w.p), w.ld, M, N, K, static_cast<const TIN *>(e.bias), static_cast<const TOUT *>(e.residual),
+        return launch_dependent(kernel, dim3((unsigned)((N + 8 * nc - 1) / (8 * nc))), dim3(256), 0, stream, static_cast<const TIN *>(x), ld_x,
+                                static_cast<const TIN *>(weight), ld_w, M, N, K, static_cast<const TIN *>(e.bias), static_cast<const TOUT *>(e.residual),
                                 e.ld_res, static_cast<TOUT *>(e.out), e.ld_out, static_cast<TIN *>(e.pre), e.ld_pre, e.act);
     };
     if (M == 1) return vec ? go(rows_kernel<TIN, TOUT, 1, 2, true>, 2) : go(rows_kernel<TIN, TOUT, 1, 2, false>, 2);
@@ -1213,18 +1152,35 @@ flashbev_status check_linear(const flashbev_linear_params *p)
     return FLASHBEV_OK;
 }
 
-Operand operand_x(const flashbev_linear_params *p) { return {p->x, dense(p->ld_x, p->in_features), false}; }
-Operand operand_w(const flashbev_linear_params *p) { return {p->weight, dense(p->ld_weight, p->in_features), false}; }
+// Scratch of a forward call: operands that have to be laid out, then partial sums.
+struct ForwardPlan {
+    Plan product;
+    bool lay_x, lay_w;
+    size_t x_at, w_at, partial_at, needed, total;  // needed: without partial sums
+};
+
+ForwardPlan plan_forward(const flashbev_linear_params *p)
+{
+    ForwardPlan q = {};
+    const bool f32 = p->dtype == FLASHBEV_F32;
+    const int M = (int)p->rows, N = p->out_features, K = p->in_features;
+    q.lay_x = f32 || !tma_ok(p->x, dense(p->ld_x, K)), q.lay_w = f32 || !tma_ok(p->weight, dense(p->ld_weight, K));
+    size_t at = 0;
+    if (q.lay_x) q.x_at = at, at += laid_out_bytes(M, K, f32);
+    if (q.lay_w) q.w_at = at, at += laid_out_bytes(N, K, f32);
+    q.needed = q.partial_at = at;
+    q.product = plan_product(false, f32, p->out_dtype == FLASHBEV_F32, M, N, K, true);
+    q.total = at + round_up(q.product.partial_bytes);
+    return q;
+}
 
 // ---- backward
 
 struct BackwardPlan {
-    bool need_dz, need_x, need_w, need_b;
-    long long ld_dz;
+    bool need_dz, need_x, need_w, need_b, lay_x, lay_w;
     Plan gx, gw;
     int per, chunks;                                // rows of a block of slope_kernel; blocks along the rows
-    size_t dz_at, sums_at, partial_at, total;
-    Operand dz;
+    size_t dz_at, x_at, w_at, sums_at, partial_at, total;
 };
 
 flashbev_status check_backward(const flashbev_linear_backward_params *p)
@@ -1254,35 +1210,29 @@ BackwardPlan plan_backward(const flashbev_linear_backward_params *p)
     BackwardPlan q = {};
     const bool f32 = p->dtype == FLASHBEV_F32;
     const int M = (int)p->rows, N = p->out_features, K = p->in_features;
-    const auto up = [](size_t v) { return (v + 255) / 256 * 256; };
     q.need_x = p->grad_x, q.need_w = p->grad_weight, q.need_b = p->grad_bias;
     if (!M) return q;
-    q.need_dz = (q.need_x || q.need_w) && (p->act != FLASHBEV_ACT_NONE || p->dtype != p->grad_dtype);
+    q.need_dz = (q.need_x || q.need_w) && (f32 || p->act != FLASHBEV_ACT_NONE || p->dtype != p->grad_dtype ||
+                                           !tma_ok(p->grad_out, dense(p->ld_grad_out, N)));
+    q.lay_x = q.need_w && (f32 || !tma_ok(p->x, dense(p->ld_x, K)));
+    q.lay_w = q.need_x && (f32 || !tma_ok(p->weight, dense(p->ld_weight, K)));
     size_t at = 0;
-    if (q.need_dz) {
-        q.ld_dz = (N + 7) / 8 * 8;
-        q.dz_at = at, at += up((size_t)M * q.ld_dz * elem_size(p->dtype));
-        q.dz = {static_cast<char *>(p->workspace) + q.dz_at, q.ld_dz, false};
-    } else {
-        q.dz = {p->grad_out, dense(p->ld_grad_out, N), false};
-    }
+    if (q.need_dz) q.dz_at = at, at += laid_out_bytes(M, N, f32);
+    if (q.lay_x) q.x_at = at, at += laid_out_bytes(M, K, f32);
+    if (q.lay_w) q.w_at = at, at += laid_out_bytes(N, K, f32);
     if (q.need_dz || q.need_b) {
-        // about four blocks per SM, but no fewer than 32 rows for each
+        // about four blocks per SM (two where only sums are wanted), but no fewer than 32 rows for each
         const int across = std::max(1, (N + 255) / 256);
         const long long blocks = std::max(1, 4 * sm_count() / across);
         q.per = (int)std::max<long long>(32, (M + blocks - 1) / blocks);
         q.chunks = (M + q.per - 1) / q.per;
         if (q.chunks > 65535) q.per = (M + 65534) / 65535, q.chunks = (M + q.per - 1) / q.per;
-        if (q.need_b) q.sums_at = at, at += up((size_t)q.chunks * N * sizeof(float));
+        if (q.need_b) q.sums_at = at, at += round_up((size_t)q.chunks * N * sizeof(float));
     }
-    const Operand w = {p->weight, dense(p->ld_weight, K), true}, x = {p->x, dense(p->ld_x, K), true};
-    Operand dzt = q.dz;
-    dzt.mn = true;
-    if (q.need_x) q.gx = plan_product(q.dz, w, f32, f32, M, K, N, true);
-    if (q.need_w) q.gw = plan_product(dzt, x, f32, f32, N, K, M, true);
+    if (q.need_x) q.gx = plan_product(true, f32, f32, M, K, N, true);
+    if (q.need_w) q.gw = plan_product(true, f32, f32, N, K, M, true);
     q.partial_at = at;  // (the products run one after the other)
-    at += up(std::max(q.gx.partial_bytes, q.gw.partial_bytes));
-    q.total = at;
+    q.total = at + round_up(std::max(q.gx.partial_bytes, q.gw.partial_bytes));
     return q;
 }
 
@@ -1291,7 +1241,8 @@ cudaError_t launch_slope(const flashbev_linear_backward_params *p, const Backwar
 {
     const int M = (int)p->rows, N = p->out_features;
     char *const ws = static_cast<char *>(p->workspace);
-    TZ *const dz = q.need_dz ? reinterpret_cast<TZ *>(ws + q.dz_at) : nullptr;
+    bf16 *const dz = q.need_dz ? reinterpret_cast<bf16 *>(ws + q.dz_at) : nullptr;
+    const long long ld_dz = laid_out_ld(N);
     float *const sums = q.need_b ? reinterpret_cast<float *>(ws + q.sums_at) : nullptr;
     const TZ *const z = p->act == FLASHBEV_ACT_NONE ? nullptr : static_cast<const TZ *>(p->preact);
     const long long ld_g = dense(p->ld_grad_out, N), ld_z = dense(p->ld_preact, N);
@@ -1299,7 +1250,7 @@ cudaError_t launch_slope(const flashbev_linear_backward_params *p, const Backwar
     const int width = 32 * (vec ? 8 : 1);
     const dim3 grid((unsigned)((N + width - 1) / width), (unsigned)q.chunks);
     return launch_dependent(vec ? slope_kernel<TG, TZ, 8> : slope_kernel<TG, TZ, 1>, grid, dim3(32 * kSlopeRows), 0, stream,
-                            static_cast<const TG *>(p->grad_out), ld_g, z, ld_z, dz, q.ld_dz, sums, M, N, q.per, p->act);
+                            static_cast<const TG *>(p->grad_out), ld_g, z, ld_z, dz, ld_dz, M * ld_dz, sums, M, N, q.per, p->act);
 }
 
 }  // namespace
@@ -1315,15 +1266,16 @@ flashbev_status flashbev_linear(const flashbev_linear_params *p, void *stream_)
     if (p->rows) {
         const bool f32 = p->dtype == FLASHBEV_F32;
         const int M = (int)p->rows, N = p->out_features, K = p->in_features;
-        const Operand x = operand_x(p), w = operand_w(p);
+        const long long ld_x = dense(p->ld_x, K), ld_w = dense(p->ld_weight, K);
         Epilogue e;
         e.bias = p->bias, e.residual = p->residual, e.out = p->out, e.pre = p->preact_out, e.act = p->act;
         e.ld_res = dense(p->ld_residual, N), e.ld_out = dense(p->ld_out, N), e.ld_pre = dense(p->ld_preact, N);
         e.out_f32 = p->out_dtype == FLASHBEV_F32;
         if (M <= kFewRows) {
             cudaError_t err;
-            if (f32) err = e.out_f32 ? launch_rows<float, float>(x, w, M, N, K, e, stream) : launch_rows<float, bf16>(x, w, M, N, K, e, stream);
-            else err = e.out_f32 ? launch_rows<bf16, float>(x, w, M, N, K, e, stream) : launch_rows<bf16, bf16>(x, w, M, N, K, e, stream);
+            const auto go = [&](auto run) { return run(p->x, ld_x, p->weight, ld_w, M, N, K, e, stream); };
+            if (f32) err = e.out_f32 ? go(launch_rows<float, float>) : go(launch_rows<float, bf16>);
+            else err = e.out_f32 ? go(launch_rows<bf16, float>) : go(launch_rows<bf16, bf16>);
             if (err != cudaSuccess || cudaGetLastError() != cudaSuccess) {
                 cudaGetLastError();
                 return FLASHBEV_CUDA_ERROR;
@@ -1331,12 +1283,32 @@ flashbev_status flashbev_linear(const flashbev_linear_params *p, void *stream_)
             launches = 1;
             t_last_kernel = "linear_rows";
         } else {
-            Plan q = plan_product(x, w, f32, e.out_f32, M, N, K, true);
-            if (q.partial_bytes && (!p->workspace || p->workspace_bytes < q.partial_bytes)) q = plan_product(x, w, f32, e.out_f32, M, N, K, false);
+            ForwardPlan q = plan_forward(p);
+            const size_t have = p->workspace ? p->workspace_bytes : 0;
+            if (have < q.needed) return FLASHBEV_TOO_SMALL;
+            if (have < q.total) q.product = plan_product(false, f32, e.out_f32, M, N, K, false);
+            char *const ws = static_cast<char *>(p->workspace);
+            Operand x = {p->x, ld_x, false}, w = {p->weight, ld_w, false};
+            LayoutJob jobs[2] = {};
+            int count = 0;
+            const auto lay = [&](Operand &o, size_t at, int rows) {
+                LayoutJob &j = jobs[count++];
+                j.from = o.p, j.to = reinterpret_cast<bf16 *>(ws + at), j.ld = o.ld, j.rows = rows, j.width = K;
+                o = {j.to, laid_out_ld(K), o.mn, rows * laid_out_ld(K)};
+            };
+            if (q.lay_x) lay(x, q.x_at, M);
+            if (q.lay_w) lay(w, q.w_at, N);
+            if (count) {
+                if ((f32 ? launch_layout<float>(jobs, count, stream) : launch_layout<bf16>(jobs, count, stream)) != cudaSuccess) {
+                    cudaGetLastError();
+                    return FLASHBEV_CUDA_ERROR;
+                }
+                ++launches;
+            }
             const flashbev_status run =
-                run_product(q, x, w, f32, M, N, K, e, static_cast<float *>(p->workspace), p->error_word, stream, launches);
+                run_product(q.product, x, w, f32, M, N, K, e, reinterpret_cast<float *>(ws + q.partial_at), p->error_word, stream, launches);
             if (run != FLASHBEV_OK) return run;
-            t_last_kernel = q.loader == kTma ? "linear_tma" : (q.loader == kCopy ? "linear_copy" : "linear_f32");
+            t_last_kernel = f32 ? "linear_f32" : (count ? "linear_bf16_laid_out" : "linear_bf16");
         }
     }
     t_last_launches = launches;
@@ -1346,9 +1318,7 @@ flashbev_status flashbev_linear(const flashbev_linear_params *p, void *stream_)
 size_t flashbev_linear_workspace_bytes(const flashbev_linear_params *p)
 {
     if (check_linear(p) != FLASHBEV_OK || p->rows <= kFewRows) return 0;
-    return plan_product(operand_x(p), operand_w(p), p->dtype == FLASHBEV_F32, p->out_dtype == FLASHBEV_F32, (int)p->rows, p->out_features,
-                        p->in_features, true)
-        .partial_bytes;
+    return plan_forward(p).total;
 }
 
 flashbev_status flashbev_linear_backward(const flashbev_linear_backward_params *p, void *stream_)
@@ -1380,8 +1350,8 @@ flashbev_status flashbev_linear_backward(const flashbev_linear_backward_params *
         if (err == cudaSuccess && q.need_b) {
             const float *const sums = reinterpret_cast<const float *>(ws + q.sums_at);
             const dim3 grid((unsigned)((N + 31) / 32));
-            if (f32) err = launch_dependent(column_sum_kernel<float>, grid, dim3(256), 0, stream, sums, q.chunks, N, static_cast<float *>(p->grad_bias));
-            else err = launch_dependent(column_sum_kernel<bf16>, grid, dim3(256), 0, stream, sums, q.chunks, N, static_cast<bf16 *>(p->grad_bias));
+            if (f32) err = launch_dependent(column_sum_kernel<float>, grid, dim3(1024), 0, stream, sums, q.chunks, N, static_cast<float *>(p->grad_bias));
+            else err = launch_dependent(column_sum_kernel<bf16>, grid, dim3(1024), 0, stream, sums, q.chunks, N, static_cast<bf16 *>(p->grad_bias));
             ++launches;
         }
         if (err != cudaSuccess) {
@@ -1389,18 +1359,35 @@ flashbev_status flashbev_linear_backward(const flashbev_linear_backward_params *
             return FLASHBEV_CUDA_ERROR;
         }
     }
+    Operand dz = {p->grad_out, dense(p->ld_grad_out, N), false};
+    if (q.need_dz) dz = {ws + q.dz_at, laid_out_ld(N), false, M * laid_out_ld(N)};
+    Operand x = {p->x, dense(p->ld_x, K), true}, w = {p->weight, dense(p->ld_weight, K), true};
+    LayoutJob jobs[2] = {};
+    int count = 0;
+    const auto lay = [&](Operand &o, size_t at, int rows) {
+        LayoutJob &j = jobs[count++];
+        j.from = o.p, j.to = reinterpret_cast<bf16 *>(ws + at), j.ld = o.ld, j.rows = rows, j.width = K;
+        o = {j.to, laid_out_ld(K), o.mn, rows * laid_out_ld(K)};
+    };
+    if (q.lay_x) lay(x, q.x_at, M);
+    if (q.lay_w) lay(w, q.w_at, N);
+    if (count) {
+        if ((f32 ? launch_layout<float>(jobs, count, stream) : launch_layout<bf16>(jobs, count, stream)) != cudaSuccess) {
+            cudaGetLastError();
+            return FLASHBEV_CUDA_ERROR;
+        }
+        ++launches;
+    }
     float *const partial = reinterpret_cast<float *>(ws + q.partial_at);
     Epilogue e;
     e.out_f32 = f32;
     if (q.need_x) {
-        const Operand w = {p->weight, dense(p->ld_weight, K), true};
         e.out = p->grad_x, e.ld_out = dense(p->ld_grad_x, K);
-        const flashbev_status run = run_product(q.gx, q.dz, w, f32, M, K, N, e, partial, p->error_word, stream, launches);
+        const flashbev_status run = run_product(q.gx, dz, w, f32, M, K, N, e, partial, p->error_word, stream, launches);
         if (run != FLASHBEV_OK) return run;
     }
     if (q.need_w) {
-        const Operand x = {p->x, dense(p->ld_x, K), true};
-        Operand dzt = q.dz;
+        Operand dzt = dz;
         dzt.mn = true;
         e.out = p->grad_weight, e.ld_out = dense(p->ld_grad_weight, K);
         const flashbev_status run = run_product(q.gw, dzt, x, f32, N, K, M, e, partial, p->error_word, stream, launches);

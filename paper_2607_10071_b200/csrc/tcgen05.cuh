@@ -64,11 +64,11 @@ __device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity)
 
 // ---- TMA ------------------------------------------------------------------------------------------------------------------
 
-// x: innermost coordinate, a multiple of 16 bytes' worth of elements.
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
+// The box of the map at (x, y, z).  x: innermost coordinate, a multiple of 16 bytes' worth of elements.
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
 {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-                 "l"(map), "r"(x), "r"(y), "r"(bar)
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
                  : "memory");
 }
 
@@ -131,18 +131,6 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn, uint32_t r
 {
     const uint64_t lead = mn ? (uint64_t)(block >> 4) : 1, step = mn ? 1024 : 8 * row, swizzle = mn || row == 128 ? 2 : 4;
     return (uint64_t)((addr & 0x3ffff) >> 4) | (lead << 16) | ((step >> 4) << 32) | (1ull << 46) | (swizzle << 61);
-}
-
-template <int N>
-__device__ __forceinline__ void more_registers()
-{
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
-}
-
-template <int N>
-__device__ __forceinline__ void fewer_registers()
-{
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
 
 // 32 columns of the warp's 32 lanes of tensor memory (a warp reaches the lanes 32 (warp % 4) and up).  The registers hold them after
