@@ -414,7 +414,8 @@ typedef enum flashbev_norm {
  * channel, a batch's size for one per sample, `rows` for one per row.  Without y, h = x and only n is computed.  Statistics and h are
  * fp32 and n is formed from the unrounded h; the mean is taken off before the squares are summed; h and n are rounded once.  One kernel;
  * rows = 0 enqueues nothing.  h may be x and n may be y (same address and stride); no other overlap.  Pointers element-aligned,
- * else FLASHBEV_MISALIGNED.  C <= FLASHBEV_NORM_MAX_CHANNELS and rows < 2^31, else FLASHBEV_UNSUPPORTED.
+ * else FLASHBEV_MISALIGNED.  C <= FLASHBEV_NORM_MAX_CHANNELS, rows and strides < 2^31, else
+ * FLASHBEV_UNSUPPORTED.
  */
 #define FLASHBEV_NORM_MAX_CHANNELS 4096
 typedef struct flashbev_block_norm_params {

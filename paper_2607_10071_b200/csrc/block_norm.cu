@@ -40,8 +40,8 @@ struct NormParams {
     void *gx, *gy, *ggate;
     float *sums;                // backward: [array][block][C] partial sums of the parameters' gradients
     int want;                   // which arrays: bit 0 after weight, 1 after bias, 2 before weight, 3 before bias, 4 gate
-    long long rows, per_gate;   // per_gate: rows that share a gate
-    long long ld_x, ld_y, ld_h, ld_n, ld_gh, ld_gn, ld_gx, ld_gy;
+    unsigned rows, per_gate;    // per_gate: rows that share a gate
+    unsigned ld_x, ld_y, ld_h, ld_n, ld_gh, ld_gn, ld_gx, ld_gy;
     int C, after, before, team; // team: threads per row
     int chunks, direct;         // backward: blocks per gate; or `direct`: a team takes whole gates
     long long gates;
@@ -56,7 +56,7 @@ struct Eight {
 
 template <typename T>
 struct Raw {
-    T v[kE];
+    uint32_t w[kE * sizeof(T) / 4];
 };
 
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
@@ -79,56 +79,77 @@ __device__ __forceinline__ bool has(int i, int t, int team, int C)
 template <typename T, int VEC>
 __device__ __forceinline__ void read(Raw<T> &r, const T *row, int t, int team, int C)
 {
+    constexpr bool kWide = sizeof(T) == 4;
     if constexpr (VEC == 8) {
-        constexpr int Q = kE * (int)sizeof(T) / 16;
         if (t * 8 < C) {
-            uint4 q[Q];
 #pragma unroll
-            for (int i = 0; i < Q; ++i) q[i] = reinterpret_cast<const uint4 *>(row + t * 8)[i];
-            memcpy(r.v, q, sizeof(q));
+            for (int i = 0; i < (kWide ? 2 : 1); ++i) {
+                const uint4 q = reinterpret_cast<const uint4 *>(row + t * 8)[i];
+                r.w[4 * i] = q.x, r.w[4 * i + 1] = q.y, r.w[4 * i + 2] = q.z, r.w[4 * i + 3] = q.w;
+            }
         }
     } else if constexpr (VEC == 2) {
-        using Pair = typename std::conditional<sizeof(T) == 4, uint2, uint32_t>::type;
 #pragma unroll
-        for (int i = 0; i < kE; i += 2)
-            if (has<2>(i, t, team, C)) {
-                const Pair q = *reinterpret_cast<const Pair *>(row + column<2>(i, t, team));
-                memcpy(r.v + i, &q, sizeof(q));
+        for (int i = 0; i < 4; ++i)
+            if (has<2>(2 * i, t, team, C)) {
+                if constexpr (kWide) {
+                    const uint2 q = *reinterpret_cast<const uint2 *>(row + column<2>(2 * i, t, team));
+                    r.w[2 * i] = q.x, r.w[2 * i + 1] = q.y;
+                } else {
+                    r.w[i] = *reinterpret_cast<const uint32_t *>(row + column<2>(2 * i, t, team));
+                }
             }
     } else {
 #pragma unroll
         for (int i = 0; i < kE; ++i)
-            if (has<1>(i, t, team, C)) r.v[i] = row[column<1>(i, t, team)];
+            if (has<1>(i, t, team, C)) {
+                if constexpr (kWide) r.w[i] = *reinterpret_cast<const uint32_t *>(row + column<1>(i, t, team));
+                else if (i % 2) r.w[i / 2] = (r.w[i / 2] & 0xffffu) | (uint32_t)*reinterpret_cast<const unsigned short *>(row + column<1>(i, t, team)) << 16;
+                else r.w[i / 2] = *reinterpret_cast<const unsigned short *>(row + column<1>(i, t, team));
+            }
     }
+}
+
+// The pair 2 i, 2 i + 1
+template <typename T>
+__device__ __forceinline__ float2 pair_of(const Raw<T> &r, int i)
+{
+    if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(r.w[2 * i]), __uint_as_float(r.w[2 * i + 1]));
+    else return make_float2(__uint_as_float(r.w[i] << 16), __uint_as_float(r.w[i] & 0xffff0000u));
+}
+
+__device__ __forceinline__ uint32_t pack(float2 v)  // two bf16
+{
+    const __nv_bfloat162 b = __floats2bfloat162_rn(v.x, v.y);
+    uint32_t r;
+    memcpy(&r, &b, 4);
+    return r;
 }
 
 template <typename T, int VEC>
 __device__ __forceinline__ void write(T *row, const Eight &f, int t, int team, int C)
 {
-    Raw<T> r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r.v[2 * i] = from_float<T>(f.p[i].x), r.v[2 * i + 1] = from_float<T>(f.p[i].y);
+    constexpr bool kWide = sizeof(T) == 4;
     if constexpr (VEC == 8) {
-        constexpr int Q = kE * (int)sizeof(T) / 16;
-        if (t * 8 < C) {
-            uint4 q[Q];
-            memcpy(q, r.v, sizeof(q));
-#pragma unroll
-            for (int i = 0; i < Q; ++i) reinterpret_cast<uint4 *>(row + t * 8)[i] = q[i];
+        if (t * 8 >= C) return;
+        uint4 *const to = reinterpret_cast<uint4 *>(row + t * 8);
+        if constexpr (kWide) {
+            to[0] = make_uint4(__float_as_uint(f.p[0].x), __float_as_uint(f.p[0].y), __float_as_uint(f.p[1].x), __float_as_uint(f.p[1].y));
+            to[1] = make_uint4(__float_as_uint(f.p[2].x), __float_as_uint(f.p[2].y), __float_as_uint(f.p[3].x), __float_as_uint(f.p[3].y));
+        } else {
+            to[0] = make_uint4(pack(f.p[0]), pack(f.p[1]), pack(f.p[2]), pack(f.p[3]));
         }
     } else if constexpr (VEC == 2) {
-        using Pair = typename std::conditional<sizeof(T) == 4, uint2, uint32_t>::type;
 #pragma unroll
-        for (int i = 0; i < kE; i += 2)
-            if (has<2>(i, t, team, C)) {
-                Pair q;
-                memcpy(&q, r.v + i, sizeof(q));
-                *reinterpret_cast<Pair *>(row + column<2>(i, t, team)) = q;
+        for (int i = 0; i < 4; ++i)
+            if (has<2>(2 * i, t, team, C)) {
+                if constexpr (kWide) *reinterpret_cast<float2 *>(row + column<2>(2 * i, t, team)) = f.p[i];
+                else *reinterpret_cast<uint32_t *>(row + column<2>(2 * i, t, team)) = pack(f.p[i]);
             }
     } else {
 #pragma unroll
         for (int i = 0; i < kE; ++i)
-            if (has<1>(i, t, team, C)) row[column<1>(i, t, team)] = r.v[i];
+            if (has<1>(i, t, team, C)) row[column<1>(i, t, team)] = from_float<T>(i % 2 ? f.p[i / 2].y : f.p[i / 2].x);
     }
 }
 
@@ -138,7 +159,7 @@ __device__ __forceinline__ void widen(Eight &f, const Raw<T> &r, int t, int team
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        f.p[i] = make_float2(to_float(r.v[2 * i]), to_float(r.v[2 * i + 1]));
+        f.p[i] = pair_of<T>(r, i);
         if (VEC != 8 && !has<VEC>(2 * i, t, team, C)) f.p[i].x = 0.0f;
         if (VEC != 8 && !has<VEC>(2 * i + 1, t, team, C)) f.p[i].y = 0.0f;
     }
@@ -326,6 +347,13 @@ __device__ __forceinline__ Team<WIDE> make_team(const NormParams &p, float2 *sha
 constexpr int kMostThreads = FLASHBEV_NORM_MAX_CHANNELS / kE;
 static_assert(kMostThreads <= 512, "the sums of a team's warps are added up by half a warp");
 
+// Row `row` of a matrix (one 32 x 32 -> 64 bit product)
+template <typename T>
+__device__ __forceinline__ T *row_of(const void *base, unsigned row, unsigned ld)
+{
+    return const_cast<T *>(static_cast<const T *>(base)) + (unsigned long long)row * ld;
+}
+
 // S, T, P: types of x and h, of y and n, of the parameters.
 template <typename S, typename T, typename P, int VEC, bool WIDE>
 __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 3) norm_kernel(const __grid_constant__ NormParams p)
@@ -337,20 +365,21 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 3) norm_
     const int t = team.t, threads = p.team, C = p.C, teams = blockDim.x / threads;
     extern __shared__ __align__(16) float params[];  // before weight, before bias, after weight, after bias
     stage_params<P, VEC>(params, {p.wb, p.bb, p.wa, p.ba}, p.after != FLASHBEV_NORM_NONE ? 4 : 2, C);
-    const long long step = (long long)gridDim.x * teams, first = (long long)blockIdx.x * teams + team.slot;
+    // (rows are below 2^31, and so is a step: none of the sums wraps)
+    const unsigned step = gridDim.x * teams, first = blockIdx.x * teams + team.slot;
     // (narrow teams share a warp's shuffles: all of them go as long as one has a row)
-    const long long lead = WIDE ? first : first - (threadIdx.x % 32) / threads;
+    const unsigned lead = WIDE ? first : first - (threadIdx.x % 32) / threads;
     Raw<S> xr;
     Raw<T> yr;
-    const auto bring = [&](long long row) {
+    const auto bring = [&](unsigned row) {
         if (row >= p.rows) return;
-        read<S, VEC>(xr, static_cast<const S *>(p.x) + row * p.ld_x, t, threads, C);
-        if (p.y) read<T, VEC>(yr, static_cast<const T *>(p.y) + row * p.ld_y, t, threads, C);
+        read<S, VEC>(xr, row_of<const S>(p.x, row, p.ld_x), t, threads, C);
+        if (p.y) read<T, VEC>(yr, row_of<const T>(p.y, row, p.ld_y), t, threads, C);
     };
     bring(first);
     Eight gate = eight(p.scale);
-    long long gate_end = 0;  // the row behind the last one with this gate
-    for (long long row = first, at = lead; at < p.rows; row += step, at += step) {
+    unsigned gate_end = 0;  // the row behind the last one with this gate
+    for (unsigned row = first, at = lead; at < p.rows; row += step, at += step) {
         const bool live = row < p.rows;
         Eight h, m;
         widen<S, VEC>(h, xr, t, threads, C);
@@ -362,18 +391,18 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 3) norm_
                 m = fma(m, read_param<VEC>(params + 2 * C, t, threads, C), read_param<VEC>(params + 3 * C, t, threads, C));
             }
             if (p.gate && live && row >= gate_end) {
-                const long long g = (int)row / (int)p.per_gate;
+                const unsigned g = row / p.per_gate;
                 gate = read_gate<P, VEC>(p.gate, g, p.scale, t, threads, C);
                 gate_end = (g + 1) * p.per_gate;
             }
             h = fma(m, gate, h);
-            if (p.h && live) write<S, VEC>(static_cast<S *>(p.h) + row * p.ld_h, h, t, threads, C);
+            if (p.h && live) write<S, VEC>(row_of<S>(p.h, row, p.ld_h), h, t, threads, C);
         }
         if (p.before != FLASHBEV_NORM_NONE) {
             trim<VEC>(h, team, C);  // (of the norm's bias)
             whiten<VEC, WIDE>(h, p.before, p, team);
             h = fma(h, read_param<VEC>(params, t, threads, C), read_param<VEC>(params + C, t, threads, C));
-            if (live) write<T, VEC>(static_cast<T *>(p.n) + row * p.ld_n, h, t, threads, C);
+            if (live) write<T, VEC>(row_of<T>(p.n, row, p.ld_n), h, t, threads, C);
         }
     }
 }
@@ -404,30 +433,30 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 2) norm_
         g = g_lead = blockIdx.x / p.chunks, g_step = p.gates;
     }
     for (; g_lead < p.gates; g += g_step, g_lead += g_step) {
-        long long row, end, step;
+        unsigned row, end, step;
         const bool mine = g < p.gates;
         if (p.direct) {
-            row = g * p.per_gate, end = mine ? row + p.per_gate : 0, step = 1;
+            row = (unsigned)(g * p.per_gate), end = mine ? row + p.per_gate : 0, step = 1;
         } else {
             const int chunk = (int)(blockIdx.x - g * p.chunks);
-            const long long base = g * p.per_gate, share = (p.per_gate + p.chunks - 1) / p.chunks;
+            const unsigned base = (unsigned)(g * p.per_gate), share = (p.per_gate + p.chunks - 1) / p.chunks;
             end = base + min(p.per_gate, (chunk + 1) * share);
             row = base + chunk * share + team.slot, step = teams;
         }
         // every team of a warp goes around as often
-        const long long rounds = p.direct ? p.per_gate : (end - (row - inside) + step - 1) / step;
+        const unsigned warp_row = row - inside, rounds = p.direct ? p.per_gate : (warp_row < end ? (end - warp_row + step - 1) / step : 0);
         const Eight gate = read_gate<P, VEC>(p.gate, mine ? g : 0, p.scale, t, threads, C);
         Raw<S> xr, ghr;
         Raw<T> yr, gnr;
-        const auto bring = [&](long long at) {
+        const auto bring = [&](unsigned at) {
             if (at >= end) return;
-            read<S, VEC>(xr, static_cast<const S *>(p.x) + at * p.ld_x, t, threads, C);
-            if (p.y) read<T, VEC>(yr, static_cast<const T *>(p.y) + at * p.ld_y, t, threads, C);
-            if (p.gn) read<T, VEC>(gnr, static_cast<const T *>(p.gn) + at * p.ld_gn, t, threads, C);
-            if (p.gh) read<S, VEC>(ghr, static_cast<const S *>(p.gh) + at * p.ld_gh, t, threads, C);
+            read<S, VEC>(xr, row_of<const S>(p.x, at, p.ld_x), t, threads, C);
+            if (p.y) read<T, VEC>(yr, row_of<const T>(p.y, at, p.ld_y), t, threads, C);
+            if (p.gn) read<T, VEC>(gnr, row_of<const T>(p.gn, at, p.ld_gn), t, threads, C);
+            if (p.gh) read<S, VEC>(ghr, row_of<const S>(p.gh, at, p.ld_gh), t, threads, C);
         };
         bring(row);
-        for (long long round = 0; round < rounds; ++round, row += step) {
+        for (unsigned round = 0; round < rounds; ++round, row += step) {
             const bool live = row < end;
             Eight u, v, gn, gh = eight(0.0f);
             widen<S, VEC>(u, xr, t, threads, C);
@@ -453,7 +482,7 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 2) norm_
                 whiten_back<VEC, WIDE>(gn, u, rb, p.before, p, team);
                 gh = gh + gn;
             }
-            if (p.gx && live) write<S, VEC>(static_cast<S *>(p.gx) + row * p.ld_gx, gh, t, threads, C);
+            if (p.gx && live) write<S, VEC>(row_of<S>(p.gx, row, p.ld_gx), gh, t, threads, C);
             if (!p.y) continue;
             if (live && p.ggate) dg = fma(gh * eight(p.scale), branch(), dg);
             gh = gh * gate;
@@ -462,7 +491,7 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 2) norm_
                 gh = gh * read_param<VEC>(params + 2 * C, t, threads, C);
                 whiten_back<VEC, WIDE>(gh, v, ra, p.after, p, team);
             }
-            if (p.gy && live) write<T, VEC>(static_cast<T *>(p.gy) + row * p.ld_gy, gh, t, threads, C);
+            if (p.gy && live) write<T, VEC>(row_of<T>(p.gy, row, p.ld_gy), gh, t, threads, C);
         }
         if (p.direct) {
             if (p.ggate && mine) write<P, VEC>(static_cast<P *>(p.ggate) + g * C, dg, t, threads, C);
@@ -541,7 +570,7 @@ __global__ void __launch_bounds__(512) norm_sum_kernel(const float *__restrict__
 bool dtype_ok(int d) { return d == FLASHBEV_F32 || d == FLASHBEV_BF16; }
 size_t elem_size(int d) { return d == FLASHBEV_F32 ? 4 : 2; }
 bool aligned(const void *p, int dtype) { return (uintptr_t)p % elem_size(dtype) == 0; }
-long long dense(long long ld, int C) { return ld ? ld : C; }
+unsigned dense(long long ld, int C) { return ld ? (unsigned)ld : (unsigned)C; }  // (below 2^31: check_common)
 
 int team_threads(int C)
 {
@@ -568,7 +597,7 @@ flashbev_status check_common(const Q *p, std::initializer_list<int64_t> strides)
     if (p->param_dtype == FLASHBEV_BF16 && p->branch_dtype == FLASHBEV_F32) return FLASHBEV_UNSUPPORTED;
     if (p->C > FLASHBEV_NORM_MAX_CHANNELS || p->rows > 2147483647LL) return FLASHBEV_UNSUPPORTED;
     for (long long ld : strides)
-        if ((double)p->rows * (double)dense(ld, p->C) >= 2305843009213693952.0) return FLASHBEV_UNSUPPORTED;
+        if (ld > 2147483647LL) return FLASHBEV_UNSUPPORTED;
     const void *const params[] = {p->gate, p->after_weight, p->after_bias, p->before_weight};
     for (const void *v : params)
         if (!aligned(v, p->param_dtype)) return FLASHBEV_MISALIGNED;
@@ -704,7 +733,7 @@ flashbev_status flashbev_block_norm(const flashbev_block_norm_params *p, void *s
     }
     NormParams k = {};
     k.x = p->x, k.y = p->y, k.gate = p->gate, k.wa = p->after_weight, k.ba = p->after_bias, k.wb = p->before_weight, k.bb = p->before_bias;
-    k.h = p->h, k.n = p->n, k.rows = p->rows, k.per_gate = p->gate ? p->rows / p->gate_groups : p->rows;
+    k.h = p->h, k.n = p->n, k.rows = (unsigned)p->rows, k.per_gate = (unsigned)(p->gate ? p->rows / p->gate_groups : p->rows);
     k.ld_x = dense(p->ld_x, p->C), k.ld_y = dense(p->ld_y, p->C), k.ld_h = dense(p->ld_h, p->C), k.ld_n = dense(p->ld_n, p->C);
     k.C = p->C, k.after = p->after, k.before = p->before, k.scale = (float)p->scale, k.eps = (float)p->eps, k.inv_c = 1.0f / (float)p->C;
     k.team = team_threads(p->C);
@@ -750,7 +779,7 @@ flashbev_status flashbev_block_norm_backward(const flashbev_block_norm_backward_
     k.x = p->x, k.y = p->y, k.gate = p->gate, k.wa = p->after_weight, k.ba = p->after_bias, k.wb = p->before_weight;
     k.gh = p->grad_h, k.gn = p->grad_n, k.gx = p->grad_x, k.gy = p->grad_y, k.ggate = p->grad_gate;
     k.sums = static_cast<float *>(p->workspace), k.want = s.want;
-    k.rows = p->rows, k.gates = s.gates, k.per_gate = p->rows / s.gates, k.chunks = s.chunks, k.direct = s.direct;
+    k.rows = (unsigned)p->rows, k.gates = s.gates, k.per_gate = (unsigned)(p->rows / s.gates), k.chunks = s.chunks, k.direct = s.direct;
     k.ld_x = dense(p->ld_x, p->C), k.ld_y = dense(p->ld_y, p->C), k.ld_gh = dense(p->ld_grad_h, p->C), k.ld_gn = dense(p->ld_grad_n, p->C);
     k.ld_gx = dense(p->ld_grad_x, p->C), k.ld_gy = dense(p->ld_grad_y, p->C);
     k.C = p->C, k.after = p->after, k.before = p->before, k.scale = (float)p->scale, k.eps = (float)p->eps, k.inv_c = 1.0f / (float)p->C;
