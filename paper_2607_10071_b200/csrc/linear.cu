@@ -175,14 +175,13 @@ __device__ __forceinline__ float2 slope_times(float2 g, float2 z, int act)
 // pieces: 1 (bf16) or 3 (float32).  K of a stage: a swizzled row of 64 numbers, or of 32 where an operand has three tiles: three stages of 48 KB
 // (two of 96 KB: 59 us against 45 for 40000 x 256 x 256).
 __host__ __device__ constexpr int block_k(int pieces) { return pieces == 3 ? 32 : 64; }
-// Warps of the epilogue: 16, as it is their latency that a short sum waits for (64-column sums of 184950 rows, 64 columns: 25 us with eight,
-// 20 us with 16).  Three pieces are six times the products; they leave eight, and shared memory for a third stage.  (Registers are those of a
-// quarter of an SM: the last warps of four, which do nothing, cost none.)
-__host__ __device__ constexpr int epilogue_warps(int pieces) { return pieces == 3 ? 8 : 16; }
-__host__ __device__ constexpr int gemm_threads(int pieces) { return 32 * (epilogue_warps(pieces) + 4); }
+// Warps of the epilogue (EW): 16 for short sums, as it is their latency that those wait for (64-column sums of 184950 rows, 64 columns:
+// 25 us with eight, 20 us with 16); eight for long ones and for pieces, which leaves shared memory for a fourth stage of 48 KB.  (Registers are
+// those of a quarter of an SM: the last warps of four, which do nothing, cost none.)
+__host__ __device__ constexpr int gemm_threads(int ew) { return 32 * (ew + 4); }
 // Bytes behind the ring: a buffer of 32 rows x 128 bytes and a bias of 64 columns per epilogue warp.
-__host__ __device__ constexpr int epilogue_bytes(int pieces) { return epilogue_warps(pieces) * (4096 + 256); }
-__host__ __device__ constexpr int ring_bytes(int pieces) { return (kSmemLimit - kControlBytes - epilogue_bytes(pieces)) / 1024 * 1024; }
+__host__ __device__ constexpr int epilogue_bytes(int ew) { return ew * (4096 + 256); }
+__host__ __device__ constexpr int ring_bytes(int ew) { return (kSmemLimit - kControlBytes - epilogue_bytes(ew)) / 1024 * 1024; }
 constexpr int kAccs = 4;            // most accumulators in tensor memory
 
 struct alignas(64) GemmParams {
@@ -365,15 +364,15 @@ __device__ __forceinline__ Share share_of(const GemmParams &p, int w)
     return s;
 }
 
-template <int kPieces, typename TOUT>
-__global__ void __launch_bounds__(gemm_threads(kPieces), 1) gemm_kernel(const __grid_constant__ GemmParams p)
+template <int kPieces, typename TOUT, int kEpilogue>
+__global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const __grid_constant__ GemmParams p)
 {
     using TIN = typename std::conditional<kPieces == 3, float, bf16>::type;
-    constexpr int kEpilogue = epilogue_warps(kPieces), BK = block_k(kPieces), kRing = ring_bytes(kPieces);
+    constexpr int BK = block_k(kPieces), kRing = ring_bytes(kEpilogue);
     extern __shared__ __align__(1024) unsigned char ring[];  // (the kernel declares no other: it starts on a swizzle's boundary)
     unsigned char *const staging = ring + kRing;
     float *const bias_rows = reinterpret_cast<float *>(staging + kEpilogue * 4096);  // 64 per warp
-    uint64_t *const bars = reinterpret_cast<uint64_t *>(staging + epilogue_bytes(kPieces));  // 2 * 8 + 2 * kAccs + 1
+    uint64_t *const bars = reinterpret_cast<uint64_t *>(staging + epilogue_bytes(kEpilogue));  // 2 * 8 + 2 * kAccs + 1
     uint32_t &tmem_slot = *reinterpret_cast<uint32_t *>(bars + 2 * 8 + 2 * kAccs + 1);
     volatile int &failed = *reinterpret_cast<volatile int *>(&tmem_slot + 1);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -967,9 +966,12 @@ bool make_store_map(CUtensorMap &map, void *p, bool f32, int M, int N, long long
 // K after which a float32 result's sum is taken out of the tensor cores: 24 instructions that cut it off, 8e-7 of it.
 constexpr int kRun = 384;
 
+// Sums up to this long wait for the epilogue.
+constexpr int kShort = 256;
+
 // Tiles and shares of a product.
 struct Plan {
-    int bn, stages, tiles_m, tiles_n, kblocks, kshare, splits, run, columns, accs, groups;
+    int ew, bn, stages, tiles_m, tiles_n, kblocks, kshare, splits, run, columns, accs, groups;
     long long ld_partial;
     size_t partial_bytes;  // 0: every tile's sum belongs to one CTA
 };
@@ -1000,11 +1002,12 @@ Plan plan_product(bool b_mn, bool f32, bool out_f32, int M, int N, int K, bool m
         if (t > 64) break;  // (wide results: the widest tiles)
     }
     q.tiles_n = (N + q.bn - 1) / q.bn;
-    q.stages = std::min(8, ring_bytes(pieces) / (pieces * (kBM + q.bn) * 2 * bk));
+    q.ew = f32 || q.kshare * bk > kShort ? 8 : 16;
+    q.stages = std::min(8, ring_bytes(q.ew) / (pieces * (kBM + q.bn) * 2 * bk));
     q.run = runs && q.kshare > kRun / bk ? kRun / bk : q.kshare;
     // Accumulators: with runs two, the running sum and, of float32 operands, that of the small products; else four where they fit (float32
     // operands: pairs).  Groups of epilogue warps: as many 64-column parts as the tile has in each, and no more of them than accumulators.
-    const int parts = f32 ? 2 : 1, warps = epilogue_warps(pieces) / 4, wide = (q.bn + 63) / 64;
+    const int parts = f32 ? 2 : 1, warps = q.ew / 4, wide = (q.bn + 63) / 64;
     const bool in_runs = q.run < q.kshare;
     q.accs = !in_runs && 4 * parts * q.bn <= 512 ? 4 : 2;
     const int used = in_runs ? (2 + parts) * q.bn : q.accs * parts * q.bn;
@@ -1032,16 +1035,16 @@ bool vec_ok(const void *p, long long ld, bool f32)
     return ((uintptr_t)p | (uintptr_t)(ld * (f32 ? 4 : 2))) % 16 == 0 && ld < (1LL << 37);
 }
 
-template <int PIECES, typename TOUT>
+template <int PIECES, typename TOUT, int EW>
 cudaError_t launch_gemm(const GemmParams &g, cudaStream_t stream)
 {
-    const auto kernel = gemm_kernel<PIECES, TOUT>;
-    constexpr int smem = ring_bytes(PIECES) + epilogue_bytes(PIECES) + kControlBytes;
-    static_assert(smem <= kSmemLimit && ring_bytes(3) >= 3 * 3 * (kBM + 128) * 2 * block_k(3), "");
+    const auto kernel = gemm_kernel<PIECES, TOUT, EW>;
+    constexpr int smem = ring_bytes(EW) + epilogue_bytes(EW) + kControlBytes;
+    static_assert(smem <= kSmemLimit && ring_bytes(8) >= 4 * 48 * 1024 && ring_bytes(16) >= 3 * 48 * 1024, "");
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     const int grid = std::min(g.tiles * g.splits, sm_count());
-    return launch_dependent(kernel, dim3((unsigned)grid), dim3((unsigned)gemm_threads(PIECES)), smem, stream, g);
+    return launch_dependent(kernel, dim3((unsigned)grid), dim3((unsigned)gemm_threads(EW)), smem, stream, g);
 }
 
 // Lays one or two operands out in the scratch
@@ -1094,8 +1097,9 @@ flashbev_status run_product(const Plan &q, const Operand &a, const Operand &b, b
         if (e.pre && !make_store_map(g.tpre, e.pre, f32, M, N, e.ld_pre, 1)) return FLASHBEV_CUDA_ERROR;
     }
     cudaError_t err;
-    if (f32) err = e.out_f32 ? launch_gemm<3, float>(g, stream) : launch_gemm<3, bf16>(g, stream);
-    else err = e.out_f32 ? launch_gemm<1, float>(g, stream) : launch_gemm<1, bf16>(g, stream);
+    if (f32) err = e.out_f32 ? launch_gemm<3, float, 8>(g, stream) : launch_gemm<3, bf16, 8>(g, stream);
+    else if (q.ew == 8) err = e.out_f32 ? launch_gemm<1, float, 8>(g, stream) : launch_gemm<1, bf16, 8>(g, stream);
+    else err = e.out_f32 ? launch_gemm<1, float, 16>(g, stream) : launch_gemm<1, bf16, 16>(g, stream);
     ++launches;
     if (err == cudaSuccess && q.splits > 1) {
         if (f32) err = e.out_f32 ? launch_join<float, float>(q, partial, M, N, e, stream) : launch_join<float, bf16>(q, partial, M, N, e, stream);
