@@ -196,6 +196,8 @@ struct alignas(64) GemmParams {
     int accs;                   // accumulators in it
     int groups;                 // of epilogue warps, which take accumulators in turn
     int store_tma;              // the results leave through TMA stores
+    int wide;                   // ... of 64 columns
+    int kept;                   // bytes of B that stay in shared memory: all of the CTA's columns, one tile per block of K; or 0
     void *out, *pre;            // pre: z, or NULL
     const void *residual, *bias;
     long long ld_out, ld_pre, ld_res;
@@ -216,10 +218,13 @@ constexpr int kPieces32 = 32 / kPiece<T>;    // pieces of a row; also the warp's
 template <typename T>
 constexpr int kRows32 = 32 / kPieces32<T>;   // rows of an access
 
+// Where a row's piece lies.  Rows of 128 bytes: float32 tiles, and bf16 ones that are half of a tile of 64 columns (`half` 0 or 1); rows of 64 bytes:
+// bf16 tiles by themselves (`half` -1).
 template <typename T>
-__device__ __forceinline__ int piece_at(int row, int piece)
+__device__ __forceinline__ int piece_at(int row, int piece, int half)
 {
-    return kPieces32<T> == 8 ? row * 128 + ((piece ^ (row & 7)) << 4) : row * 64 + ((piece ^ (row >> 1 & 3)) << 4);
+    if (kPieces32<T> == 8) return row * 128 + ((piece ^ (row & 7)) << 4);
+    return half < 0 ? row * 64 + ((piece ^ (row >> 1 & 3)) << 4) : row * 128 + (((piece + 4 * half) ^ (row & 7)) << 4);
 }
 
 template <typename T>
@@ -261,19 +266,19 @@ __device__ __forceinline__ uint4 piece_of(const float *v)
 
 // The lane's row into a tile
 template <typename T>
-__device__ __forceinline__ void row_store(const float (&v)[32], unsigned char *tile, int lane)
+__device__ __forceinline__ void row_store(const float (&v)[32], unsigned char *tile, int half, int lane)
 {
 #pragma unroll
-    for (int c = 0; c < kPieces32<T>; ++c) *reinterpret_cast<uint4 *>(tile + piece_at<T>(lane, c)) = piece_of<T>(v + kPiece<T> * c);
+    for (int c = 0; c < kPieces32<T>; ++c) *reinterpret_cast<uint4 *>(tile + piece_at<T>(lane, c, half)) = piece_of<T>(v + kPiece<T> * c);
 }
 
 // ... and added to from one
 template <typename T>
-__device__ __forceinline__ void row_add(float (&v)[32], const unsigned char *tile, int lane)
+__device__ __forceinline__ void row_add(float (&v)[32], const unsigned char *tile, int half, int lane)
 {
 #pragma unroll
     for (int c = 0; c < kPieces32<T>; ++c) {
-        const uint4 q = *reinterpret_cast<const uint4 *>(tile + piece_at<T>(lane, c));
+        const uint4 q = *reinterpret_cast<const uint4 *>(tile + piece_at<T>(lane, c, half));
         const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -304,17 +309,17 @@ __device__ __forceinline__ void tile_load(uint4 (&r)[kPieces32<T>], const T *bas
 }
 
 template <typename T>
-__device__ __forceinline__ void tile_stage(const uint4 (&r)[kPieces32<T>], bool vec, unsigned char *tile, int lane)
+__device__ __forceinline__ void tile_stage(const uint4 (&r)[kPieces32<T>], bool vec, unsigned char *tile, int half, int lane)
 {
     if (vec) {
 #pragma unroll
         for (int i = 0; i < kPieces32<T>; ++i)
-            *reinterpret_cast<uint4 *>(tile + piece_at<T>(kRows32<T> * i + lane / kPieces32<T>, lane % kPieces32<T>)) = r[i];
+            *reinterpret_cast<uint4 *>(tile + piece_at<T>(kRows32<T> * i + lane / kPieces32<T>, lane % kPieces32<T>, half)) = r[i];
     } else {
         T v[32];
         memcpy(v, r, sizeof(v));
 #pragma unroll
-        for (int i = 0; i < 32; ++i) reinterpret_cast<T *>(tile + piece_at<T>(i, lane / kPiece<T>))[lane % kPiece<T>] = v[i];
+        for (int i = 0; i < 32; ++i) reinterpret_cast<T *>(tile + piece_at<T>(i, lane / kPiece<T>, half))[lane % kPiece<T>] = v[i];
     }
     __syncwarp();
 }
@@ -336,35 +341,45 @@ __device__ __forceinline__ void tile_leave(const unsigned char *tile, const CUte
         T *p = base + row * ld + col;
 #pragma unroll
         for (int i = 0; i < kPieces32<T>; ++i, p += kRows32<T> * ld) {
-            const uint4 q = *reinterpret_cast<const uint4 *>(tile + piece_at<T>(kRows32<T> * i + lane / kPieces32<T>, lane % kPieces32<T>));
+            const uint4 q = *reinterpret_cast<const uint4 *>(tile + piece_at<T>(kRows32<T> * i + lane / kPieces32<T>, lane % kPieces32<T>, -1));
             if (row + kRows32<T> * i < M && col < N) store_piece(p, q, N - col);
         }
     } else if (col0 + lane < N) {
         T *p = base + row0 * ld + col0 + lane;
 #pragma unroll 8
-        for (int i = 0; i < min(32, M - row0); ++i, p += ld) *p = reinterpret_cast<const T *>(tile + piece_at<T>(i, lane / kPiece<T>))[lane % kPiece<T>];
+        for (int i = 0; i < min(32, M - row0); ++i, p += ld) *p = reinterpret_cast<const T *>(tile + piece_at<T>(i, lane / kPiece<T>, -1))[lane % kPiece<T>];
     }
     __syncwarp();
 }
 
-// A share of a tile's sum: tile (m0, n0) and the blocks [k, end) of K.
-struct Share {
-    int m0, n0, k, end, split;
+// The shares of tiles' sums that a CTA takes, every gridDim.x-th: tile (m0, n0) and the blocks [k, end) of K.
+struct Shares {
+    int w, m, n, dm, dn, m0, n0, k, end, split;
+
+    __device__ __forceinline__ explicit Shares(const GemmParams &p)
+    {
+        w = blockIdx.x, split = w / p.tiles;
+        const int t = w - split * p.tiles;
+        m = t / p.tiles_n, n = t - m * p.tiles_n;
+        dm = gridDim.x / p.tiles_n, dn = gridDim.x - dm * p.tiles_n;
+        k = split * p.kshare, end = min(k + p.kshare, p.kblocks);
+        m0 = m * kBM, n0 = n * p.bn;
+    }
+    __device__ __forceinline__ bool more(const GemmParams &p) const { return w < p.tiles * p.splits; }
+    // (with several shares to a tile the grid has a CTA for each of them)
+    __device__ __forceinline__ void next(const GemmParams &p)
+    {
+        w += gridDim.x, m += dm, n += dn;
+        if (n >= p.tiles_n) n -= p.tiles_n, ++m;
+        m0 = m * kBM, n0 = n * p.bn;
+    }
 };
 
-__device__ __forceinline__ Share share_of(const GemmParams &p, int w)
-{
-    Share s;
-    s.split = w / p.tiles;
-    const int t = w - s.split * p.tiles;
-    const int m = t / p.tiles_n;
-    s.m0 = m * kBM, s.n0 = (t - m * p.tiles_n) * p.bn;
-    s.k = s.split * p.kshare;
-    s.end = min(s.k + p.kshare, p.kblocks);
-    return s;
-}
+// MODE: an activation, for bf16 results that leave by TMA, or kAny: everything as the parameters say.  What an instance does not need would be in its
+// way: the code of the other activations and of rows of any alignment, skipped, cost 8 of 37 us (184950 x 64 x 256) in instruction fetches.
+constexpr int kAny = 4;
 
-template <int kPieces, typename TOUT, int kEpilogue>
+template <int kPieces, typename TOUT, int kEpilogue, int MODE>
 __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const __grid_constant__ GemmParams p)
 {
     using TIN = typename std::conditional<kPieces == 3, float, bf16>::type;
@@ -372,17 +387,17 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
     extern __shared__ __align__(1024) unsigned char ring[];  // (the kernel declares no other: it starts on a swizzle's boundary)
     unsigned char *const staging = ring + kRing;
     float *const bias_rows = reinterpret_cast<float *>(staging + kEpilogue * 4096);  // 64 per warp
-    uint64_t *const bars = reinterpret_cast<uint64_t *>(staging + epilogue_bytes(kEpilogue));  // 2 * 8 + 2 * kAccs + 1
-    uint32_t &tmem_slot = *reinterpret_cast<uint32_t *>(bars + 2 * 8 + 2 * kAccs + 1);
+    uint64_t *const bars = reinterpret_cast<uint64_t *>(staging + epilogue_bytes(kEpilogue));  // 2 * 8 + 2 * kAccs + 2
+    uint32_t &tmem_slot = *reinterpret_cast<uint32_t *>(bars + 2 * 8 + 2 * kAccs + 2);
     volatile int &failed = *reinterpret_cast<volatile int *>(&tmem_slot + 1);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const uint32_t full = smem_u32(bars), empty = full + 64, acc_full = full + 128, acc_empty = acc_full + 8 * kAccs, last = acc_empty + 8 * kAccs;
+    const uint32_t full = smem_u32(bars), empty = full + 64, acc_full = full + 128, acc_empty = acc_full + 8 * kAccs, last = acc_empty + 8 * kAccs, kept_full = last + 8;
     // Tensor memory.  Two to four accumulators, so that some are taken out while another is filled.  The tensor cores cut a sum off, not round it, at
     // every instruction, by 3e-8 of the sum on the average.  So (1) pieces have a second accumulator for all products but p0 p0, which keeps the five
     // small products of each step from cutting at the large sum; (2) after `run` blocks the sum is added to a running one that stays in tensor
     // memory too, behind the accumulators, and so does the small products' then.
     constexpr int kParts = kPieces == 3 ? 2 : 1;
-    const bool runs = p.run < p.kshare;
+    const bool runs = MODE == kAny && p.run < p.kshare;  // (float32 results)
     const int acc_step = runs ? p.bn : kParts * p.bn, sum_at = 2 * p.bn;  // (with runs there are two accumulators)
     const unsigned acc_mask = p.accs - 1, acc_shift = p.accs == 4 ? 2 : 1;
 
@@ -394,6 +409,7 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
         }
         for (int b = 0; b < p.accs; ++b) mbar_init(acc_full + 8 * b, 1), mbar_init(acc_empty + 8 * b, kEpilogue / p.groups);
         mbar_init(last, 1);
+        mbar_init(kept_full, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -405,8 +421,8 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
 
-    const int total = p.tiles * p.splits;
-    const int a_bytes = kBM * 2 * BK, b_bytes = p.bn * 2 * BK, stage_bytes = kPieces * (a_bytes + b_bytes);
+    const int a_bytes = kBM * 2 * BK, b_bytes = p.bn * 2 * BK, stage_bytes = kPieces * (a_bytes + (p.kept ? 0 : b_bytes));
+    const uint32_t stages_at = smem_u32(ring) + p.kept;
 
     if (warp < kEpilogue) {
         // ---- epilogue: the 32 lanes 32 (warp % 4) and up, parts of 64 columns in two tiles of 32.  16 warps are as many as the widest product
@@ -415,7 +431,8 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
         unsigned char *const buffer = staging + warp * 4096;  // a float32 tile, or two bf16 ones: for the part's two, or for the result and z
         float *const bias = bias_rows + warp * 64;
         const uint32_t lanes = tmem + ((uint32_t)(warp % 4 * 32) << 16);
-        const CUtensorMap *const tout = p.store_tma ? &p.tout : nullptr, *const tpre = p.store_tma ? &p.tpre : nullptr;
+        const bool tma = MODE != kAny || p.store_tma, partial = MODE == kAny && p.partial, res_vec = MODE != kAny || p.res_vec;
+        const CUtensorMap *const tout = tma ? &p.tout : nullptr, *const tpre = tma ? &p.tpre : nullptr;
         unsigned u = 0;          // accumulators of the CTA so far
         int bias_at = -1;        // the column that the bias in shared memory starts at
         const auto stores_done = [&] {  // (with the buffer)
@@ -423,8 +440,7 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
             __syncwarp();
         };
         bool ok = true;
-        for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
-            const Share s = share_of(p, w);
+        for (Shares s(p); s.more(p) && ok; s.next(p)) {
             const int row0 = s.m0 + warp % 4 * 32, tiles = row0 < p.M ? (min(p.bn, p.N - s.n0) + 31) / 32 : 0;
             for (int k0 = s.k; k0 < s.end; k0 += p.run, ++u) {
                 if (u % p.groups != group) continue;
@@ -435,9 +451,9 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
                     const int c0 = s.n0 + 32 * h0;
                     uint4 res[kPieces32<TOUT>];
                     const auto bring = [&](int col0) {
-                        tile_load<TOUT>(res, static_cast<const TOUT *>(p.residual), p.ld_res, p.res_vec, row0, col0, p.M, p.N, lane);
+                        tile_load<TOUT>(res, static_cast<const TOUT *>(p.residual), p.ld_res, res_vec, row0, col0, p.M, p.N, lane);
                     };
-                    if (ends && !p.partial) {  // what does not need the sums
+                    if (ends && !partial) {  // what does not need the sums
                         if (p.residual) bring(c0);
                         if (bias_at != c0) {
                             bias_at = c0;
@@ -452,7 +468,7 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
                         tcgen05_fence_after();
                         waited = true;
                     }
-#pragma unroll
+#pragma unroll 1
                     for (int odd = 0; odd < 2; ++odd) {
                         const int h = h0 + odd, col0 = c0 + 32 * odd;
                         if (h >= tiles) break;
@@ -477,9 +493,9 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
                             continue;
                         }
                         if (kParts == 2) add(runs ? sum + p.bn : acc + p.bn);
-                        if (p.partial) {
+                        if (partial) {
                             stores_done();
-                            row_store<float>(v, buffer, lane);
+                            row_store<float>(v, buffer, -1, lane);
                             tile_leave<float>(buffer, &p.tout, nullptr, 0, true, row0, col0, p.M, p.N, s.split, lane);
                             continue;
                         }
@@ -494,19 +510,22 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
                         if (p.pre) {
                             unsigned char *const tile = buffer + (sizeof(TIN) == 2 && sizeof(TOUT) == 2 ? 2048 : 0);
                             if (odd) stores_done();
-                            row_store<TIN>(v, tile, lane);
+                            row_store<TIN>(v, tile, -1, lane);
                             tile_leave<TIN>(tile, tpre, static_cast<TIN *>(p.pre), p.ld_pre, p.pre_vec, row0, col0, p.M, p.N, 0, lane);
                         }
-                        activate_all<std::is_same<TOUT, bf16>::value>(v, p.act);
-                        unsigned char *const tile = buffer + (sizeof(TOUT) == 2 && odd && !p.pre ? 2048 : 0);
+                        activate_all<std::is_same<TOUT, bf16>::value>(v, MODE == kAny ? p.act : MODE);
+                        // (a bf16 result without z: both halves leave at once, in rows of 128 bytes, where no other CTA has the second half's columns)
+                        const int half = p.wide ? odd : -1;
+                        unsigned char *const tile = buffer + (sizeof(TOUT) == 2 && odd && !p.pre && !p.wide ? 2048 : 0);
                         if (p.pre ? sizeof(TIN) == 4 || sizeof(TOUT) == 4 : odd && sizeof(TOUT) == 4) stores_done();
                         if (p.residual) {
-                            tile_stage<TOUT>(res, p.res_vec, tile, lane);
+                            tile_stage<TOUT>(res, res_vec, tile, half, lane);
                             if (!odd && h + 1 < tiles) bring(col0 + 32);
-                            row_add<TOUT>(v, tile, lane);
+                            row_add<TOUT>(v, tile, half, lane);
                         }
-                        row_store<TOUT>(v, tile, lane);
-                        tile_leave<TOUT>(tile, tout, static_cast<TOUT *>(p.out), p.ld_out, p.out_vec, row0, col0, p.M, p.N, 0, lane);
+                        row_store<TOUT>(v, tile, half, lane);
+                        if (!p.wide) tile_leave<TOUT>(tile, tout, static_cast<TOUT *>(p.out), p.ld_out, p.out_vec, row0, col0, p.M, p.N, 0, lane);
+                        else if (odd || h + 1 == tiles) tile_leave<TOUT>(tile, tout, nullptr, 0, true, row0, c0, p.M, p.N, 0, lane);
                     }
                 }
                 if (ok && !waited) ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * a, u >> acc_shift & 1, &failed));
@@ -520,14 +539,13 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
         __syncwarp();
     } else if (warp == kEpilogue) {
         // ---- products, by one thread
-        if (lane == 0) {
+        if (elect_one()) {
             const uint32_t idesc = mma_idesc(p.bn, p.a_mn, p.b_mn);
             const int a_step = p.a_mn ? 2048 >> 4 : 32 >> 4, b_step = p.b_mn ? 2048 >> 4 : 32 >> 4;  // 16 of K further
             int stage = 0, phase = 0;
             unsigned u = 0;  // accumulators filled so far
-            bool ok = true;
-            for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
-                const Share s = share_of(p, w);
+            bool ok = !p.kept || mbar_wait(kept_full, 0, &failed);
+            for (Shares s(p); s.more(p) && ok; s.next(p)) {
                 for (int k0 = s.k; k0 < s.end && ok; k0 += p.run, ++u) {
                     const unsigned acc = u & acc_mask;
                     ok = mbar_wait(acc_empty + 8 * acc, (u >> acc_shift & 1) ^ 1, &failed);
@@ -540,8 +558,8 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
                     for (int k = k0; k < k1; ++k) {
                         if (!(ok = mbar_wait(full + 8 * stage, phase, &failed))) break;
                         tcgen05_fence_after();
-                        const uint32_t at = smem_u32(ring) + stage * stage_bytes;
-                        const uint64_t a = smem_desc(at, p.a_mn, 2 * BK, 128 * BK), b = smem_desc(at + kPieces * a_bytes, p.b_mn, 2 * BK, 128 * BK);
+                        const uint32_t at = stages_at + stage * stage_bytes, b_at = p.kept ? smem_u32(ring) + k * b_bytes : at + kPieces * a_bytes;
+                        const uint64_t a = smem_desc(at, p.a_mn, 2 * BK, 128 * BK), b = smem_desc(b_at, p.b_mn, 2 * BK, 128 * BK);
                         if constexpr (kPieces == 1) {
 #pragma unroll
                             for (int i = 0; i < BK / 16; ++i) mma_bf16(d, a + i * a_step, b + i * b_step, idesc, k > k0 || i > 0);
@@ -568,28 +586,33 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
         __syncwarp();
     } else if (warp == kEpilogue + 1) {
         // ---- loads, by one thread
-        if (lane == 0) {
+        if (elect_one()) {
             int stage = 0, phase = 0;
             bool ok = true;
-            for (int w = blockIdx.x; w < total && ok; w += gridDim.x) {
-                const Share s = share_of(p, w);
+            const auto load_b = [&](uint32_t at, int n0, int k, int piece, uint32_t bar) {  // (an operand whose rows run along M or N: 64 of it at a time)
+                if (!p.b_mn) tma_load_3d(at, &p.tb, k * BK, n0, piece, bar);
+                else
+                    for (int i = 0; i < p.bn / 64; ++i) tma_load_3d(at + 128 * BK * i, &p.tb, n0 + 64 * i, k * BK, piece, bar);
+            };
+            if (p.kept) {  // (the CTAs' number is a multiple of the tiles along N: a CTA's tiles all have the same columns)
+                mbar_expect(kept_full, p.kept);
+                for (int k = 0; k < p.kblocks; ++k) load_b(smem_u32(ring) + k * b_bytes, Shares(p).n0, k, 0, kept_full);
+            }
+            for (Shares s(p); s.more(p) && ok; s.next(p)) {
                 for (int k = s.k; k < s.end; ++k) {
                     if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, &failed))) break;
                     const uint32_t bar = full + 8 * stage;
-                    uint32_t at = smem_u32(ring) + stage * stage_bytes;
+                    uint32_t at = stages_at + stage * stage_bytes;
                     mbar_expect(bar, stage_bytes);
-                    // (an operand whose rows run along M or N: 64 of it at a time)
                     for (int piece = 0; piece < kPieces; ++piece, at += a_bytes)
                         if (!p.a_mn) tma_load_3d(at, &p.ta, k * BK, s.m0, piece, bar);
                         else
                             for (int i = 0; i < kBM / 64; ++i) tma_load_3d(at + 128 * BK * i, &p.ta, s.m0 + 64 * i, k * BK, piece, bar);
-                    for (int piece = 0; piece < kPieces; ++piece, at += b_bytes)
-                        if (!p.b_mn) tma_load_3d(at, &p.tb, k * BK, s.n0, piece, bar);
-                        else
-                            for (int i = 0; i < p.bn / 64; ++i) tma_load_3d(at + 128 * BK * i, &p.tb, s.n0 + 64 * i, k * BK, piece, bar);
+                    for (int piece = 0; piece < kPieces && !p.kept; ++piece, at += b_bytes) load_b(at, s.n0, k, piece, bar);
                     if (++stage == p.stages) stage = 0, phase ^= 1;
                 }
             }
+            if (!ok && p.kept) mbar_drain(kept_full, 0);
             if (!ok)  // the last load into every stage: the ones before `stage` in this round of the ring, the others in the round before
                 for (int i = 0; i < p.stages; ++i) mbar_drain(full + 8 * i, i < stage ? phase : phase ^ 1);
         }
@@ -949,17 +972,17 @@ bool make_map(CUtensorMap &map, const Operand &o, int pieces, int across, int K,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Results: `layers` matrices of M rows, stored in tiles of 32 x 32
-bool make_store_map(CUtensorMap &map, void *p, bool f32, int M, int N, long long ld, int layers)
+// Results: `layers` matrices of M rows, stored in tiles of 32 x 32 (wide: 64 columns of bf16)
+bool make_store_map(CUtensorMap &map, void *p, bool f32, bool wide, int M, int N, long long ld, int layers)
 {
     const EncodeTiled encode = encode_tiled();
     if (!encode) return false;
     const int elem = f32 ? 4 : 2;
     const cuuint64_t size[3] = {(cuuint64_t)N, (cuuint64_t)M, (cuuint64_t)layers};
     const cuuint64_t pitch[2] = {(cuuint64_t)ld * elem, (cuuint64_t)ld * elem * (cuuint64_t)(layers > 1 ? M : 1)};
-    const cuuint32_t box[3] = {32, 32, 1}, step[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {wide ? 64u : 32u, 32, 1}, step[3] = {1, 1, 1};
     return encode(&map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, p, size, pitch, box, step,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, f32 || wide ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -971,7 +994,7 @@ constexpr int kShort = 256;
 
 // Tiles and shares of a product.
 struct Plan {
-    int ew, bn, stages, tiles_m, tiles_n, kblocks, kshare, splits, run, columns, accs, groups;
+    int ew, bn, stages, grid, kept, tiles_m, tiles_n, kblocks, kshare, splits, run, columns, accs, groups;
     long long ld_partial;
     size_t partial_bytes;  // 0: every tile's sum belongs to one CTA
 };
@@ -1002,8 +1025,15 @@ Plan plan_product(bool b_mn, bool f32, bool out_f32, int M, int N, int K, bool m
         if (t > 64) break;  // (wide results: the widest tiles)
     }
     q.tiles_n = (N + q.bn - 1) / q.bn;
-    q.ew = f32 || q.kshare * bk > kShort ? 8 : 16;
-    q.stages = std::min(8, ring_bytes(q.ew) / (pieces * (kBM + q.bn) * 2 * bk));
+    // B stays in shared memory where all of K fits beside three stages of A and a CTA has several tiles: its loads are two thirds of a 128 x 256
+    // tile's.
+    const long long tiles = (long long)q.tiles_m * q.tiles_n;
+    const int b_bytes = q.kblocks * q.bn * 2 * bk, a_bytes = pieces * kBM * 2 * bk, spread = sms / q.tiles_n * q.tiles_n;
+    q.grid = (int)std::min<long long>(tiles * q.splits, sms);
+    if (!f32 && q.splits == 1 && b_bytes + 3 * a_bytes <= ring_bytes(8) && tiles > spread && spread > 0 && spread * 20 >= sms * 19)
+        q.kept = b_bytes, q.grid = spread;
+    q.ew = f32 || q.kept || q.kshare * bk > kShort ? 8 : 16;
+    q.stages = std::min(8, (ring_bytes(q.ew) - q.kept) / (a_bytes + (q.kept ? 0 : pieces * q.bn * 2 * bk)));
     q.run = runs && q.kshare > kRun / bk ? kRun / bk : q.kshare;
     // Accumulators: with runs two, the running sum and, of float32 operands, that of the small products; else four where they fit (float32
     // operands: pairs).  Groups of epilogue warps: as many 64-column parts as the tile has in each, and no more of them than accumulators.
@@ -1035,16 +1065,26 @@ bool vec_ok(const void *p, long long ld, bool f32)
     return ((uintptr_t)p | (uintptr_t)(ld * (f32 ? 4 : 2))) % 16 == 0 && ld < (1LL << 37);
 }
 
-template <int PIECES, typename TOUT, int EW>
-cudaError_t launch_gemm(const GemmParams &g, cudaStream_t stream)
+template <int PIECES, typename TOUT, int EW, int MODE>
+cudaError_t launch_gemm(const GemmParams &g, int grid, cudaStream_t stream)
 {
-    const auto kernel = gemm_kernel<PIECES, TOUT, EW>;
+    const auto kernel = gemm_kernel<PIECES, TOUT, EW, MODE>;
     constexpr int smem = ring_bytes(EW) + epilogue_bytes(EW) + kControlBytes;
     static_assert(smem <= kSmemLimit && ring_bytes(8) >= 4 * 48 * 1024 && ring_bytes(16) >= 3 * 48 * 1024, "");
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    const int grid = std::min(g.tiles * g.splits, sm_count());
     return launch_dependent(kernel, dim3((unsigned)grid), dim3((unsigned)gemm_threads(EW)), smem, stream, g);
+}
+
+template <int EW>
+cudaError_t launch_bf16(const GemmParams &g, int grid, cudaStream_t stream)
+{
+    switch (g.act) {
+    case FLASHBEV_ACT_RELU: return launch_gemm<1, bf16, EW, FLASHBEV_ACT_RELU>(g, grid, stream);
+    case FLASHBEV_ACT_GELU: return launch_gemm<1, bf16, EW, FLASHBEV_ACT_GELU>(g, grid, stream);
+    case FLASHBEV_ACT_SILU: return launch_gemm<1, bf16, EW, FLASHBEV_ACT_SILU>(g, grid, stream);
+    default: return launch_gemm<1, bf16, EW, FLASHBEV_ACT_NONE>(g, grid, stream);
+    }
 }
 
 // Lays one or two operands out in the scratch
@@ -1081,7 +1121,7 @@ flashbev_status run_product(const Plan &q, const Operand &a, const Operand &b, b
     if (!make_map(g.ta, a, pieces, M, K, kBM) || !make_map(g.tb, b, pieces, N, K, q.bn)) return FLASHBEV_CUDA_ERROR;
     g.a_mn = a.mn, g.b_mn = b.mn;
     g.M = M, g.N = N, g.K = K, g.bn = q.bn, g.stages = q.stages;
-    g.run = q.run, g.columns = q.columns, g.accs = q.accs, g.groups = q.groups;
+    g.run = q.run, g.columns = q.columns, g.accs = q.accs, g.groups = q.groups, g.kept = q.kept;
     g.tiles_n = q.tiles_n, g.tiles = q.tiles_m * q.tiles_n, g.kblocks = q.kblocks, g.kshare = q.kshare, g.splits = q.splits;
     g.out = e.out, g.pre = e.pre, g.residual = e.residual, g.bias = e.bias, g.act = e.act;
     g.ld_out = e.ld_out, g.ld_pre = e.ld_pre, g.ld_res = e.ld_res;
@@ -1090,16 +1130,21 @@ flashbev_status run_product(const Plan &q, const Operand &a, const Operand &b, b
     if (q.splits > 1) {
         g.partial = partial, g.ld_partial = q.ld_partial;
         // (partial sums have no other results)
-        if (!make_store_map(g.tout, partial, true, M, N, q.ld_partial, q.splits)) return FLASHBEV_CUDA_ERROR;
+        if (!make_store_map(g.tout, partial, true, false, M, N, q.ld_partial, q.splits)) return FLASHBEV_CUDA_ERROR;
     } else if (g.out_vec && (!e.pre || g.pre_vec)) {
         g.store_tma = 1;
-        if (!make_store_map(g.tout, e.out, e.out_f32, M, N, e.ld_out, 1)) return FLASHBEV_CUDA_ERROR;
-        if (e.pre && !make_store_map(g.tpre, e.pre, f32, M, N, e.ld_pre, 1)) return FLASHBEV_CUDA_ERROR;
+        g.wide = !e.out_f32 && !e.pre && (q.bn % 64 == 0 || q.tiles_n == 1);
+        if (!make_store_map(g.tout, e.out, e.out_f32, g.wide, M, N, e.ld_out, 1)) return FLASHBEV_CUDA_ERROR;
+        if (e.pre && !make_store_map(g.tpre, e.pre, f32, false, M, N, e.ld_pre, 1)) return FLASHBEV_CUDA_ERROR;
     }
     cudaError_t err;
-    if (f32) err = e.out_f32 ? launch_gemm<3, float, 8>(g, stream) : launch_gemm<3, bf16, 8>(g, stream);
-    else if (q.ew == 8) err = e.out_f32 ? launch_gemm<1, float, 8>(g, stream) : launch_gemm<1, bf16, 8>(g, stream);
-    else err = e.out_f32 ? launch_gemm<1, float, 16>(g, stream) : launch_gemm<1, bf16, 16>(g, stream);
+    // (partial sums are float32)
+    const bool out_f32 = e.out_f32 || g.partial;
+    if (f32) err = out_f32 ? launch_gemm<3, float, 8, kAny>(g, q.grid, stream) : launch_gemm<3, bf16, 8, kAny>(g, q.grid, stream);
+    else if (out_f32) err = q.ew == 8 ? launch_gemm<1, float, 8, kAny>(g, q.grid, stream) : launch_gemm<1, float, 16, kAny>(g, q.grid, stream);
+    else if (!g.store_tma || (e.residual && !g.res_vec))
+        err = q.ew == 8 ? launch_gemm<1, bf16, 8, kAny>(g, q.grid, stream) : launch_gemm<1, bf16, 16, kAny>(g, q.grid, stream);
+    else err = q.ew == 8 ? launch_bf16<8>(g, q.grid, stream) : launch_bf16<16>(g, q.grid, stream);
     ++launches;
     if (err == cudaSuccess && q.splits > 1) {
         if (f32) err = e.out_f32 ? launch_join<float, float>(q, partial, M, N, e, stream) : launch_join<float, bf16>(q, partial, M, N, e, stream);
