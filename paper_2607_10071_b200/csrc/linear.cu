@@ -204,7 +204,7 @@ struct alignas(64) GemmParams {
     void *out, *pre;            // pre: z, or NULL
     const void *residual, *bias;
     long long ld_out, ld_pre, ld_res;
-    int out_vec, pre_vec, res_vec;  // 16-byte accesses are allowed
+    int out_vec, pre_vec, res_vec;  // bytes that every row's start is a multiple of: 16, 4 or 2
     int act;
     float *partial;             // instead of the epilogue: [splits][M][ld_partial] sums
     long long ld_partial;
@@ -291,12 +291,23 @@ __device__ __forceinline__ void row_add(float (&v)[32], const unsigned char *til
     }
 }
 
-// A tile from a matrix to registers, and from there to shared memory.  Rows of any alignment (`vec` false): a lane has a column, so that the warp
-// touches every sector of a row once; 16 rows in a register per 8 of them with 16-byte pieces.
+// A tile from a matrix to registers, and from there to shared memory.  vec: bytes that every row's start is a multiple of.  16: pieces.  Less: a lane has
+// a column, or of bf16 rows on 4-byte boundaries two, so that the warp touches every sector of a row once.
 template <typename T>
-__device__ __forceinline__ void tile_load(uint4 (&r)[kPieces32<T>], const T *base, long long ld, bool vec, int row0, int col0, int M, int N, int lane)
+__device__ __forceinline__ void tile_load(uint4 (&r)[kPieces32<T>], const T *base, long long ld, int vec, int row0, int col0, int M, int N, int lane)
 {
-    if (vec) {
+    if (sizeof(T) == 2 && vec == 4) {
+        const T *p = base + (row0 + lane / 16) * ld + col0 + lane % 16 * 2;
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i, p += 2 * ld) {
+            const int have = row0 + 2 * i + lane / 16 < M ? N - (col0 + lane % 16 * 2) : 0;
+            w[i] = have >= 2 ? *reinterpret_cast<const uint32_t *>(p) : (have == 1 ? *reinterpret_cast<const unsigned short *>(p) : 0);
+        }
+        memcpy(r, w, sizeof(w));
+        return;
+    }
+    if (vec == 16) {
         const int row = row0 + lane / kPieces32<T>, col = col0 + lane % kPieces32<T> * kPiece<T>;
         const T *p = base + row * ld + col;
 #pragma unroll
@@ -312,9 +323,15 @@ __device__ __forceinline__ void tile_load(uint4 (&r)[kPieces32<T>], const T *bas
 }
 
 template <typename T>
-__device__ __forceinline__ void tile_stage(const uint4 (&r)[kPieces32<T>], bool vec, unsigned char *tile, int half, int lane)
+__device__ __forceinline__ void tile_stage(const uint4 (&r)[kPieces32<T>], int vec, unsigned char *tile, int half, int lane)
 {
-    if (vec) {
+    if (sizeof(T) == 2 && vec == 4) {
+        uint32_t w[16];
+        memcpy(w, r, sizeof(w));
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            reinterpret_cast<uint32_t *>(tile + piece_at<T>(2 * i + lane / 16, lane % 16 / 4, half))[lane % 4] = w[i];
+    } else if (vec == 16) {
 #pragma unroll
         for (int i = 0; i < kPieces32<T>; ++i)
             *reinterpret_cast<uint4 *>(tile + piece_at<T>(kRows32<T> * i + lane / kPieces32<T>, lane % kPieces32<T>, half)) = r[i];
@@ -329,7 +346,7 @@ __device__ __forceinline__ void tile_stage(const uint4 (&r)[kPieces32<T>], bool 
 
 // A tile leaves: by one TMA store, which goes on while the warp does, or by ordinary ones.
 template <typename T>
-__device__ __forceinline__ void tile_leave(const unsigned char *tile, const CUtensorMap *map, T *base, long long ld, bool vec, int row0, int col0, int M,
+__device__ __forceinline__ void tile_leave(const unsigned char *tile, const CUtensorMap *map, T *base, long long ld, int vec, int row0, int col0, int M,
                                            int N, int layer, int lane)
 {
     if (map) {
@@ -339,7 +356,16 @@ __device__ __forceinline__ void tile_leave(const unsigned char *tile, const CUte
         return;
     }
     __syncwarp();
-    if (vec) {
+    if (sizeof(T) == 2 && vec == 4) {
+        T *p = base + (row0 + lane / 16) * ld + col0 + lane % 16 * 2;
+        const int have = N - (col0 + lane % 16 * 2), rows = M - row0 - lane / 16;
+#pragma unroll 8
+        for (int i = 0; i < 16; ++i, p += 2 * ld) {
+            const uint32_t w = reinterpret_cast<const uint32_t *>(tile + piece_at<T>(2 * i + lane / 16, lane % 16 / 4, -1))[lane % 4];
+            if (2 * i < rows && have >= 2) *reinterpret_cast<uint32_t *>(p) = w;
+            else if (2 * i < rows && have == 1) *reinterpret_cast<unsigned short *>(p) = (unsigned short)w;
+        }
+    } else if (vec == 16) {
         const int row = row0 + lane / kPieces32<T>, col = col0 + lane % kPieces32<T> * kPiece<T>;
         T *p = base + row * ld + col;
 #pragma unroll
@@ -434,7 +460,8 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
         unsigned char *const buffer = staging + warp * 4096;  // a float32 tile, or two bf16 ones: for the part's two, or for the result and z
         float *const bias = bias_rows + warp * 64;
         const uint32_t lanes = tmem + ((uint32_t)(warp % 4 * 32) << 16);
-        const bool tma = MODE != kAny || p.store_tma, partial = MODE == kAny && p.partial, res_vec = MODE != kAny || p.res_vec;
+        const bool tma = MODE != kAny || p.store_tma, partial = MODE == kAny && p.partial;
+        const int res_vec = MODE != kAny ? 16 : p.res_vec;
         const CUtensorMap *const tout = tma ? &p.tout : nullptr, *const tpre = tma ? &p.tpre : nullptr;
         unsigned u = 0;          // accumulators of the CTA so far
         int bias_at = -1;        // the column that the bias in shared memory starts at
@@ -499,7 +526,7 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
                         if (partial) {
                             stores_done();
                             row_store<float>(v, buffer, -1, lane);
-                            tile_leave<float>(buffer, &p.tout, nullptr, 0, true, row0, col0, p.M, p.N, s.split, lane);
+                            tile_leave<float>(buffer, &p.tout, nullptr, 0, 16, row0, col0, p.M, p.N, s.split, lane);
                             continue;
                         }
 #pragma unroll
@@ -528,7 +555,7 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
                         }
                         row_store<TOUT>(v, tile, half, lane);
                         if (!p.wide) tile_leave<TOUT>(tile, tout, static_cast<TOUT *>(p.out), p.ld_out, p.out_vec, row0, col0, p.M, p.N, 0, lane);
-                        else if (odd || h + 1 == tiles) tile_leave<TOUT>(tile, tout, nullptr, 0, true, row0, c0, p.M, p.N, 0, lane);
+                        else if (odd || h + 1 == tiles) tile_leave<TOUT>(tile, tout, nullptr, 0, 16, row0, c0, p.M, p.N, 0, lane);
                     }
                 }
                 if (ok && !waited) ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * a, u >> acc_shift & 1, &failed));
@@ -632,28 +659,41 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
 
 // ---- sums that several CTAs shared ----------------------------------------------------------------------------------------
 
-// Adds the shares up in their order and does what the epilogue would have done.  Four columns of a row per thread.
+// Adds the shares up in a fixed order and does what the epilogue would have done.  Four columns of a row per thread; with few of them (`groups` > 1)
+// as many threads take every so manieth share, and the first of them joins their sums.
 template <typename TIN, typename TOUT>
-__global__ void __launch_bounds__(256) join_kernel(const float *__restrict__ partial, long long ld_partial, int splits, int M, int N,
+__global__ void __launch_bounds__(256) join_kernel(const float *__restrict__ partial, long long ld_partial, int splits, int groups, int M, int N,
                                                    const TIN *__restrict__ bias, const TOUT *residual, long long ld_res, TOUT *out, long long ld_out,
                                                    TIN *pre, long long ld_pre, int act)
 {
     constexpr bool kFast = std::is_same<TOUT, bf16>::value;
+    __shared__ float4 joined[256];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
-    const int quads = (int)(ld_partial / 4);
-    const long long all = (long long)M * quads;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
-        const long long row = i / quads;
+    const int quads = (int)(ld_partial / 4), width = 256 / groups, group = threadIdx.x / width, t = threadIdx.x % width;
+    const long long all = (long long)M * quads, step = (long long)M * ld_partial / 4;
+    for (long long i0 = (long long)blockIdx.x * width; i0 < all; i0 += (long long)gridDim.x * width) {
+        const long long i = i0 + t, row = i / quads;
         const int col = (int)(i - row * quads) * 4;
-        const float4 *src = reinterpret_cast<const float4 *>(partial + row * ld_partial + col);
-        const long long step = (long long)M * ld_partial / 4;
+        const float4 *src = reinterpret_cast<const float4 *>(partial) + row * (ld_partial / 4) + col / 4;
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (i < all)
 #pragma unroll 8
-        for (int s = 0; s < splits; ++s) {
-            const float4 q = __ldcs(src + s * step);
-            v[0] += q.x, v[1] += q.y, v[2] += q.z, v[3] += q.w;
+            for (int s = group; s < splits; s += groups) {
+                const float4 q = __ldcs(src + s * step);
+                v[0] += q.x, v[1] += q.y, v[2] += q.z, v[3] += q.w;
+            }
+        if (groups > 1) {
+            joined[threadIdx.x] = make_float4(v[0], v[1], v[2], v[3]);
+            __syncthreads();
+            if (group == 0)
+                for (int g = 1; g < groups; ++g) {
+                    const float4 q = joined[g * width + t];
+                    v[0] += q.x, v[1] += q.y, v[2] += q.z, v[3] += q.w;
+                }
+            __syncthreads();
         }
+        if (group || i >= all) continue;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (col + j >= N) break;
@@ -715,10 +755,12 @@ __global__ void __launch_bounds__(256) layout_kernel(const LayoutJob first, cons
     const bool is_first = blockIdx.x < first_blocks;
     const LayoutJob &q = is_first ? first : second;
     const unsigned block = is_first ? blockIdx.x : blockIdx.x - first_blocks, blocks = is_first ? first_blocks : gridDim.x - first_blocks;
-    const unsigned long long all = (unsigned long long)q.rows * q.lanes;
-    for (unsigned long long i = block * 256ull + threadIdx.x; i < all; i += blocks * 256ull) {
-        const unsigned long long row = i / q.lanes;
-        const int lane = (int)(i - row * q.lanes);
+    // (place in the row and row, a grid's step on: no division for every piece)
+    const unsigned start = block * 256 + threadIdx.x, step = blocks * 256;
+    unsigned row = start / q.lanes, lane = start - row * q.lanes;
+    const unsigned step_rows = step / q.lanes, step_lanes = step - step_rows * q.lanes;
+#pragma unroll 4
+    for (; row < (unsigned)q.rows; row += step_rows, lane += step_lanes, row += lane >= q.lanes, lane -= lane >= q.lanes ? q.lanes : 0) {
         const T *src = static_cast<const T *>(q.from) + row * q.ld;
         bf16 *dst = q.to + row * q.ld_to;
         if (q.vec) {
@@ -732,8 +774,8 @@ __global__ void __launch_bounds__(256) layout_kernel(const LayoutJob first, cons
                 *reinterpret_cast<uint4 *>(dst) = __ldcs(reinterpret_cast<const uint4 *>(src));
             }
         } else {
-            const int col = 2 * lane;
-            const T a = src[col], b = col + 1 < q.width ? src[col + 1] : from_float<T>(0.0f);
+            const int col = 2 * (int)lane;
+            const T a = __ldg(src + col), b = col + 1 < q.width ? __ldg(src + col + 1) : from_float<T>(0.0f);
             if constexpr (kP == 3) {
                 uint32_t p[3];
                 split(make_float2(a, b), p);
@@ -1068,6 +1110,12 @@ bool vec_ok(const void *p, long long ld, bool f32)
     return ((uintptr_t)p | (uintptr_t)(ld * (f32 ? 4 : 2))) % 16 == 0 && ld < (1LL << 37);
 }
 
+int row_bytes(const void *p, long long ld, bool f32)
+{
+    if (vec_ok(p, ld, f32)) return 16;
+    return ((uintptr_t)p | (uintptr_t)(ld * (f32 ? 4 : 2))) % 4 == 0 ? 4 : 2;
+}
+
 template <int PIECES, typename TOUT, int EW, int MODE>
 cudaError_t launch_gemm(const GemmParams &g, int grid, cudaStream_t stream)
 {
@@ -1109,8 +1157,10 @@ template <typename TIN, typename TOUT>
 cudaError_t launch_join(const Plan &q, const float *partial, int M, int N, const Epilogue &e, cudaStream_t stream)
 {
     const long long quads = (long long)M * (q.ld_partial / 4);
-    const unsigned blocks = (unsigned)std::min<long long>((quads + 255) / 256, 8LL * sm_count());
-    return launch_dependent(join_kernel<TIN, TOUT>, dim3(blocks), dim3(256), 0, stream, partial, q.ld_partial, q.splits, M, N,
+    int groups = 1;
+    while (groups < 16 && groups * 2 <= q.splits && quads * groups < 1024LL * sm_count()) groups *= 2;
+    const unsigned blocks = (unsigned)std::min<long long>((quads * groups + 255) / 256, 8LL * sm_count());
+    return launch_dependent(join_kernel<TIN, TOUT>, dim3(blocks), dim3(256), 0, stream, partial, q.ld_partial, q.splits, groups, M, N,
                             static_cast<const TIN *>(e.bias), static_cast<const TOUT *>(e.residual), e.ld_res, static_cast<TOUT *>(e.out), e.ld_out,
                             static_cast<TIN *>(e.pre), e.ld_pre, e.act);
 }
@@ -1128,13 +1178,13 @@ flashbev_status run_product(const Plan &q, const Operand &a, const Operand &b, b
     g.tiles_n = q.tiles_n, g.tiles = q.tiles_m * q.tiles_n, g.kblocks = q.kblocks, g.kshare = q.kshare, g.splits = q.splits;
     g.out = e.out, g.pre = e.pre, g.residual = e.residual, g.bias = e.bias, g.act = e.act;
     g.ld_out = e.ld_out, g.ld_pre = e.ld_pre, g.ld_res = e.ld_res;
-    g.out_vec = vec_ok(e.out, e.ld_out, e.out_f32), g.pre_vec = vec_ok(e.pre, e.ld_pre, f32), g.res_vec = vec_ok(e.residual, e.ld_res, e.out_f32);
+    g.out_vec = row_bytes(e.out, e.ld_out, e.out_f32), g.pre_vec = row_bytes(e.pre, e.ld_pre, f32), g.res_vec = row_bytes(e.residual, e.ld_res, e.out_f32);
     g.error_word = error_word;
     if (q.splits > 1) {
         g.partial = partial, g.ld_partial = q.ld_partial;
         // (partial sums have no other results)
         if (!make_store_map(g.tout, partial, true, false, M, N, q.ld_partial, q.splits)) return FLASHBEV_CUDA_ERROR;
-    } else if (g.out_vec && (!e.pre || g.pre_vec)) {
+    } else if (g.out_vec == 16 && (!e.pre || g.pre_vec == 16)) {
         g.store_tma = 1;
         g.wide = !e.out_f32 && !e.pre && (q.bn % 64 == 0 || q.tiles_n == 1);
         if (!make_store_map(g.tout, e.out, e.out_f32, g.wide, M, N, e.ld_out, 1)) return FLASHBEV_CUDA_ERROR;
@@ -1145,7 +1195,7 @@ flashbev_status run_product(const Plan &q, const Operand &a, const Operand &b, b
     const bool out_f32 = e.out_f32 || g.partial;
     if (f32) err = out_f32 ? launch_gemm<3, float, 8, kAny>(g, q.grid, stream) : launch_gemm<3, bf16, 8, kAny>(g, q.grid, stream);
     else if (out_f32) err = q.ew == 8 ? launch_gemm<1, float, 8, kAny>(g, q.grid, stream) : launch_gemm<1, float, 16, kAny>(g, q.grid, stream);
-    else if (!g.store_tma || (e.residual && !g.res_vec))
+    else if (!g.store_tma || (e.residual && g.res_vec != 16))
         err = q.ew == 8 ? launch_gemm<1, bf16, 8, kAny>(g, q.grid, stream) : launch_gemm<1, bf16, 16, kAny>(g, q.grid, stream);
     else err = q.ew == 8 ? launch_bf16<8>(g, q.grid, stream) : launch_bf16<16>(g, q.grid, stream);
     ++launches;
