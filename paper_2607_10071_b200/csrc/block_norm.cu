@@ -589,7 +589,7 @@ flashbev_status check_common(const Q *p, std::initializer_list<int64_t> strides)
     if (!isfinite(p->scale) || !isfinite(p->eps) || p->eps < 0.0) return FLASHBEV_INVALID_ARG;
     for (long long ld : strides)
         if (ld != 0 && ld < p->C) return FLASHBEV_INVALID_ARG;
-    if (p->gate && (p->gate_groups <= 0 || p->rows % p->gate_groups || !p->y)) return FLASHBEV_INVALID_ARG;
+    if (p->gate && (p->gate_groups <= 0 || p->rows % p->gate_groups || (!p->y && p->rows))) return FLASHBEV_INVALID_ARG;
     if (!p->y && p->after != FLASHBEV_NORM_NONE && p->rows) return FLASHBEV_INVALID_ARG;
     if (p->after == FLASHBEV_NORM_NONE && (p->after_weight || p->after_bias)) return FLASHBEV_INVALID_ARG;
     if (p->before == FLASHBEV_NORM_NONE && p->before_weight) return FLASHBEV_INVALID_ARG;

@@ -1044,7 +1044,7 @@ struct Plan {
     size_t partial_bytes;  // 0: every tile's sum belongs to one CTA
 };
 
-Plan plan_product(bool b_mn, bool f32, bool out_f32, int act, int M, int N, int K, bool may_split)
+Plan plan_product(bool b_mn, bool f32, bool out_f32, bool heavy, int M, int N, int K, bool may_split)
 {
     Plan q = {};
     const int sms = sm_count(), pieces = f32 ? 3 : 1;
@@ -1075,7 +1075,7 @@ Plan plan_product(bool b_mn, bool f32, bool out_f32, int act, int M, int N, int 
     const long long tiles = (long long)q.tiles_m * q.tiles_n;
     const int b_bytes = q.kblocks * q.bn * 2 * bk, a_bytes = pieces * kBM * 2 * bk, spread = sms / q.tiles_n * q.tiles_n;
     q.grid = (int)std::min<long long>(tiles * q.splits, sms);
-    if (!f32 && act < FLASHBEV_ACT_GELU && q.splits == 1 && b_bytes + 3 * a_bytes <= ring_bytes(8) && tiles > spread && spread > 0 && spread * 20 >= sms * 19)
+    if (!f32 && !heavy && q.splits == 1 && b_bytes + 3 * a_bytes <= ring_bytes(8) && tiles > spread && spread > 0 && spread * 20 >= sms * 19)
         q.kept = b_bytes, q.grid = spread;
     q.ew = f32 || q.kept || q.kshare * bk > kShort ? 8 : 16;
     q.stages = std::min(8, (ring_bytes(q.ew) - q.kept) / (a_bytes + (q.kept ? 0 : pieces * q.bn * 2 * bk)));
@@ -1261,6 +1261,10 @@ struct ForwardPlan {
     size_t x_at, w_at, partial_at, needed, total;  // needed: without partial sums
 };
 
+// An epilogue that 16 warps are worth more for than weights that stay in shared memory: special functions, a residual to wait for
+// (184950 x 256 x 256, GELU 52 us with eight, 40 with 16; with a residual 59 and 49)
+bool heavy_epilogue(const flashbev_linear_params *p) { return p->act >= FLASHBEV_ACT_GELU || p->residual; }
+
 ForwardPlan plan_forward(const flashbev_linear_params *p)
 {
     ForwardPlan q = {};
@@ -1271,7 +1275,7 @@ ForwardPlan plan_forward(const flashbev_linear_params *p)
     if (q.lay_x) q.x_at = at, at += laid_out_bytes(M, K, f32);
     if (q.lay_w) q.w_at = at, at += laid_out_bytes(N, K, f32);
     q.needed = q.partial_at = at;
-    q.product = plan_product(false, f32, p->out_dtype == FLASHBEV_F32, p->act, M, N, K, true);
+    q.product = plan_product(false, f32, p->out_dtype == FLASHBEV_F32, heavy_epilogue(p), M, N, K, true);
     q.total = at + round_up(q.product.partial_bytes);
     return q;
 }
@@ -1331,8 +1335,8 @@ BackwardPlan plan_backward(const flashbev_linear_backward_params *p)
         if (q.chunks > 65535) q.per = (M + 65534) / 65535, q.chunks = (M + q.per - 1) / q.per;
         if (q.need_b) q.sums_at = at, at += round_up((size_t)q.chunks * N * sizeof(float));
     }
-    if (q.need_x) q.gx = plan_product(true, f32, f32, FLASHBEV_ACT_NONE, M, K, N, true);
-    if (q.need_w) q.gw = plan_product(true, f32, f32, FLASHBEV_ACT_NONE, N, K, M, true);
+    if (q.need_x) q.gx = plan_product(true, f32, f32, false, M, K, N, true);
+    if (q.need_w) q.gw = plan_product(true, f32, f32, false, N, K, M, true);
     q.partial_at = at;  // (the products run one after the other)
     q.total = at + round_up(std::max(q.gx.partial_bytes, q.gw.partial_bytes));
     return q;
@@ -1388,7 +1392,7 @@ flashbev_status flashbev_linear(const flashbev_linear_params *p, void *stream_)
             ForwardPlan q = plan_forward(p);
             const size_t have = p->workspace ? p->workspace_bytes : 0;
             if (have < q.needed) return FLASHBEV_TOO_SMALL;
-            if (have < q.total) q.product = plan_product(false, f32, e.out_f32, p->act, M, N, K, false);
+            if (have < q.total) q.product = plan_product(false, f32, e.out_f32, heavy_epilogue(p), M, N, K, false);
             char *const ws = static_cast<char *>(p->workspace);
             Operand x = {p->x, ld_x, false}, w = {p->weight, ld_w, false};
             LayoutJob jobs[2] = {};
