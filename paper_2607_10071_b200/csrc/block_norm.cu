@@ -703,8 +703,8 @@ BackwardShape backward_shape(const flashbev_block_norm_backward_params *p)
     s.gates = p->gate ? p->gate_groups : 1;
     const long long per = p->rows / s.gates;
     const long long resident = s.threads > 512 ? sm_count() : 2LL * sm_count();
-    // Few rows per gate, or more gates than teams: a team sums a gate's rows by itself.
-    s.direct = p->gate && (per <= 4 || s.gates >= resident * s.teams);
+    // More gates than teams, or a good many with few rows each: a team sums a gate's rows by itself.
+    s.direct = p->gate && (s.gates >= resident * s.teams || (per <= 4 && s.gates >= resident));
     const void *const outs[5] = {p->grad_after_weight, p->grad_after_bias, p->grad_before_weight, p->grad_before_bias, p->grad_gate};
     for (int i = 0; i < 5; ++i)
         if (outs[i] && !(i == 4 && s.direct)) s.want |= 1 << i, ++s.arrays;

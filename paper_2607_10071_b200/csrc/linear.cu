@@ -404,7 +404,7 @@ struct Shares {
     }
 };
 
-// MODE: an activation, for bf16 results that leave by TMA, or kAny: everything as the parameters say.  What an instance does not need would be in its
+// MODE: an activation, for results of unshared sums that leave by TMA, or kAny: everything as the parameters say.  What an instance does not need would be in its
 // way: the code of the other activations and of rows of any alignment, skipped, cost 8 of 37 us (184950 x 64 x 256) in instruction fetches.
 constexpr int kAny = 4;
 
@@ -897,46 +897,49 @@ __global__ void __launch_bounds__(1024) column_sum_kernel(const float *__restric
 // ---- few rows ---------------------------------------------------------------------------------------------------------------
 
 // Up to R rows of x: bound by reading the weights once, so no tensor cores (their tiles would be empty rows).  A warp forms NC
-// neighbouring columns of all rows, its lanes 8 elements of the sum each at a time.
+// neighbouring columns of all rows, its lanes 8 elements of the sum each at a time.  Where that leaves most SMs without a warp, the block's
+// eight warps share the sum of the same columns (`shared`).  VEC: bytes that every row's start is a multiple of, 16 or an element.
 template <typename TIN, typename TOUT, int R, int NC, bool VEC>
 __global__ void __launch_bounds__(256) rows_kernel(const TIN *__restrict__ x, long long ld_x, const TIN *__restrict__ weight, long long ld_w, int M,
-                                                   int N, int K, const TIN *__restrict__ bias, const TOUT *residual, long long ld_res, TOUT *out,
-                                                   long long ld_out, TIN *pre, long long ld_pre, int act)
+                                                   int N, int K, int shared, const TIN *__restrict__ bias, const TOUT *residual, long long ld_res,
+                                                   TOUT *out, long long ld_out, TIN *pre, long long ld_pre, int act)
 {
     constexpr bool kFast = std::is_same<TOUT, bf16>::value;
     constexpr int Q = 8 * (int)sizeof(TIN) / 16;
+    __shared__ float joined[8][R * NC];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
-    const int lane = threadIdx.x % 32, n0 = (blockIdx.x * 8 + threadIdx.x / 32) * NC;
-    if (n0 >= N) return;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, n0 = (shared ? blockIdx.x : blockIdx.x * 8 + warp) * NC;
+    if (n0 >= N) return;  // (all of the block where it shares)
     float acc[R][NC];
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int c = 0; c < NC; ++c) acc[r][c] = 0.0f;
-    const auto bring = [&](float (&v)[8], const TIN *p, int have) {
-        if (VEC && have >= 8) {
+    // VEC: the lane's eight elements are neighbours, else every 32nd of the warp's 256, so that its loads are too
+    const auto bring = [&](float (&v)[8], const TIN *row, int k) {
+        if constexpr (VEC) {
             uint4 q[Q];
             TIN t[8];
 #pragma unroll
-            for (int i = 0; i < Q; ++i) q[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+            for (int i = 0; i < Q; ++i) q[i] = k + lane * 8 < K ? __ldg(reinterpret_cast<const uint4 *>(row + k + lane * 8) + i) : make_uint4(0, 0, 0, 0);
             memcpy(t, q, sizeof(t));
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = to_float(t[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = i < have ? to_float(p[i]) : 0.0f;
+            for (int i = 0; i < 8; ++i) v[i] = k + lane + 32 * i < K ? to_float(__ldg(row + k + lane + 32 * i)) : 0.0f;
         }
     };
 #pragma unroll 2
-    for (int k = lane * 8; k < K; k += 256) {
+    for (int k = shared ? warp * 256 : 0; k < K; k += shared ? 2048 : 256) {
         float wv[NC][8];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) bring(wv[c], weight + min(n0 + c, N - 1) * ld_w + k, K - k);
+        for (int c = 0; c < NC; ++c) bring(wv[c], weight + min(n0 + c, N - 1) * ld_w, k);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             float xv[8];
-            bring(xv, x + min(r, M - 1) * ld_x + k, K - k);
+            bring(xv, x + min(r, M - 1) * ld_x, k);
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -949,12 +952,24 @@ __global__ void __launch_bounds__(256) rows_kernel(const TIN *__restrict__ x, lo
         for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int d = 16; d; d /= 2) acc[r][c] += __shfl_xor_sync(0xffffffffu, acc[r][c], d);
+    if (shared) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                if (lane == r * NC + c) joined[warp][lane] = acc[r][c];
+        __syncthreads();
+        if (warp) return;
+    }
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             if (lane != r * NC + c || r >= M || n0 + c >= N) continue;
-            float z[2] = {acc[r][c] + (bias ? to_float(bias[n0 + c]) : 0.0f), 0.0f};
+            float z[2] = {acc[r][c], 0.0f};
+            if (shared)
+                for (int w = 1; w < 8; ++w) z[0] += joined[w][lane];
+            if (bias) z[0] += to_float(bias[n0 + c]);
             if (pre) pre[r * ld_pre + n0 + c] = from_float<TIN>(z[0]);
             activate_all<kFast>(z, act);
             if (residual) z[0] += to_float(residual[r * ld_res + n0 + c]);
@@ -1127,14 +1142,15 @@ cudaError_t launch_gemm(const GemmParams &g, int grid, cudaStream_t stream)
     return launch_dependent(kernel, dim3((unsigned)grid), dim3((unsigned)gemm_threads(EW)), smem, stream, g);
 }
 
-template <int EW>
-cudaError_t launch_bf16(const GemmParams &g, int grid, cudaStream_t stream)
+template <int PIECES, typename TOUT, int EW>
+cudaError_t launch_mode(const GemmParams &g, int grid, cudaStream_t stream)
 {
+    if (g.partial || g.run < g.kshare || !g.store_tma || (g.residual && g.res_vec != 16)) return launch_gemm<PIECES, TOUT, EW, kAny>(g, grid, stream);
     switch (g.act) {
-    case FLASHBEV_ACT_RELU: return launch_gemm<1, bf16, EW, FLASHBEV_ACT_RELU>(g, grid, stream);
-    case FLASHBEV_ACT_GELU: return launch_gemm<1, bf16, EW, FLASHBEV_ACT_GELU>(g, grid, stream);
-    case FLASHBEV_ACT_SILU: return launch_gemm<1, bf16, EW, FLASHBEV_ACT_SILU>(g, grid, stream);
-    default: return launch_gemm<1, bf16, EW, FLASHBEV_ACT_NONE>(g, grid, stream);
+    case FLASHBEV_ACT_RELU: return launch_gemm<PIECES, TOUT, EW, FLASHBEV_ACT_RELU>(g, grid, stream);
+    case FLASHBEV_ACT_GELU: return launch_gemm<PIECES, TOUT, EW, FLASHBEV_ACT_GELU>(g, grid, stream);
+    case FLASHBEV_ACT_SILU: return launch_gemm<PIECES, TOUT, EW, FLASHBEV_ACT_SILU>(g, grid, stream);
+    default: return launch_gemm<PIECES, TOUT, EW, FLASHBEV_ACT_NONE>(g, grid, stream);
     }
 }
 
@@ -1193,11 +1209,9 @@ flashbev_status run_product(const Plan &q, const Operand &a, const Operand &b, b
     cudaError_t err;
     // (partial sums are float32)
     const bool out_f32 = e.out_f32 || g.partial;
-    if (f32) err = out_f32 ? launch_gemm<3, float, 8, kAny>(g, q.grid, stream) : launch_gemm<3, bf16, 8, kAny>(g, q.grid, stream);
-    else if (out_f32) err = q.ew == 8 ? launch_gemm<1, float, 8, kAny>(g, q.grid, stream) : launch_gemm<1, float, 16, kAny>(g, q.grid, stream);
-    else if (!g.store_tma || (e.residual && g.res_vec != 16))
-        err = q.ew == 8 ? launch_gemm<1, bf16, 8, kAny>(g, q.grid, stream) : launch_gemm<1, bf16, 16, kAny>(g, q.grid, stream);
-    else err = q.ew == 8 ? launch_bf16<8>(g, q.grid, stream) : launch_bf16<16>(g, q.grid, stream);
+    if (f32) err = out_f32 ? launch_mode<3, float, 8>(g, q.grid, stream) : launch_mode<3, bf16, 8>(g, q.grid, stream);
+    else if (out_f32) err = q.ew == 8 ? launch_mode<1, float, 8>(g, q.grid, stream) : launch_mode<1, float, 16>(g, q.grid, stream);
+    else err = q.ew == 8 ? launch_mode<1, bf16, 8>(g, q.grid, stream) : launch_mode<1, bf16, 16>(g, q.grid, stream);
     ++launches;
     if (err == cudaSuccess && q.splits > 1) {
         if (f32) err = e.out_f32 ? launch_join<float, float>(q, partial, M, N, e, stream) : launch_join<float, bf16>(q, partial, M, N, e, stream);
@@ -1214,10 +1228,11 @@ flashbev_status run_product(const Plan &q, const Operand &a, const Operand &b, b
 template <typename TIN, typename TOUT>
 cudaError_t launch_rows(const void *x, long long ld_x, const void *weight, long long ld_w, int M, int N, int K, const Epilogue &e, cudaStream_t stream)
 {
-    const bool vec = (((uintptr_t)x | (uintptr_t)weight) | (uintptr_t)((ld_x | ld_w) * (long long)sizeof(TIN))) % 16 == 0;
+    const bool vec = K % 8 == 0 && (((uintptr_t)x | (uintptr_t)weight) | (uintptr_t)((ld_x | ld_w) * (long long)sizeof(TIN))) % 16 == 0;
     const auto go = [&](auto kernel, int nc) {
-        return launch_dependent(kernel, dim3((unsigned)((N + 8 * nc - 1) / (8 * nc))), dim3(256), 0, stream, static_cast<const TIN *>(x), ld_x,
-                                static_cast<const TIN *>(weight), ld_w, M, N, K, static_cast<const TIN *>(e.bias), static_cast<const TOUT *>(e.residual),
+        const int warps = (N + nc - 1) / nc, shared = K > 512 && warps < 4 * sm_count();
+        return launch_dependent(kernel, dim3((unsigned)(shared ? warps : (warps + 7) / 8)), dim3(256), 0, stream, static_cast<const TIN *>(x), ld_x,
+                                static_cast<const TIN *>(weight), ld_w, M, N, K, shared, static_cast<const TIN *>(e.bias), static_cast<const TOUT *>(e.residual),
                                 e.ld_res, static_cast<TOUT *>(e.out), e.ld_out, static_cast<TIN *>(e.pre), e.ld_pre, e.act);
     };
     if (M == 1) return vec ? go(rows_kernel<TIN, TOUT, 1, 2, true>, 2) : go(rows_kernel<TIN, TOUT, 1, 2, false>, 2);
