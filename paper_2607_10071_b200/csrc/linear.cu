@@ -175,11 +175,12 @@ __device__ __forceinline__ float2 slope_times(float2 g, float2 z, int act)
 
 // ---- the product ------------------------------------------------------------------------------------------------------------
 
-// pieces: 1 (bf16) or 3 (float32).  K of a stage: a swizzled row of 64 numbers, or of 32 where an operand has three tiles: three stages of 48 KB
-// (two of 96 KB: 59 us against 45 for 40000 x 256 x 256).
-__host__ __device__ constexpr int block_k(int pieces) { return pieces == 3 ? 32 : 64; }
+constexpr int kBK = 64;             // K of a stage: a swizzled row of 128 bytes (with rows of 64, TMA takes twice as long for the same bytes)
+constexpr int kMostStages = 12;
+constexpr int kSlot = 16 * 1024;    // float32 operands: a tile of one piece
+
 // Warps of the epilogue (EW): 16 for short sums, as it is their latency that those wait for (64-column sums of 184950 rows, 64 columns:
-// 25 us with eight, 20 us with 16); eight for long ones and for pieces, which leaves shared memory for a fourth stage of 48 KB.  (Registers are
+// 25 us with eight, 20 us with 16); eight for long ones, which leaves shared memory for a fourth stage of 48 KB, and for pieces (12 slots).  (Registers are
 // those of a quarter of an SM: the last warps of four, which do nothing, cost none.)
 __host__ __device__ constexpr int gemm_threads(int ew) { return 32 * (ew + 4); }
 // Bytes behind the ring: a buffer of 32 rows x 128 bytes and a bias of 64 columns per epilogue warp.
@@ -404,6 +405,25 @@ struct Shares {
     }
 };
 
+// float32 operands: every tile of a piece has a slot of shared memory and barriers of its own, twelve in all, six of one block and six of
+// the next.  A block's tiles come in the order below, and are released, from the first product that is their last on, in the order of
+// `released`; the tiles of the block after the next take the slots in that order, so that they are on their way while the last two sixths of this
+// block's products and all of the next one's run.  (Whole blocks in a ring of two: 36 us for 40000 x 256 x 256, so 27.)
+enum PieceTile { kA0 = 0, kB0 = 1, kB1 = 2, kA1 = 3, kB2 = 4, kA2 = 5 };
+
+struct Slots {
+    unsigned now = 0x543210u, after = 0xba9876u;  // slot of tile i of this block and of the next: four bits each
+    unsigned turn = 0;                            // parity of every slot's next use
+
+    __device__ __forceinline__ int of(int tile) const { return (int)(now >> 4 * tile & 15u); }
+    __device__ __forceinline__ void released()
+    {
+        const unsigned a0 = now & 15u, b0 = now >> 4 & 15u, b1 = now >> 8 & 15u, a1 = now >> 12 & 15u, b2 = now >> 16 & 15u, a2 = now >> 20 & 15u;
+        now = after;
+        after = b1 | a1 << 4 | a0 << 8 | b2 << 12 | b0 << 16 | a2 << 20;
+    }
+};
+
 // MODE: an activation, for results of unshared sums that leave by TMA, or kAny: everything as the parameters say.  What an instance does not need would be in its
 // way: the code of the other activations and of rows of any alignment, skipped, cost 8 of 37 us (184950 x 64 x 256) in instruction fetches.
 constexpr int kAny = 4;
@@ -412,15 +432,15 @@ template <int kPieces, typename TOUT, int kEpilogue, int MODE>
 __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const __grid_constant__ GemmParams p)
 {
     using TIN = typename std::conditional<kPieces == 3, float, bf16>::type;
-    constexpr int BK = block_k(kPieces), kRing = ring_bytes(kEpilogue);
+    constexpr int BK = kBK, kRing = ring_bytes(kEpilogue);
     extern __shared__ __align__(1024) unsigned char ring[];  // (the kernel declares no other: it starts on a swizzle's boundary)
     unsigned char *const staging = ring + kRing;
     float *const bias_rows = reinterpret_cast<float *>(staging + kEpilogue * 4096);  // 64 per warp
-    uint64_t *const bars = reinterpret_cast<uint64_t *>(staging + epilogue_bytes(kEpilogue));  // 2 * 8 + 2 * kAccs + 2
-    uint32_t &tmem_slot = *reinterpret_cast<uint32_t *>(bars + 2 * 8 + 2 * kAccs + 2);
+    uint64_t *const bars = reinterpret_cast<uint64_t *>(staging + epilogue_bytes(kEpilogue));  // 2 * kMostStages + 2 * kAccs + 2
+    uint32_t &tmem_slot = *reinterpret_cast<uint32_t *>(bars + 2 * kMostStages + 2 * kAccs + 2);
     volatile int &failed = *reinterpret_cast<volatile int *>(&tmem_slot + 1);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const uint32_t full = smem_u32(bars), empty = full + 64, acc_full = full + 128, acc_empty = acc_full + 8 * kAccs, last = acc_empty + 8 * kAccs, kept_full = last + 8;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * kMostStages, acc_full = empty + 8 * kMostStages, acc_empty = acc_full + 8 * kAccs, last = acc_empty + 8 * kAccs, kept_full = last + 8;
     // Tensor memory.  Two to four accumulators, so that some are taken out while another is filled.  The tensor cores cut a sum off, not round it, at
     // every instruction, by 3e-8 of the sum on the average.  So (1) pieces have a second accumulator for all products but p0 p0, which keeps the five
     // small products of each step from cutting at the large sum; (2) after `run` blocks the sum is added to a running one that stays in tensor
@@ -432,7 +452,7 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
 
     if (threadIdx.x == 0) {
         failed = 0;
-        for (int s = 0; s < p.stages; ++s) {
+        for (int s = 0; s < (kPieces == 3 ? kMostStages : p.stages); ++s) {
             mbar_init(full + 8 * s, 1);
             mbar_init(empty + 8 * s, 1);
         }
@@ -450,7 +470,7 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
 
-    const int a_bytes = kBM * 2 * BK, b_bytes = p.bn * 2 * BK, stage_bytes = kPieces * (a_bytes + (p.kept ? 0 : b_bytes));
+    const int a_bytes = kBM * 2 * BK, b_bytes = p.bn * 2 * BK, stage_bytes = a_bytes + (p.kept ? 0 : b_bytes);
     const uint32_t stages_at = smem_u32(ring) + p.kept;
 
     if (warp < kEpilogue) {
@@ -573,6 +593,7 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
             const uint32_t idesc = mma_idesc(p.bn, p.a_mn, p.b_mn);
             const int a_step = p.a_mn ? 2048 >> 4 : 32 >> 4, b_step = p.b_mn ? 2048 >> 4 : 32 >> 4;  // 16 of K further
             int stage = 0, phase = 0;
+            Slots slots;
             unsigned u = 0;  // accumulators filled so far
             bool ok = !p.kept || mbar_wait(kept_full, 0, &failed);
             for (Shares s(p); s.more(p) && ok; s.next(p)) {
@@ -586,24 +607,53 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
                     const uint32_t d = tmem + acc * acc_step, small = runs ? tmem + 3 * p.bn : d + p.bn;
                     const int k1 = min(k0 + p.run, s.end);
                     for (int k = k0; k < k1; ++k) {
-                        if (!(ok = mbar_wait(full + 8 * stage, phase, &failed))) break;
-                        tcgen05_fence_after();
-                        const uint32_t at = stages_at + stage * stage_bytes, b_at = p.kept ? smem_u32(ring) + k * b_bytes : at + kPieces * a_bytes;
-                        const uint64_t a = smem_desc(at, p.a_mn, 2 * BK, 128 * BK), b = smem_desc(b_at, p.b_mn, 2 * BK, 128 * BK);
                         if constexpr (kPieces == 1) {
+                            if (!(ok = mbar_wait(full + 8 * stage, phase, &failed))) break;
+                            tcgen05_fence_after();
+                            const uint32_t at = stages_at + stage * stage_bytes, b_at = p.kept ? smem_u32(ring) + k * b_bytes : at + a_bytes;
+                            const uint64_t a = smem_desc(at, p.a_mn, 128 * BK), b = smem_desc(b_at, p.b_mn, 128 * BK);
 #pragma unroll
                             for (int i = 0; i < BK / 16; ++i) mma_bf16(d, a + i * a_step, b + i * b_step, idesc, k > k0 || i > 0);
+                            mma_commit(empty + 8 * stage);
+                            if (++stage == p.stages) stage = 0, phase ^= 1;
                         } else {
-                            constexpr int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
+                            const auto arrived = [&](int tile) {
+                                const int slot = slots.of(tile);
+                                ok = ok && mbar_wait(full + 8 * slot, slots.turn >> slot & 1, &failed);
+                                slots.turn ^= 1u << slot;
+                            };
+                            const auto multiply = [&](uint32_t to, int ta, int tb, bool add) {
+                                const uint64_t a = smem_desc(smem_u32(ring) + slots.of(ta) * kSlot, p.a_mn, 128 * BK),
+                                               b = smem_desc(smem_u32(ring) + slots.of(tb) * kSlot, p.b_mn, 128 * BK);
 #pragma unroll
-                            for (int j = 0; j < 6; ++j)
-#pragma unroll
-                                for (int i = 0; i < BK / 16; ++i)
-                                    mma_bf16(j < 5 ? small : d, a + pa[j] * (a_bytes >> 4) + i * a_step, b + pb[j] * (b_bytes >> 4) + i * b_step, idesc,
-                                             i > 0 || (j < 5 ? k > s.k || j > 0 : k > k0));
+                                for (int i = 0; i < BK / 16; ++i) mma_bf16(to, a + i * a_step, b + i * b_step, idesc, add || i > 0);
+                            };
+                            const auto release = [&](int tile) { mma_commit(empty + 8 * slots.of(tile)); };
+                            arrived(kA0), arrived(kB0);
+                            if (!ok) break;
+                            tcgen05_fence_after();
+                            multiply(d, kA0, kB0, k > k0);
+                            arrived(kB1);
+                            if (!ok) break;
+                            tcgen05_fence_after();
+                            multiply(small, kA0, kB1, k > s.k);
+                            arrived(kA1);
+                            if (!ok) break;
+                            tcgen05_fence_after();
+                            multiply(small, kA1, kB0, true), multiply(small, kA1, kB1, true);
+                            release(kB1), release(kA1);
+                            arrived(kB2);
+                            if (!ok) break;
+                            tcgen05_fence_after();
+                            multiply(small, kA0, kB2, true);
+                            release(kA0), release(kB2);
+                            arrived(kA2);
+                            if (!ok) break;
+                            tcgen05_fence_after();
+                            multiply(small, kA2, kB0, true);
+                            release(kB0), release(kA2);
+                            slots.released();
                         }
-                        mma_commit(empty + 8 * stage);
-                        if (++stage == p.stages) stage = 0, phase ^= 1;
                     }
                     if (ok) mma_commit(acc_full + 8 * acc);
                 }
@@ -624,27 +674,47 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
                 else
                     for (int i = 0; i < p.bn / 64; ++i) tma_load_3d(at + 128 * BK * i, &p.tb, n0 + 64 * i, k * BK, piece, bar);
             };
+            const auto load_a = [&](uint32_t at, int m0, int k, int piece, uint32_t bar) {
+                if (!p.a_mn) tma_load_3d(at, &p.ta, k * BK, m0, piece, bar);
+                else
+                    for (int i = 0; i < kBM / 64; ++i) tma_load_3d(at + 128 * BK * i, &p.ta, m0 + 64 * i, k * BK, piece, bar);
+            };
             if (p.kept) {  // (the CTAs' number is a multiple of the tiles along N: a CTA's tiles all have the same columns)
                 mbar_expect(kept_full, p.kept);
                 for (int k = 0; k < p.kblocks; ++k) load_b(smem_u32(ring) + k * b_bytes, Shares(p).n0, k, 0, kept_full);
             }
+            Slots slots;
             for (Shares s(p); s.more(p) && ok; s.next(p)) {
                 for (int k = s.k; k < s.end; ++k) {
-                    if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, &failed))) break;
-                    const uint32_t bar = full + 8 * stage;
-                    uint32_t at = stages_at + stage * stage_bytes;
-                    mbar_expect(bar, stage_bytes);
-                    for (int piece = 0; piece < kPieces; ++piece, at += a_bytes)
-                        if (!p.a_mn) tma_load_3d(at, &p.ta, k * BK, s.m0, piece, bar);
-                        else
-                            for (int i = 0; i < kBM / 64; ++i) tma_load_3d(at + 128 * BK * i, &p.ta, s.m0 + 64 * i, k * BK, piece, bar);
-                    for (int piece = 0; piece < kPieces && !p.kept; ++piece, at += b_bytes) load_b(at, s.n0, k, piece, bar);
-                    if (++stage == p.stages) stage = 0, phase ^= 1;
+                    if constexpr (kPieces == 1) {
+                        if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, &failed))) break;
+                        const uint32_t bar = full + 8 * stage, at = stages_at + stage * stage_bytes;
+                        mbar_expect(bar, stage_bytes);
+                        load_a(at, s.m0, k, 0, bar);
+                        if (!p.kept) load_b(at + a_bytes, s.n0, k, 0, bar);
+                        if (++stage == p.stages) stage = 0, phase ^= 1;
+                    } else {
+#pragma unroll
+                        for (int tile = 0; tile < 6; ++tile) {
+                            const int slot = slots.of(tile), piece = tile == kA0 || tile == kB0 ? 0 : (tile == kA1 || tile == kB1 ? 1 : 2);
+                            if (!(ok = ok && mbar_wait(empty + 8 * slot, (slots.turn >> slot & 1) ^ 1, &failed))) break;
+                            slots.turn ^= 1u << slot;
+                            const bool is_a = tile == kA0 || tile == kA1 || tile == kA2;
+                            const uint32_t bar = full + 8 * slot, at = smem_u32(ring) + slot * kSlot;
+                            mbar_expect(bar, is_a ? a_bytes : b_bytes);
+                            if (is_a) load_a(at, s.m0, k, piece, bar);
+                            else load_b(at, s.n0, k, piece, bar);
+                        }
+                        slots.released();
+                        if (!ok) break;
+                    }
                 }
             }
             if (!ok && p.kept) mbar_drain(kept_full, 0);
-            if (!ok)  // the last load into every stage: the ones before `stage` in this round of the ring, the others in the round before
+            if (!ok && kPieces == 1)  // the last load into every stage: the ones before `stage` in this round of the ring, the others in the round before
                 for (int i = 0; i < p.stages; ++i) mbar_drain(full + 8 * i, i < stage ? phase : phase ^ 1);
+            if (!ok && kPieces == 3)
+                for (int i = 0; i < kMostStages; ++i) mbar_drain(full + 8 * i, (slots.turn >> i & 1) ^ 1);
         }
         __syncwarp();
     }
@@ -1023,12 +1093,12 @@ bool make_map(CUtensorMap &map, const Operand &o, int pieces, int across, int K,
 {
     const EncodeTiled encode = encode_tiled();
     if (!encode) return false;
-    const int bk = block_k(pieces);
+    constexpr int bk = kBK;
     const cuuint64_t size[3] = {(cuuint64_t)(o.mn ? across : K), (cuuint64_t)(o.mn ? K : across), (cuuint64_t)pieces};
     const cuuint64_t pitch[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)(pieces == 1 ? o.ld : o.layer) * 2};
     const cuuint32_t box[3] = {(cuuint32_t)(o.mn ? 64 : bk), (cuuint32_t)(o.mn ? bk : rows), 1}, step[3] = {1, 1, 1};
     return encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(o.p), size, pitch, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  o.mn || bk == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -1062,9 +1132,9 @@ struct Plan {
 Plan plan_product(bool b_mn, bool f32, bool out_f32, bool heavy, int M, int N, int K, bool may_split)
 {
     Plan q = {};
-    const int sms = sm_count(), pieces = f32 ? 3 : 1;
+    const int sms = sm_count();
     q.tiles_m = (M + kBM - 1) / kBM;
-    const int bk = block_k(pieces);
+    constexpr int bk = kBK;
     q.kblocks = (K + bk - 1) / bk;
     const bool runs = out_f32 && K > kRun;
     // Widths: the columns in equal parts, at most 256 (128 where accumulators for pieces or a running sum take tensor memory); and shares of
@@ -1078,7 +1148,7 @@ Plan plan_product(bool b_mn, bool f32, bool out_f32, bool heavy, int M, int N, i
         const long long tiles = (long long)q.tiles_m * ((N + bn - 1) / bn);
         const int most = may_split && tiles * 2 <= sms ? (int)std::min<long long>(sms / tiles, (long long)q.kblocks * bk / 128) : 1;
         const int share = (q.kblocks + std::max(1, most) - 1) / std::max(1, most), splits = (q.kblocks + share - 1) / share;
-        const double items = (double)((tiles * splits + sms - 1) / sms), main = share * (f32 ? 8.0 : 2.15) * std::max(kBM + bn, f32 ? 0 : 360);
+        const double items = (double)((tiles * splits + sms - 1) / sms), main = share * (f32 ? 10.0 : 2.15) * std::max(kBM + bn, f32 ? 0 : 360);
         const double rest = 12.0 * bn + 800.0, join = splits > 1 ? 4000.0 + splits * 8.0 * M * N / 2000.0 : 0.0;
         const double cost = items * std::max(main, rest) + std::min(main, rest) + join;
         if (q.bn == 0 || cost < best) best = cost, q.bn = bn, q.kshare = share, q.splits = splits;
@@ -1088,12 +1158,12 @@ Plan plan_product(bool b_mn, bool f32, bool out_f32, bool heavy, int M, int N, i
     // B stays in shared memory where all of K fits beside three stages of A and a CTA has several tiles: its loads are two thirds of a 128 x 256
     // tile's.
     const long long tiles = (long long)q.tiles_m * q.tiles_n;
-    const int b_bytes = q.kblocks * q.bn * 2 * bk, a_bytes = pieces * kBM * 2 * bk, spread = sms / q.tiles_n * q.tiles_n;
+    const int b_bytes = q.kblocks * q.bn * 2 * bk, a_bytes = kBM * 2 * bk, spread = sms / q.tiles_n * q.tiles_n;
     q.grid = (int)std::min<long long>(tiles * q.splits, sms);
     if (!f32 && !heavy && q.splits == 1 && b_bytes + 3 * a_bytes <= ring_bytes(8) && tiles > spread && spread > 0 && spread * 20 >= sms * 19)
         q.kept = b_bytes, q.grid = spread;
     q.ew = f32 || q.kept || q.kshare * bk > kShort ? 8 : 16;
-    q.stages = std::min(8, (ring_bytes(q.ew) - q.kept) / (a_bytes + (q.kept ? 0 : pieces * q.bn * 2 * bk)));
+    q.stages = std::min(8, (ring_bytes(q.ew) - q.kept) / (a_bytes + (q.kept ? 0 : q.bn * 2 * bk)));  // (of bf16 operands)
     q.run = runs && q.kshare > kRun / bk ? kRun / bk : q.kshare;
     // Accumulators: with runs two, the running sum and, of float32 operands, that of the small products; else four where they fit (float32
     // operands: pairs).  Groups of epilogue warps: as many 64-column parts as the tile has in each, and no more of them than accumulators.
@@ -1136,7 +1206,7 @@ cudaError_t launch_gemm(const GemmParams &g, int grid, cudaStream_t stream)
 {
     const auto kernel = gemm_kernel<PIECES, TOUT, EW, MODE>;
     constexpr int smem = ring_bytes(EW) + epilogue_bytes(EW) + kControlBytes;
-    static_assert(smem <= kSmemLimit && ring_bytes(8) >= 4 * 48 * 1024 && ring_bytes(16) >= 3 * 48 * 1024, "");
+    static_assert(smem <= kSmemLimit && ring_bytes(8) >= kMostStages * kSlot && ring_bytes(16) >= 3 * 48 * 1024, "");
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     return launch_dependent(kernel, dim3((unsigned)grid), dim3((unsigned)gemm_threads(EW)), smem, stream, g);
@@ -1278,7 +1348,12 @@ struct ForwardPlan {
 
 // An epilogue that 16 warps are worth more for than weights that stay in shared memory: special functions, a residual to wait for
 // (184950 x 256 x 256, GELU 52 us with eight, 40 with 16; with a residual 59 and 49)
-bool heavy_epilogue(const flashbev_linear_params *p) { return p->act >= FLASHBEV_ACT_GELU || p->residual; }
+bool heavy_epilogue(const flashbev_linear_params *p)
+{
+    const bool out_f32 = p->out_dtype == FLASHBEV_F32;
+    return p->act >= FLASHBEV_ACT_GELU || (p->residual && vec_ok(p->residual, dense(p->ld_residual, p->out_features), out_f32) &&
+                                           vec_ok(p->out, dense(p->ld_out, p->out_features), out_f32));
+}
 
 ForwardPlan plan_forward(const flashbev_linear_params *p)
 {

@@ -134,13 +134,13 @@ __host__ __device__ constexpr uint32_t mma_idesc(int n, bool a_mn, bool b_mn)
            ((128u >> 4) << 24);
 }
 
-// Shared-memory descriptor of a tile, its base a multiple of 1024 bytes.  K-major: a row of the operand is `row` bytes of K, 128 or 64,
-// swizzled over 128 or 64 bytes, eight rows are 8 `row` apart.  MN-major: a row is 64 elements along M or N at one k (128 bytes, swizzled
-// so), eight k are 1024 bytes apart, the next 64 along M or N `block` bytes.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn, uint32_t row, uint32_t block)
+// Shared-memory descriptor of a tile of 128-byte rows with 128-byte swizzle, its base a multiple of 1024 bytes.  K-major: a row of
+// the operand is 64 elements of K, eight rows are 1024 bytes apart.  MN-major: a row is 64 elements along M or N at one k, eight k
+// are 1024 bytes apart, the next 64 along M or N `block` bytes.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn, uint32_t block)
 {
-    const uint64_t lead = mn ? (uint64_t)(block >> 4) : 1, step = mn ? 1024 : 8 * row, swizzle = mn || row == 128 ? 2 : 4;
-    return (uint64_t)((addr & 0x3ffff) >> 4) | (lead << 16) | ((step >> 4) << 32) | (1ull << 46) | (swizzle << 61);
+    const uint64_t lead = mn ? (uint64_t)(block >> 4) : 1;
+    return (uint64_t)((addr & 0x3ffff) >> 4) | (lead << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
 // 32 columns of the warp's 32 lanes of tensor memory (a warp reaches the lanes 32 (warp % 4) and up).  The registers hold them after
