@@ -408,7 +408,8 @@ struct Shares {
 // float32 operands: every tile of a piece has a slot of shared memory and barriers of its own, twelve in all, six of one block and six of
 // the next.  A block's tiles come in the order below, and are released, from the first product that is their last on, in the order of
 // `released`; the tiles of the block after the next take the slots in that order, so that they are on their way while the last two sixths of this
-// block's products and all of the next one's run.  (Whole blocks in a ring of two: 36 us for 40000 x 256 x 256, so 27.)
+// block's products and all of the next one's run.  (40000 x 256 x 256: 31 us, of which the loads by themselves take 17 and loads and products 25;
+// stages of 32 of K in a ring of four, their rows of 64 bytes, 36.)
 enum PieceTile { kA0 = 0, kB0 = 1, kB1 = 2, kA1 = 3, kB2 = 4, kA2 = 5 };
 
 struct Slots {
@@ -729,20 +730,59 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
 
 // ---- sums that several CTAs shared ----------------------------------------------------------------------------------------
 
+// Column sums of partial sums, `rows` rows of N: 32 columns per block of eight warps, which take every eighth row.
+template <typename T>
+struct ColumnSums {
+    const float *sums;
+    int rows, N;
+    T *out;   // NULL: none
+};
+
+template <typename T>
+__device__ __forceinline__ void column_sums(const ColumnSums<T> &q, int block, float (&part)[8][33])
+{
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, col = block * 32 + lane;
+    float v = 0.0f;
+    if (col < q.N)
+#pragma unroll 16
+        for (int r = warp; r < q.rows; r += 8) v += q.sums[(long long)r * q.N + col];
+    part[warp][lane] = v;
+    __syncthreads();
+    if (warp == 0 && col < q.N) {
+        v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) v += part[w][lane];
+        q.out[col] = from_float<T>(v);
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) column_sum_kernel(const ColumnSums<T> q)
+{
+    __shared__ float part[8][33];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+    column_sums(q, blockIdx.x, part);
+}
+
 // Adds the shares up in a fixed order and does what the epilogue would have done.  Four columns of a row per thread; with few of them (`groups` > 1)
-// as many threads take every so manieth share, and the first of them joins their sums.
+// as many threads take every so manieth share, and the first of them joins their sums.  The last blocks (from `first_sum` on) add up column sums.
 template <typename TIN, typename TOUT>
 __global__ void __launch_bounds__(256) join_kernel(const float *__restrict__ partial, long long ld_partial, int splits, int groups, int M, int N,
                                                    const TIN *__restrict__ bias, const TOUT *residual, long long ld_res, TOUT *out, long long ld_out,
-                                                   TIN *pre, long long ld_pre, int act)
+                                                   TIN *pre, long long ld_pre, int act, const ColumnSums<TIN> columns, int first_sum)
 {
     constexpr bool kFast = std::is_same<TOUT, bf16>::value;
-    __shared__ float4 joined[256];
+    __shared__ float4 joined[8 * 33];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
+    if ((int)blockIdx.x >= first_sum) {
+        column_sums(columns, blockIdx.x - first_sum, reinterpret_cast<float (&)[8][33]>(joined));
+        return;
+    }
     const int quads = (int)(ld_partial / 4), width = 256 / groups, group = threadIdx.x / width, t = threadIdx.x % width;
     const long long all = (long long)M * quads, step = (long long)M * ld_partial / 4;
-    for (long long i0 = (long long)blockIdx.x * width; i0 < all; i0 += (long long)gridDim.x * width) {
+    for (long long i0 = (long long)blockIdx.x * width; i0 < all; i0 += (long long)first_sum * width) {
         const long long i = i0 + t, row = i / quads;
         const int col = (int)(i - row * quads) * 4;
         const float4 *src = reinterpret_cast<const float4 *>(partial) + row * (ld_partial / 4) + col / 4;
@@ -814,17 +854,11 @@ struct LayoutJob {
     unsigned lanes;         // threads of a row: one for eight elements, or for two
 };
 
-// Two jobs, x and the weights: whole blocks of either.  Rows of whole vectors: a thread has eight elements; others: two, so that a warp touches
-// each sector once.
+// Rows of whole vectors: a thread has eight elements; others: two, so that a warp touches each sector once.
 template <typename T>
-__global__ void __launch_bounds__(256) layout_kernel(const LayoutJob first, const LayoutJob second, unsigned first_blocks)
+__device__ __forceinline__ void lay_out(const LayoutJob &q, unsigned block, unsigned blocks)
 {
     constexpr int kP = sizeof(T) == 4 ? 3 : 1;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;");
-    const bool is_first = blockIdx.x < first_blocks;
-    const LayoutJob &q = is_first ? first : second;
-    const unsigned block = is_first ? blockIdx.x : blockIdx.x - first_blocks, blocks = is_first ? first_blocks : gridDim.x - first_blocks;
     // (place in the row and row, a grid's step on: no division for every piece)
     const unsigned start = block * 256 + threadIdx.x, step = blocks * 256;
     unsigned row = start / q.lanes, lane = start - row * q.lanes;
@@ -858,29 +892,55 @@ __global__ void __launch_bounds__(256) layout_kernel(const LayoutJob first, cons
     }
 }
 
+// Two jobs, x and the weights: whole blocks of either.
+struct LayoutJobs {
+    LayoutJob first, second;
+    unsigned first_blocks, blocks;  // 0: none
+
+    template <typename T>
+    __device__ __forceinline__ void run(unsigned block) const
+    {
+        if (block < first_blocks) lay_out<T>(first, block, first_blocks);
+        else lay_out<T>(second, block - first_blocks, blocks - first_blocks);
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(256) layout_kernel(const __grid_constant__ LayoutJobs jobs)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+    jobs.run<T>(blockIdx.x);
+}
+
 // ---- dz = grad_out act'(z), and its column sums ---------------------------------------------------------------------------
 
 constexpr int kSlopeRows = 8;  // warps of a block: each takes every eighth row of the block's
 
-// A lane has VEC neighbouring columns, a warp a stretch of a row, the block `per` rows.  dz, in bf16 numbers or three pieces `layer` apart, may be NULL
+// A lane has VEC neighbouring columns, a warp a stretch of a row, the block `per` rows; blocks behind those lay the other operands out.  dz, in bf16 numbers or three pieces `layer` apart, may be NULL
 // (column sums only), sums too.
 template <typename TG, typename TZ, int VEC>
 __global__ void __launch_bounds__(32 * kSlopeRows) slope_kernel(const TG *__restrict__ g, long long ld_g, const TZ *__restrict__ z, long long ld_z,
                                                                 bf16 *__restrict__ dz, long long ld_dz, long long layer, float *__restrict__ sums, int M,
-                                                                int N, int per, int act)
+                                                                int N, int per, int act, unsigned across, unsigned blocks,
+                                                                const __grid_constant__ LayoutJobs jobs)
 {
     constexpr bool kFast = std::is_same<TZ, bf16>::value;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int col = (blockIdx.x * 32 + lane) * VEC;
-    const long long row1 = min((long long)M, (long long)(blockIdx.y + 1) * per);
+    if (blockIdx.x >= blocks) {
+        jobs.run<TZ>(blockIdx.x - blocks);
+        return;
+    }
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, chunk = blockIdx.x / across;
+    const int block = blockIdx.x - chunk * across, col = (block * 32 + lane) * VEC;
+    const long long row1 = min((long long)M, (long long)(chunk + 1) * per);
     float acc[VEC];
 #pragma unroll
     for (int j = 0; j < VEC; ++j) acc[j] = 0.0f;
     if (col < N)
 #pragma unroll 4
-        for (long long row = (long long)blockIdx.y * per + warp; row < row1; row += kSlopeRows) {
+        for (long long row = (long long)chunk * per + warp; row < row1; row += kSlopeRows) {
             TG gv[VEC];
             TZ zv[VEC];
             if constexpr (VEC > 1) {
@@ -934,34 +994,13 @@ __global__ void __launch_bounds__(32 * kSlopeRows) slope_kernel(const TG *__rest
     for (int j = 0; j < VEC; ++j) part[warp][lane * VEC + j] = acc[j];
     __syncthreads();
     for (int c = threadIdx.x; c < 32 * VEC; c += 32 * kSlopeRows) {
-        const int at = blockIdx.x * 32 * VEC + c;
+        const int at = block * 32 * VEC + c;
         if (at >= N) break;
         float v = 0.0f;
 #pragma unroll
         for (int w = 0; w < kSlopeRows; ++w) v += part[w][c];
-        sums[(long long)blockIdx.y * N + at] = v;
+        sums[(long long)chunk * N + at] = v;
     }
-}
-
-// Column sums of `rows` rows of partial sums: 32 columns per block, its 32 warps take every 32nd row.
-template <typename T>
-__global__ void __launch_bounds__(1024) column_sum_kernel(const float *__restrict__ sums, int rows, int N, T *__restrict__ out)
-{
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;");
-    __shared__ float part[32][33];
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, col = blockIdx.x * 32 + lane;
-    float v = 0.0f;
-    if (col < N)
-#pragma unroll 8
-        for (int r = warp; r < rows; r += 32) v += sums[(long long)r * N + col];
-    part[warp][lane] = v;
-    __syncthreads();
-    // a column's 32 numbers by a warp of their own
-    v = part[lane][warp];
-#pragma unroll
-    for (int d = 16; d; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
-    if (lane == 0 && blockIdx.x * 32 + warp < N) out[blockIdx.x * 32 + warp] = from_float<T>(v);
 }
 
 // ---- few rows ---------------------------------------------------------------------------------------------------------------
@@ -1188,6 +1227,10 @@ struct Epilogue {
     long long ld_res = 0, ld_out = 0, ld_pre = 0;
     int act = FLASHBEV_ACT_NONE;
     bool out_f32 = false;
+    // column sums that a kernel which joins shares adds up beside them
+    const float *sums = nullptr;
+    int sum_rows = 0, sum_columns = 0;
+    void *sum_out = nullptr;
 };
 
 bool vec_ok(const void *p, long long ld, bool f32)
@@ -1224,20 +1267,28 @@ cudaError_t launch_mode(const GemmParams &g, int grid, cudaStream_t stream)
     }
 }
 
-// Lays one or two operands out in the scratch
-template <typename T>
-cudaError_t launch_layout(LayoutJob *jobs, int count, cudaStream_t stream)
-{
-    unsigned blocks[2] = {0, 0};
-    for (int i = 0; i < count; ++i) {
-        LayoutJob &q = jobs[i];
-        q.ld_to = laid_out_ld(q.width), q.layer = q.rows * q.ld_to;
-        q.vec = q.width % 8 == 0 && ((uintptr_t)q.from | (uintptr_t)(q.ld * (long long)sizeof(T))) % 16 == 0;
-        q.lanes = (unsigned)(q.vec ? q.width / 8 : (q.width + 1) / 2);
-        blocks[i] = (unsigned)std::min<long long>(((long long)q.rows * q.lanes + 255) / 256, 8LL * sm_count());
+// Operands to be laid out in the scratch
+struct Layouts {
+    LayoutJobs jobs = {};
+    int count = 0;
+
+    // `o` becomes the operand's place in the scratch
+    void add(Operand &o, char *to, int rows, int width, bool f32)
+    {
+        LayoutJob &q = count++ ? jobs.second : jobs.first;
+        q.from = o.p, q.to = reinterpret_cast<bf16 *>(to), q.ld = o.ld, q.rows = rows, q.width = width;
+        q.ld_to = laid_out_ld(width), q.layer = rows * q.ld_to;
+        q.vec = width % 8 == 0 && ((uintptr_t)q.from | (uintptr_t)(q.ld * (f32 ? 4 : 2))) % 16 == 0;
+        q.lanes = (unsigned)(q.vec ? width / 8 : (width + 1) / 2);
+        jobs.blocks += (unsigned)std::min<long long>(((long long)rows * q.lanes + 255) / 256, 8LL * sm_count());
+        if (count == 1) jobs.first_blocks = jobs.blocks;
+        o = {q.to, q.ld_to, o.mn, q.layer};
     }
-    return launch_dependent(layout_kernel<T>, dim3(blocks[0] + blocks[1]), dim3(256), 0, stream, jobs[0], jobs[count - 1], blocks[0]);
-}
+    cudaError_t launch(bool f32, cudaStream_t stream) const
+    {
+        return launch_dependent(f32 ? layout_kernel<float> : layout_kernel<bf16>, dim3(jobs.blocks), dim3(256), 0, stream, jobs);
+    }
+};
 
 template <typename TIN, typename TOUT>
 cudaError_t launch_join(const Plan &q, const float *partial, int M, int N, const Epilogue &e, cudaStream_t stream)
@@ -1246,9 +1297,10 @@ cudaError_t launch_join(const Plan &q, const float *partial, int M, int N, const
     int groups = 1;
     while (groups < 16 && groups * 2 <= q.splits && quads * groups < 1024LL * sm_count()) groups *= 2;
     const unsigned blocks = (unsigned)std::min<long long>((quads * groups + 255) / 256, 8LL * sm_count());
-    return launch_dependent(join_kernel<TIN, TOUT>, dim3(blocks), dim3(256), 0, stream, partial, q.ld_partial, q.splits, groups, M, N,
+    const ColumnSums<TIN> columns = {e.sums, e.sum_rows, e.sum_columns, static_cast<TIN *>(e.sum_out)};
+    return launch_dependent(join_kernel<TIN, TOUT>, dim3(blocks + (e.sum_out ? (unsigned)(e.sum_columns + 31) / 32 : 0)), dim3(256), 0, stream, partial, q.ld_partial, q.splits, groups, M, N,
                             static_cast<const TIN *>(e.bias), static_cast<const TOUT *>(e.residual), e.ld_res, static_cast<TOUT *>(e.out), e.ld_out,
-                            static_cast<TIN *>(e.pre), e.ld_pre, e.act);
+                            static_cast<TIN *>(e.pre), e.ld_pre, e.act, columns, (int)blocks);
 }
 
 // Enqueues one product; adds the kernels to `launches`.
@@ -1422,7 +1474,6 @@ BackwardPlan plan_backward(const flashbev_linear_backward_params *p)
         const long long blocks = std::max(1, 4 * sm_count() / across);
         q.per = (int)std::max<long long>(32, (M + blocks - 1) / blocks);
         q.chunks = (M + q.per - 1) / q.per;
-        if (q.chunks > 65535) q.per = (M + 65534) / 65535, q.chunks = (M + q.per - 1) / q.per;
         if (q.need_b) q.sums_at = at, at += round_up((size_t)q.chunks * N * sizeof(float));
     }
     if (q.need_x) q.gx = plan_product(true, f32, f32, false, M, K, N, true);
@@ -1433,7 +1484,7 @@ BackwardPlan plan_backward(const flashbev_linear_backward_params *p)
 }
 
 template <typename TG, typename TZ>
-cudaError_t launch_slope(const flashbev_linear_backward_params *p, const BackwardPlan &q, cudaStream_t stream)
+cudaError_t launch_slope(const flashbev_linear_backward_params *p, const BackwardPlan &q, const LayoutJobs &jobs, cudaStream_t stream)
 {
     const int M = (int)p->rows, N = p->out_features;
     char *const ws = static_cast<char *>(p->workspace);
@@ -1444,9 +1495,9 @@ cudaError_t launch_slope(const flashbev_linear_backward_params *p, const Backwar
     const long long ld_g = dense(p->ld_grad_out, N), ld_z = dense(p->ld_preact, N);
     const bool vec = N % 8 == 0 && vec_ok(p->grad_out, ld_g, sizeof(TG) == 4) && (!z || vec_ok(z, ld_z, sizeof(TZ) == 4));
     const int width = 32 * (vec ? 8 : 1);
-    const dim3 grid((unsigned)((N + width - 1) / width), (unsigned)q.chunks);
-    return launch_dependent(vec ? slope_kernel<TG, TZ, 8> : slope_kernel<TG, TZ, 1>, grid, dim3(32 * kSlopeRows), 0, stream,
-                            static_cast<const TG *>(p->grad_out), ld_g, z, ld_z, dz, ld_dz, M * ld_dz, sums, M, N, q.per, p->act);
+    const unsigned across = (unsigned)((N + width - 1) / width), blocks = across * (unsigned)q.chunks;
+    return launch_dependent(vec ? slope_kernel<TG, TZ, 8> : slope_kernel<TG, TZ, 1>, dim3(blocks + jobs.blocks), dim3(32 * kSlopeRows), 0, stream,
+                            static_cast<const TG *>(p->grad_out), ld_g, z, ld_z, dz, ld_dz, M * ld_dz, sums, M, N, q.per, p->act, across, blocks, jobs);
 }
 
 }  // namespace
@@ -1485,17 +1536,11 @@ flashbev_status flashbev_linear(const flashbev_linear_params *p, void *stream_)
             if (have < q.total) q.product = plan_product(false, f32, e.out_f32, heavy_epilogue(p), M, N, K, false);
             char *const ws = static_cast<char *>(p->workspace);
             Operand x = {p->x, ld_x, false}, w = {p->weight, ld_w, false};
-            LayoutJob jobs[2] = {};
-            int count = 0;
-            const auto lay = [&](Operand &o, size_t at, int rows) {
-                LayoutJob &j = jobs[count++];
-                j.from = o.p, j.to = reinterpret_cast<bf16 *>(ws + at), j.ld = o.ld, j.rows = rows, j.width = K;
-                o = {j.to, laid_out_ld(K), o.mn, rows * laid_out_ld(K)};
-            };
-            if (q.lay_x) lay(x, q.x_at, M);
-            if (q.lay_w) lay(w, q.w_at, N);
-            if (count) {
-                if ((f32 ? launch_layout<float>(jobs, count, stream) : launch_layout<bf16>(jobs, count, stream)) != cudaSuccess) {
+            Layouts layouts;
+            if (q.lay_x) layouts.add(x, ws + q.x_at, M, K, f32);
+            if (q.lay_w) layouts.add(w, ws + q.w_at, N, K, f32);
+            if (layouts.count) {
+                if (layouts.launch(f32, stream) != cudaSuccess) {
                     cudaGetLastError();
                     return FLASHBEV_CUDA_ERROR;
                 }
@@ -1504,7 +1549,7 @@ flashbev_status flashbev_linear(const flashbev_linear_params *p, void *stream_)
             const flashbev_status run =
                 run_product(q.product, x, w, f32, M, N, K, e, reinterpret_cast<float *>(ws + q.partial_at), p->error_word, stream, launches);
             if (run != FLASHBEV_OK) return run;
-            t_last_kernel = f32 ? "linear_f32" : (count ? "linear_bf16_laid_out" : "linear_bf16");
+            t_last_kernel = f32 ? "linear_f32" : (layouts.count ? "linear_bf16_laid_out" : "linear_bf16");
         }
     }
     t_last_launches = launches;
@@ -1539,44 +1584,39 @@ flashbev_status flashbev_linear_backward(const flashbev_linear_backward_params *
     }
     char *const ws = static_cast<char *>(p->workspace);
     cudaError_t err = cudaSuccess;
+    Operand dz = {p->grad_out, dense(p->ld_grad_out, N), false};
+    if (q.need_dz) dz = {ws + q.dz_at, laid_out_ld(N), false, M * laid_out_ld(N)};
+    Operand x = {p->x, dense(p->ld_x, K), true}, w = {p->weight, dense(p->ld_weight, K), true};
+    Layouts layouts;
+    if (q.lay_x) layouts.add(x, ws + q.x_at, M, K, f32);
+    if (q.lay_w) layouts.add(w, ws + q.w_at, N, K, f32);
     if (q.need_dz || q.need_b) {
-        if (f32) err = launch_slope<float, float>(p, q, stream);
-        else err = p->grad_dtype == FLASHBEV_F32 ? launch_slope<float, bf16>(p, q, stream) : launch_slope<bf16, bf16>(p, q, stream);
+        if (f32) err = launch_slope<float, float>(p, q, layouts.jobs, stream);
+        else err = p->grad_dtype == FLASHBEV_F32 ? launch_slope<float, bf16>(p, q, layouts.jobs, stream) : launch_slope<bf16, bf16>(p, q, layouts.jobs, stream);
         ++launches;
-        if (err == cudaSuccess && q.need_b) {
-            const float *const sums = reinterpret_cast<const float *>(ws + q.sums_at);
-            const dim3 grid((unsigned)((N + 31) / 32));
-            if (f32) err = launch_dependent(column_sum_kernel<float>, grid, dim3(1024), 0, stream, sums, q.chunks, N, static_cast<float *>(p->grad_bias));
-            else err = launch_dependent(column_sum_kernel<bf16>, grid, dim3(1024), 0, stream, sums, q.chunks, N, static_cast<bf16 *>(p->grad_bias));
-            ++launches;
-        }
+    } else if (layouts.count) {
+        err = layouts.launch(f32, stream);
+        ++launches;
+    }
+    if (err != cudaSuccess) {
+        cudaGetLastError();
+        return FLASHBEV_CUDA_ERROR;
+    }
+    float *const partial = reinterpret_cast<float *>(ws + q.partial_at);
+    Epilogue e;
+    e.out_f32 = f32;
+    const float *const sums = reinterpret_cast<const float *>(ws + q.sums_at);
+    const bool joins = q.need_w && q.gw.splits > 1;  // the bias' gradient from the kernel that joins the weights'
+    if (q.need_b && !joins) {
+        const dim3 grid((unsigned)((N + 31) / 32));
+        if (f32) err = launch_dependent(column_sum_kernel<float>, grid, dim3(256), 0, stream, ColumnSums<float>{sums, q.chunks, N, static_cast<float *>(p->grad_bias)});
+        else err = launch_dependent(column_sum_kernel<bf16>, grid, dim3(256), 0, stream, ColumnSums<bf16>{sums, q.chunks, N, static_cast<bf16 *>(p->grad_bias)});
+        ++launches;
         if (err != cudaSuccess) {
             cudaGetLastError();
             return FLASHBEV_CUDA_ERROR;
         }
     }
-    Operand dz = {p->grad_out, dense(p->ld_grad_out, N), false};
-    if (q.need_dz) dz = {ws + q.dz_at, laid_out_ld(N), false, M * laid_out_ld(N)};
-    Operand x = {p->x, dense(p->ld_x, K), true}, w = {p->weight, dense(p->ld_weight, K), true};
-    LayoutJob jobs[2] = {};
-    int count = 0;
-    const auto lay = [&](Operand &o, size_t at, int rows) {
-        LayoutJob &j = jobs[count++];
-        j.from = o.p, j.to = reinterpret_cast<bf16 *>(ws + at), j.ld = o.ld, j.rows = rows, j.width = K;
-        o = {j.to, laid_out_ld(K), o.mn, rows * laid_out_ld(K)};
-    };
-    if (q.lay_x) lay(x, q.x_at, M);
-    if (q.lay_w) lay(w, q.w_at, N);
-    if (count) {
-        if ((f32 ? launch_layout<float>(jobs, count, stream) : launch_layout<bf16>(jobs, count, stream)) != cudaSuccess) {
-            cudaGetLastError();
-            return FLASHBEV_CUDA_ERROR;
-        }
-        ++launches;
-    }
-    float *const partial = reinterpret_cast<float *>(ws + q.partial_at);
-    Epilogue e;
-    e.out_f32 = f32;
     if (q.need_x) {
         e.out = p->grad_x, e.ld_out = dense(p->ld_grad_x, K);
         const flashbev_status run = run_product(q.gx, dz, w, f32, M, K, N, e, partial, p->error_word, stream, launches);
@@ -1586,6 +1626,7 @@ flashbev_status flashbev_linear_backward(const flashbev_linear_backward_params *
         Operand dzt = dz;
         dzt.mn = true;
         e.out = p->grad_weight, e.ld_out = dense(p->ld_grad_weight, K);
+        if (q.need_b && joins) e.sums = sums, e.sum_rows = q.chunks, e.sum_columns = N, e.sum_out = p->grad_bias;
         const flashbev_status run = run_product(q.gw, dzt, x, f32, N, K, M, e, partial, p->error_word, stream, launches);
         if (run != FLASHBEV_OK) return run;
     }
