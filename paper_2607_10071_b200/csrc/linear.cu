@@ -770,7 +770,7 @@ __device__ __forceinline__ void column_sums(const ColumnSums<T> &q, int block, f
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, col = block * 32 + lane;
     float v = 0.0f;
     if (col < q.N)
-#pragma unroll 16
+#pragma unroll 32
         for (int r = warp; r < q.rows; r += 8) v += q.sums[(long long)r * q.N + col];
     part[warp][lane] = v;
     __syncthreads();
@@ -792,23 +792,24 @@ __global__ void __launch_bounds__(256) column_sum_kernel(const ColumnSums<T> q)
 }
 
 // Adds the shares up in a fixed order and does what the epilogue would have done.  Four columns of a row per thread; with few of them (`groups` > 1)
-// as many threads take every so manieth share, and the first of them joins their sums.  The last blocks (from `first_sum` on) add up column sums.
+// as many threads take every so manieth share, and the first of them joins their sums.  The first blocks (`sum_blocks`, which take longest) add up column sums.
 template <typename TIN, typename TOUT>
 __global__ void __launch_bounds__(256) join_kernel(const float *__restrict__ partial, long long ld_partial, int splits, int groups, int M, int N,
                                                    const TIN *__restrict__ bias, const TOUT *residual, long long ld_res, TOUT *out, long long ld_out,
-                                                   TIN *pre, long long ld_pre, int act, const ColumnSums<TIN> columns, int first_sum)
+                                                   TIN *pre, long long ld_pre, int act, const ColumnSums<TIN> columns, int sum_blocks)
 {
     constexpr bool kFast = std::is_same<TOUT, bf16>::value;
     __shared__ float4 joined[8 * 33];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
-    if ((int)blockIdx.x >= first_sum) {
-        column_sums(columns, blockIdx.x - first_sum, reinterpret_cast<float (&)[8][33]>(joined));
+    const int block = (int)blockIdx.x - sum_blocks, blocks = (int)gridDim.x - sum_blocks;
+    if (block < 0) {
+        column_sums(columns, blockIdx.x, reinterpret_cast<float (&)[8][33]>(joined));
         return;
     }
     const int quads = (int)(ld_partial / 4), width = 256 / groups, group = threadIdx.x / width, t = threadIdx.x % width;
     const long long all = (long long)M * quads, step = (long long)M * ld_partial / 4;
-    for (long long i0 = (long long)blockIdx.x * width; i0 < all; i0 += (long long)first_sum * width) {
+    for (long long i0 = (long long)block * width; i0 < all; i0 += (long long)blocks * width) {
         const long long i = i0 + t, row = i / quads;
         const int col = (int)(i - row * quads) * 4;
         const float4 *src = reinterpret_cast<const float4 *>(partial) + row * (ld_partial / 4) + col / 4;
@@ -943,30 +944,32 @@ __global__ void __launch_bounds__(256) layout_kernel(const __grid_constant__ Lay
 
 constexpr int kSlopeRows = 8;  // warps of a block: each takes every eighth row of the block's
 
-// A lane has VEC neighbouring columns, a warp a stretch of a row, the block `per` rows; blocks behind those lay the other operands out.  dz, in bf16 numbers or three pieces `layer` apart, may be NULL
+// A lane has VEC neighbouring columns, a warp a stretch of a row, the block `per` rows.  dz, in bf16 numbers or three pieces `layer` apart, may be NULL
 // (column sums only), sums too.
 template <typename TG, typename TZ, int VEC>
 __global__ void __launch_bounds__(32 * kSlopeRows) slope_kernel(const TG *__restrict__ g, long long ld_g, const TZ *__restrict__ z, long long ld_z,
                                                                 bf16 *__restrict__ dz, long long ld_dz, long long layer, float *__restrict__ sums, int M,
-                                                                int N, int per, int act, unsigned across, unsigned blocks,
-                                                                const __grid_constant__ LayoutJobs jobs)
+                                                                int N, int per, int act, const __grid_constant__ LayoutJobs jobs)
 {
     constexpr bool kFast = std::is_same<TZ, bf16>::value;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
-    if (blockIdx.x >= blocks) {
-        jobs.run<TZ>(blockIdx.x - blocks);
-        return;
+    if constexpr (sizeof(TZ) == 4) {
+        const unsigned y = blockIdx.y - (unsigned)((M + per - 1) / per);
+        if ((int)y >= 0) {
+            if (y * gridDim.x + blockIdx.x < jobs.blocks) jobs.run<TZ>(y * gridDim.x + blockIdx.x);
+            return;
+        }
     }
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, chunk = blockIdx.x / across;
-    const int block = blockIdx.x - chunk * across, col = (block * 32 + lane) * VEC;
-    const long long row1 = min((long long)M, (long long)(chunk + 1) * per);
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int col = (blockIdx.x * 32 + lane) * VEC;
+    const long long row1 = min((long long)M, (long long)(blockIdx.y + 1) * per);
     float acc[VEC];
 #pragma unroll
     for (int j = 0; j < VEC; ++j) acc[j] = 0.0f;
     if (col < N)
 #pragma unroll 4
-        for (long long row = (long long)chunk * per + warp; row < row1; row += kSlopeRows) {
+        for (long long row = (long long)blockIdx.y * per + warp; row < row1; row += kSlopeRows) {
             TG gv[VEC];
             TZ zv[VEC];
             if constexpr (VEC > 1) {
@@ -1020,12 +1023,12 @@ __global__ void __launch_bounds__(32 * kSlopeRows) slope_kernel(const TG *__rest
     for (int j = 0; j < VEC; ++j) part[warp][lane * VEC + j] = acc[j];
     __syncthreads();
     for (int c = threadIdx.x; c < 32 * VEC; c += 32 * kSlopeRows) {
-        const int at = block * 32 * VEC + c;
+        const int at = blockIdx.x * 32 * VEC + c;
         if (at >= N) break;
         float v = 0.0f;
 #pragma unroll
         for (int w = 0; w < kSlopeRows; ++w) v += part[w][c];
-        sums[(long long)chunk * N + at] = v;
+        sums[(long long)blockIdx.y * N + at] = v;
     }
 }
 
@@ -1324,9 +1327,10 @@ cudaError_t launch_join(const Plan &q, const float *partial, int M, int N, const
     while (groups < 16 && groups * 2 <= q.splits && quads * groups < 1024LL * sm_count()) groups *= 2;
     const unsigned blocks = (unsigned)std::min<long long>((quads * groups + 255) / 256, 8LL * sm_count());
     const ColumnSums<TIN> columns = {e.sums, e.sum_rows, e.sum_columns, static_cast<TIN *>(e.sum_out)};
-    return launch_dependent(join_kernel<TIN, TOUT>, dim3(blocks + (e.sum_out ? (unsigned)(e.sum_columns + 31) / 32 : 0)), dim3(256), 0, stream, partial, q.ld_partial, q.splits, groups, M, N,
+    const unsigned sum_blocks = e.sum_out ? (unsigned)(e.sum_columns + 31) / 32 : 0;
+    return launch_dependent(join_kernel<TIN, TOUT>, dim3(sum_blocks + blocks), dim3(256), 0, stream, partial, q.ld_partial, q.splits, groups, M, N,
                             static_cast<const TIN *>(e.bias), static_cast<const TOUT *>(e.residual), e.ld_res, static_cast<TOUT *>(e.out), e.ld_out,
-                            static_cast<TIN *>(e.pre), e.ld_pre, e.act, columns, (int)blocks);
+                            static_cast<TIN *>(e.pre), e.ld_pre, e.act, columns, (int)sum_blocks);
 }
 
 // Enqueues one product; adds the kernels to `launches`.
@@ -1521,9 +1525,10 @@ cudaError_t launch_slope(const flashbev_linear_backward_params *p, const Backwar
     const long long ld_g = dense(p->ld_grad_out, N), ld_z = dense(p->ld_preact, N);
     const bool vec = N % 8 == 0 && vec_ok(p->grad_out, ld_g, sizeof(TG) == 4) && (!z || vec_ok(z, ld_z, sizeof(TZ) == 4));
     const int width = 32 * (vec ? 8 : 1);
-    const unsigned across = (unsigned)((N + width - 1) / width), blocks = across * (unsigned)q.chunks;
-    return launch_dependent(vec ? slope_kernel<TG, TZ, 8> : slope_kernel<TG, TZ, 1>, dim3(blocks + jobs.blocks), dim3(32 * kSlopeRows), 0, stream,
-                            static_cast<const TG *>(p->grad_out), ld_g, z, ld_z, dz, ld_dz, M * ld_dz, sums, M, N, q.per, p->act, across, blocks, jobs);
+    const unsigned across = (unsigned)((N + width - 1) / width);
+    const dim3 grid(across, (unsigned)q.chunks + (jobs.blocks + across - 1) / across);
+    return launch_dependent(vec ? slope_kernel<TG, TZ, 8> : slope_kernel<TG, TZ, 1>, grid, dim3(32 * kSlopeRows), 0, stream,
+                            static_cast<const TG *>(p->grad_out), ld_g, z, ld_z, dz, ld_dz, M * ld_dz, sums, M, N, q.per, p->act, jobs);
 }
 
 }  // namespace
@@ -1618,9 +1623,10 @@ flashbev_status flashbev_linear_backward(const flashbev_linear_backward_params *
     if (q.lay_w) layouts.add(w, ws + q.w_at, N, K, f32);
     if (q.need_dz || q.need_b) {
         if (f32) err = launch_slope<float, float>(p, q, layouts.jobs, stream);
-        else err = p->grad_dtype == FLASHBEV_F32 ? launch_slope<float, bf16>(p, q, layouts.jobs, stream) : launch_slope<bf16, bf16>(p, q, layouts.jobs, stream);
+        else err = p->grad_dtype == FLASHBEV_F32 ? launch_slope<float, bf16>(p, q, {}, stream) : launch_slope<bf16, bf16>(p, q, {}, stream);
         ++launches;
-    } else if (layouts.count) {
+    }
+    if (err == cudaSuccess && layouts.count && !(f32 && launches)) {
         err = layouts.launch(f32, stream);
         ++launches;
     }
