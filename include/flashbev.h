@@ -1,10 +1,11 @@
 /*
  * flashbev.h -- C ABI of the B200 (sm_100a) fused Sampling-VT library.
  *
- * One operator: the exact sampling-based BEV view transformation of the FlashBEV
- * paper, executed as a single fused gather-reduction (Sec. 3.3, Algorithm 2) so
- * that only the B x X x Y x C output is ever written and no height-dependent
- * intermediate exists.
+ * The exact sampling-based BEV view transformation of the FlashBEV paper, executed as a
+ * single fused gather-reduction (Sec. 3.3, Algorithm 2) so that only the B x X x Y x C
+ * output is ever written and no height-dependent intermediate exists; its relatives
+ * (backward, pyramid, spatial cross-attention); and the matrix products and norms of a
+ * transformer layer around the cross-attention.
  *
  * Plain C: pointers and sizes only.  Every pointer in `flashbev_vt_params` is a
  * DEVICE pointer unless the entry point says otherwise.  The caller owns every
@@ -333,10 +334,11 @@ typedef enum flashbev_act {
  * pieces each and the six products above 2^-24 of the whole are summed (a finite operand beyond 3.38e38 and
  * an infinite one give NaN there).  The result is reproducible bit for bit.
  *
- * Enqueues one kernel, or two where a long sum is shared by several thread blocks (see `workspace`).  rows = 0
- * is allowed and enqueues nothing.  `out` and `preact_out` may not overlap any input, but `out` may be
+ * Enqueues one kernel; one before it where operands have to be laid out in the scratch (float32 ones, bf16 ones that are
+ * not 16-byte aligned with strides of whole 16-byte vectors; not for up to eight rows), and one behind it where a long sum
+ * is shared by several thread blocks.  rows = 0 is allowed and enqueues nothing.  `out` and `preact_out` may not overlap any input, but `out` may be
  * `residual` itself (same address and stride).  All pointers element-aligned, else FLASHBEV_MISALIGNED; 16-byte
- * aligned addresses and strides of whole 16-byte vectors are the fast layout (TMA loads for bf16).  rows < 2^31
+ * aligned addresses and strides of whole 16-byte vectors are the fast layout.  rows < 2^31
  * and in_features, out_features <= 2^24, else FLASHBEV_UNSUPPORTED.
  */
 typedef struct flashbev_linear_params {
@@ -353,16 +355,17 @@ typedef struct flashbev_linear_params {
     int32_t dtype, out_dtype;  /* flashbev_dtype */
     int32_t act;               /* flashbev_act */
     int32_t reserved;          /* 0 */
-    void *workspace;           /* optional DEVICE scratch, 16-byte aligned: with flashbev_linear_workspace_bytes(p) bytes calls of few
-                                  rows and long sums are shared by more thread blocks.  Calls that may overlap on the GPU (two
-                                  streams, two graphs) need scratch of their own */
+    void *workspace;           /* DEVICE scratch, 16-byte aligned, flashbev_linear_workspace_bytes(p) bytes.  With less, long sums of
+                                  few rows are not shared by thread blocks (slower); with less than operands that have to be
+                                  laid out need, FLASHBEV_TOO_SMALL.  May be NULL where that is 0.  Calls that may overlap on the GPU
+                                  (two streams, two graphs) need scratch of their own */
     size_t workspace_bytes;
     uint32_t *error_word;      /* optional DEVICE word: counts thread blocks whose waits for their own loads or products did not end
                                   within seconds (the block gives up instead of hanging; its results are not valid) */
 } flashbev_linear_params;
 
 flashbev_status flashbev_linear(const flashbev_linear_params *p, void *stream);
-size_t flashbev_linear_workspace_bytes(const flashbev_linear_params *p); /* 0 if nothing is gained, or `p` is invalid */
+size_t flashbev_linear_workspace_bytes(const flashbev_linear_params *p); /* 0 if none is used, or `p` is invalid */
 
 /*
  * Gradients of flashbev_linear:
@@ -469,8 +472,8 @@ typedef struct flashbev_block_norm_backward_params {
 flashbev_status flashbev_block_norm_backward(const flashbev_block_norm_backward_params *p, void *stream);
 size_t flashbev_block_norm_backward_workspace_bytes(const flashbev_block_norm_backward_params *p);
 
-/* Number of kernels the last successful call of flashbev_sampling_vt[_host] on this thread
- * enqueued (always 1), and a short name of the kernel instance it chose (static storage). */
+/* Number of kernels the last successful call on this thread enqueued (1 of flashbev_sampling_vt with channels-last tensors of
+ * whole vectors), and a short name of the kernel instance it chose (static storage). */
 int flashbev_last_launch_count(void);
 const char *flashbev_last_kernel_name(void);
 

@@ -195,7 +195,7 @@ struct alignas(64) GemmParams {
     int M, N, K;
     int bn, stages;             // columns of a tile; stages in the ring
     int tiles_n, tiles, kblocks, kshare, splits;  // a tile's sum is cut into `splits` of `kshare` blocks of K (the last may have fewer)
-    int run;                    // blocks that are summed in tensor memory before the sum is taken on in registers; kshare or more: never
+    int run;                    // blocks after which the sum is added to the running one; kshare or more: never
     int columns;                // of tensor memory
     int accs;                   // accumulators in it
     int groups;                 // of epilogue warps, which take accumulators in turn
@@ -467,7 +467,8 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
     uint32_t &tmem_slot = *reinterpret_cast<uint32_t *>(bars + 2 * kMostStages + 2 * kAccs + 2);
     volatile int &failed = *reinterpret_cast<volatile int *>(&tmem_slot + 1);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const uint32_t full = smem_u32(bars), empty = full + 8 * kMostStages, acc_full = empty + 8 * kMostStages, acc_empty = acc_full + 8 * kAccs, last = acc_empty + 8 * kAccs, kept_full = last + 8;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * kMostStages, acc_full = empty + 8 * kMostStages, acc_empty = acc_full + 8 * kAccs,
+                   last = acc_empty + 8 * kAccs, kept_full = last + 8;
     // Tensor memory.  Two to four accumulators, so that some are taken out while another is filled.  The tensor cores cut a sum off, not round it, at
     // every instruction, by 3e-8 of the sum on the average.  So (1) pieces have a second accumulator for all products but p0 p0, which keeps the five
     // small products of each step from cutting at the large sum; (2) after `run` blocks the sum is added to a running one that stays in tensor
@@ -955,7 +956,7 @@ __global__ void __launch_bounds__(32 * kSlopeRows) slope_kernel(const TG *__rest
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     if constexpr (sizeof(TZ) == 4) {
-        const unsigned y = blockIdx.y - (unsigned)((M + per - 1) / per);
+        const unsigned y = blockIdx.y - ((unsigned)M + per - 1) / per;
         if ((int)y >= 0) {
             if (y * gridDim.x + blockIdx.x < jobs.blocks) jobs.run<TZ>(y * gridDim.x + blockIdx.x);
             return;
@@ -1226,10 +1227,11 @@ Plan plan_product(bool b_mn, bool f32, bool out_f32, bool heavy, int M, int N, i
     // B stays in shared memory where all of K fits beside three stages of A and a CTA has several tiles: its loads are two thirds of a 128 x 256
     // tile's.
     const long long tiles = (long long)q.tiles_m * q.tiles_n;
-    const int b_bytes = q.kblocks * q.bn * 2 * bk, a_bytes = kBM * 2 * bk, spread = sms / q.tiles_n * q.tiles_n;
+    const long long kept = (long long)q.kblocks * q.bn * 2 * bk;
+    const int a_bytes = kBM * 2 * bk, spread = sms / q.tiles_n * q.tiles_n;
     q.grid = (int)std::min<long long>(tiles * q.splits, sms);
-    if (!f32 && !heavy && q.splits == 1 && b_bytes + 3 * a_bytes <= ring_bytes(8) && tiles > spread && spread > 0 && spread * 20 >= sms * 19)
-        q.kept = b_bytes, q.grid = spread;
+    if (!f32 && !heavy && q.splits == 1 && kept + 3 * a_bytes <= ring_bytes(8) && tiles > spread && spread > 0 && spread * 20 >= sms * 19)
+        q.kept = (int)kept, q.grid = spread;
     q.ew = f32 || q.kept || q.kshare * bk > kShort ? 8 : 16;
     q.stages = std::min(8, (ring_bytes(q.ew) - q.kept) / (a_bytes + (q.kept ? 0 : q.bn * 2 * bk)));  // (of bf16 operands)
     q.run = runs && q.kshare > kRun / bk ? kRun / bk : q.kshare;
@@ -1503,7 +1505,7 @@ BackwardPlan plan_backward(const flashbev_linear_backward_params *p)
         const int across = std::max(1, (N + 255) / 256);
         const long long blocks = std::max(1, 4 * sm_count() / across);
         q.per = (int)std::max<long long>(32, (M + blocks - 1) / blocks);
-        q.chunks = (M + q.per - 1) / q.per;
+        q.chunks = (int)(((long long)M + q.per - 1) / q.per);
         if (q.need_b) q.sums_at = at, at += round_up((size_t)q.chunks * N * sizeof(float));
     }
     if (q.need_x) q.gx = plan_product(true, f32, f32, false, M, K, N, true);
