@@ -2,9 +2,10 @@
 // flashbev.h), and their gradients.
 //
 // All of a row is in the registers of a team of threads, eight elements each: every tensor is read once and written once, and the
-// two or three statistics of a row are sums over the team (shuffles; across warps through shared memory).  Bound by memory traffic.  A
-// team is the power of two of threads, from 4 to 1024, that holds the row, so that narrow rows share a warp; blocks stay and
-// walk over the rows with the parameters in registers, and the next row's loads are under way while one is worked on.
+// two or three statistics of a row are sums over the team (shuffles; across warps through shared memory).  The floor is memory
+// traffic.  A team is the power of two of threads, from 4 to 512, that holds the row, so that narrow rows share a warp; blocks stay
+// and walk over the rows with the parameters in shared memory and the gate in registers, and the next row's loads are under way, in
+// registers too, while one is worked on.  What each kernel measured stands at it.
 #include "flashbev.h"
 #include "launch.cuh"
 
@@ -268,6 +269,15 @@ struct Team {
             const int warps = threads / 32;
             if (t % 32 == 0) buf[t / 32] = make_float2(a, b);
             asm volatile("bar.sync %0, %1;" ::"r"(1 + slot), "r"(threads) : "memory");
+            if (warps <= 4) {  // (every thread adds them up: fewer instructions than a tree)
+                const float4 u = *reinterpret_cast<const float4 *>(buf);
+                a = u.x + u.z, b = u.y + u.w;
+                if (warps == 4) {
+                    const float4 w = *reinterpret_cast<const float4 *>(buf + 2);
+                    a += w.x + w.z, b += w.y + w.w;
+                }
+                return make_float2(a, b);
+            }
             const float2 v = t % 16 < warps ? buf[t % 16] : make_float2(0.0f, 0.0f);  // (both halves of a warp alike)
             a = v.x, b = v.y;
 #pragma unroll
@@ -287,6 +297,11 @@ struct Team {
             turn ^= 1;
             if (t % 32 == 0) buf[t / 32].x = a;
             asm volatile("bar.sync %0, %1;" ::"r"(1 + slot), "r"(threads) : "memory");
+            if (threads <= 128) {
+                a = buf[0].x + buf[1].x;
+                if (threads == 128) a += buf[2].x + buf[3].x;
+                return a;
+            }
             a = t % 16 < threads / 32 ? buf[t % 16].x : 0.0f;
 #pragma unroll
             for (int d = 8; d; d /= 2) a += __shfl_xor_sync(0xffffffffu, a, d);
@@ -299,11 +314,12 @@ struct Team {
 template <int VEC, bool WIDE>
 __device__ __forceinline__ void trim(Eight &v, const Team<WIDE> &team, int C)
 {
-    if (VEC == 8) return;
+    if constexpr (VEC != 8) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (!has<VEC>(2 * i, team.t, team.threads, C)) v.p[i].x = 0.0f;
-        if (!has<VEC>(2 * i + 1, team.t, team.threads, C)) v.p[i].y = 0.0f;
+        for (int i = 0; i < 4; ++i) {
+            if (!has<VEC>(2 * i, team.t, team.threads, C)) v.p[i].x = 0.0f;
+            if (!has<VEC>(2 * i + 1, team.t, team.threads, C)) v.p[i].y = 0.0f;
+        }
     }
 }
 
@@ -355,10 +371,15 @@ __device__ __forceinline__ T *row_of(const void *base, unsigned row, unsigned ld
 }
 
 // S, T, P: types of x and h, of y and n, of the parameters.
+//
+// Measured, 256 columns: 40000 bf16 rows, a norm ahead only, 18 us (4.4 TB/s); with x and h in float32 23 us (5.5 TB/s); 184950 bf16
+// rows 68 us (5.6 TB/s); 80000 bf16 rows, two norms and a gate, 33 us (4.9 TB/s, 59 % of the issue slots).  Bound by traffic and, close
+// behind, by the instructions of the conversions and shuffles: two-wide arithmetic (Eight) made the last 45 -> 34 us.  Rows of an odd C,
+// element by element, reach 0.9 TB/s.  A ring of asynchronous copies in place of the prefetch in registers was slower.
 template <typename S, typename T, typename P, int VEC, bool WIDE>
 __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 3) norm_kernel(const __grid_constant__ NormParams p)
 {
-    __shared__ float2 shared[WIDE ? 64 * 4 : 1];  // (at most four teams of 64 threads in a block)
+    __shared__ __align__(16) float2 shared[WIDE ? 64 * 4 : 1];  // (at most four teams of 64 threads in a block)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     Team<WIDE> team = make_team<VEC, WIDE>(p, shared);
@@ -408,12 +429,16 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 3) norm_
 }
 
 // Gradients.  The rows of a gate are shared by `chunks` blocks, whose teams take every so manieth row; sums over rows stay in
-// registers until the block's end, when they are added up over its teams in a fixed order.  `direct`: there are many gates with few rows, and a
-// team takes the rows of one gate after another and writes the gate's gradient itself.
+// registers until the block's end, when they are added up over its teams in a fixed order.  `direct`: there are many gates with few
+// rows, and a team takes the rows of one gate after another and writes the gate's gradient itself.
+//
+// Measured, 256 columns: 40000 bf16 rows, a norm ahead only, 37 us (3.3 TB/s); 184950 of them 119 us (4.7 TB/s); 80000 with two norms
+// and a gate 71 us (3.4 TB/s, 50 % of the issue slots); 14927 x 936, float32 stream, two norms: 113 us (1.7 TB/s).  Bound by latency:
+// five sums over rows beside this row and the next take 128 registers, which leaves 16 warps on an SM; in wide rows by the barriers too.
 template <typename S, typename T, typename P, int VEC, bool WIDE>
 __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 2) norm_backward_kernel(const __grid_constant__ NormParams p)
 {
-    __shared__ float2 shared[WIDE ? 64 * 4 : 1];
+    __shared__ __align__(16) float2 shared[WIDE ? 64 * 4 : 1];
     __shared__ float joined[2048];  // [teams (warps, where a warp has several)][C]
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
@@ -476,11 +501,34 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 2) norm_
                     u = fma(branch(), gate, u);
                     trim<VEC>(u, team, C);
                 }
-                const float rb = whiten<VEC, WIDE>(u, p.before, p, team);
-                if (live) dwb = fma(gn, u, dwb), dbb = dbb + gn;
-                gn = gn * read_param<VEC>(params, t, threads, C);
-                whiten_back<VEC, WIDE>(gn, u, rb, p.before, p, team);
-                gh = gh + gn;
+                if constexpr (WIDE) {
+                    // The sums over warps cost most: those of the statistics and of the gradient go together.  g (u - mean) gives g
+                    // t once the deviation is known, so that two sums over the team are enough, one for root mean squares, instead
+                    // of three and two (20000 x 512: 43 us instead of 47; narrow teams would be slower, 41 us instead of 33 at
+                    // 36743 x 82, by the instructions).
+                    float mean_g = 0.0f;
+                    if (p.before == FLASHBEV_NORM_LAYER) {
+                        const float2 s = team.sum(total(u), total(gn * read_param<VEC>(params, t, threads, C)));
+                        u = u + eight(-s.x * p.inv_c), mean_g = s.y * p.inv_c;
+                        trim<VEC>(u, team, C);
+                    }
+                    const float2 s = team.sum(total(u * u), total(gn * read_param<VEC>(params, t, threads, C) * u));
+                    const float rb = rsqrtf(fmaf(s.x, p.inv_c, p.eps));
+                    u = u * eight(rb);
+                    if (live) dwb = fma(gn, u, dwb), dbb = dbb + gn;
+                    gn = fma(u, eight(-s.y * rb * p.inv_c), gn * read_param<VEC>(params, t, threads, C));
+                    if (p.before == FLASHBEV_NORM_LAYER) {
+                        gn = gn + eight(-mean_g);
+                        trim<VEC>(gn, team, C);
+                    }
+                    gh = fma(gn, eight(rb), gh);
+                } else {
+                    const float rb = whiten<VEC, WIDE>(u, p.before, p, team);
+                    if (live) dwb = fma(gn, u, dwb), dbb = dbb + gn;
+                    gn = gn * read_param<VEC>(params, t, threads, C);
+                    whiten_back<VEC, WIDE>(gn, u, rb, p.before, p, team);
+                    gh = gh + gn;
+                }
             }
             if (p.gx && live) write<S, VEC>(row_of<S>(p.gx, row, p.ld_gx), gh, t, threads, C);
             if (!p.y) continue;
@@ -539,7 +587,7 @@ struct SumJobs {
     int blocks, per, C;         // partial rows of an array; those of one output row of the gate (job 4 sums every `per` of them)
 };
 
-// Adds the blocks' sums up in a fixed order: 16 warps take every sixteenth.
+// Adds the blocks' sums up in a fixed order: 16 warps take every sixteenth.  Bound by latency, 3 to 4 us for the sums of 296 blocks.
 template <typename P>
 __global__ void __launch_bounds__(512) norm_sum_kernel(const float *__restrict__ sums, const __grid_constant__ SumJobs q)
 {

@@ -10,9 +10,10 @@
 // tensor memory, and 8 or 16 warps take finished sums from there through bias, activation and residual to global memory.  In every tile,
 // operands are rows of bf16 numbers with the swizzle of TMA, whether a row runs along K or along M or N.
 //
-// Operands that TMA cannot read so -- float32 ones, which become three bf16 pieces, and bf16 ones whose rows are no whole 16-byte vectors
-// -- are laid out in the caller's scratch by a kernel ahead of the product.  (Sixteen warps that load, split and store the stages in the product itself
-// were bound by the latency of what they can have in flight: 40000 x 1024 x 256, float32: 172 us, tensor cores busy for 39 %.)
+// Operands that TMA cannot read so -- float32 ones, which become three bf16 pieces, and bf16 ones whose rows are no whole 16-byte
+// vectors -- are laid out in the caller's scratch by a kernel ahead of the product.  (Sixteen warps that load, split and store the
+// stages in the product itself were bound by the latency of what they can have in flight: 40000 x 1024 x 256, float32: 172 us,
+// tensor cores busy for 39 %.)
 #include "flashbev.h"
 #include "launch.cuh"
 #include "tcgen05.cuh"
@@ -83,10 +84,11 @@ __device__ __forceinline__ float max_nan(float a, float b)
 
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
-// Phi(-a) of the standard normal distribution for 0 <= a <= 14, to 3e-5 of itself up to a = 6 (bf16 rounds to 2e-3): log2 Phi(-a) is smooth,
-// and the polynomial below is its least-maximum fit of degree 8 over that range, the error weighted by 1 / (1 + 20 (a - 6)) behind 6 (reweighted least
-// squares).  Eight two-wide multiply-adds and one special function; erfc by rational forms takes two of those, and with them the epilogue of
-// 184950 x 256 numbers waits for the special function unit: 54 us against 36 without an activation, 45 so.
+// Phi(-a) of the standard normal distribution for 0 <= a <= 14, to 3e-5 of itself up to a = 6 (bf16 rounds to 2e-3): log2 Phi(-a)
+// is smooth, and the polynomial below is its least-maximum fit of degree 8 over that range, the error weighted by 1 / (1 + 20 (a -
+// 6)) behind 6 (reweighted least squares).  Eight two-wide multiply-adds and one special function; erfc by rational forms takes two
+// of those, and with them the epilogue of 184950 x 256 numbers waits for the special function unit: 54 us against 36 without an
+// activation, 45 so.
 __device__ __forceinline__ float2 normal_tail(float2 a)
 {
     float2 q = __ffma2_rn(a, both(3.97813622e-8f), both(-2.38079224e-6f));
@@ -179,9 +181,9 @@ constexpr int kBK = 64;             // K of a stage: a swizzled row of 128 bytes
 constexpr int kMostStages = 12;
 constexpr int kSlot = 16 * 1024;    // float32 operands: a tile of one piece
 
-// Warps of the epilogue (EW): 16 for short sums, as it is their latency that those wait for (64-column sums of 184950 rows, 64 columns:
-// 25 us with eight, 20 us with 16); eight for long ones, which leaves shared memory for a fourth stage of 48 KB, and for pieces (12 slots).  (Registers are
-// those of a quarter of an SM: the last warps of four, which do nothing, cost none.)
+// Warps of the epilogue (EW): 16 for short sums, as it is their latency that those wait for (64-column sums of 184950 rows, 64
+// columns: 25 us with eight, 20 us with 16); eight for long ones, which leaves shared memory for a fourth stage of 48 KB, and for
+// pieces (12 slots).  (Registers are those of a quarter of an SM: the last warps of four, which do nothing, cost none.)
 __host__ __device__ constexpr int gemm_threads(int ew) { return 32 * (ew + 4); }
 // Bytes behind the ring: a buffer of 32 rows x 128 bytes and a bias of 64 columns per epilogue warp.
 __host__ __device__ constexpr int epilogue_bytes(int ew) { return ew * (4096 + 256); }
@@ -222,8 +224,8 @@ constexpr int kPieces32 = 32 / kPiece<T>;    // pieces of a row; also the warp's
 template <typename T>
 constexpr int kRows32 = 32 / kPieces32<T>;   // rows of an access
 
-// Where a row's piece lies.  Rows of 128 bytes: float32 tiles, and bf16 ones that are half of a tile of 64 columns (`half` 0 or 1); rows of 64 bytes:
-// bf16 tiles by themselves (`half` -1).
+// Where a row's piece lies.  Rows of 128 bytes: float32 tiles, and bf16 ones that are half of a tile of 64 columns (`half` 0 or 1);
+// rows of 64 bytes: bf16 tiles by themselves (`half` -1).
 template <typename T>
 __device__ __forceinline__ int piece_at(int row, int piece, int half)
 {
@@ -292,9 +294,9 @@ __device__ __forceinline__ void row_add(float (&v)[32], const unsigned char *til
     }
 }
 
-// The lane's row through the activation.  Without the short formulas a number takes about 40 instructions; 32 of them in a row are more code than the
-// instruction cache brings in the time of a call (1846 x 72 x 846, GELU: 20 us against 17), so the row goes through the warp's buffer, four
-// numbers at a time.
+// The lane's row through the activation.  Without the short formulas a number takes about 40 instructions; 32 of them in a row are
+// more code than the instruction cache brings in the time of a call (1846 x 72 x 846, GELU: 20 us against 17), so the row goes
+// through the warp's buffer, four numbers at a time.
 template <bool FAST>
 __device__ __forceinline__ void activate_row(float (&v)[32], int act, unsigned char *buffer, int lane)
 {
@@ -318,8 +320,9 @@ __device__ __forceinline__ void activate_row(float (&v)[32], int act, unsigned c
     __syncwarp();
 }
 
-// A tile from a matrix to registers, and from there to shared memory.  vec: bytes that every row's start is a multiple of.  16: pieces.  Less: a lane has
-// a column, or of bf16 rows on 4-byte boundaries two, so that the warp touches every sector of a row once.
+// A tile from a matrix to registers, and from there to shared memory.  vec: bytes that every row's start is a multiple of.  16:
+// pieces.  Less: a lane has a column, or of bf16 rows on 4-byte boundaries two, so that the warp touches every sector of a row
+// once.
 template <typename T>
 __device__ __forceinline__ void tile_load(uint4 (&r)[kPieces32<T>], const T *base, long long ld, int vec, int row0, int col0, int M, int N, int lane)
 {
@@ -431,11 +434,11 @@ struct Shares {
     }
 };
 
-// float32 operands: every tile of a piece has a slot of shared memory and barriers of its own, twelve in all, six of one block and six of
-// the next.  A block's tiles come in the order below, and are released, from the first product that is their last on, in the order of
-// `released`; the tiles of the block after the next take the slots in that order, so that they are on their way while the last two sixths of this
-// block's products and all of the next one's run.  (40000 x 256 x 256: 31 us, of which the loads by themselves take 17 and loads and products 25;
-// stages of 32 of K in a ring of four, their rows of 64 bytes, 36.)
+// float32 operands: every tile of a piece has a slot of shared memory and barriers of its own, twelve in all, six of one block and
+// six of the next.  A block's tiles come in the order below, and are released, from the first product that is their last on, in the
+// order of `released`; the tiles of the block after the next take the slots in that order, so that they are on their way while the
+// last two sixths of this block's products and all of the next one's run.  (40000 x 256 x 256: 31 us, of which the loads by
+// themselves take 17 and loads and products 25; stages of 32 of K in a ring of four, their rows of 64 bytes, 36.)
 enum PieceTile { kA0 = 0, kB0 = 1, kB1 = 2, kA1 = 3, kB2 = 4, kA2 = 5 };
 
 struct Slots {
@@ -451,8 +454,14 @@ struct Slots {
     }
 };
 
-// MODE: an activation, for results of unshared sums that leave by TMA, or kAny: everything as the parameters say.  What an instance does not need would be in its
-// way: the code of the other activations and of rows of any alignment, skipped, cost 8 of 37 us (184950 x 64 x 256) in instruction fetches.
+// MODE: an activation, for results of unshared sums that leave by TMA, or kAny: everything as the parameters say.  What an instance
+// does not need would be in its way: the code of the other activations and of rows of any alignment, skipped, cost 8 of 37 us
+// (184950 x 64 x 256) in instruction fetches.
+//
+// Measured: 8192 x 4096 x 4096, bf16, SiLU: 185 us by itself, the tensor cores busy for 85 % (237 us and 1.16 PFLOP/s in a long
+// run, where the power limit holds the clock down); 184950 x 256 x 256: 34 to 39 us, 4.8 TB/s, bound by what is read and written;
+// with 1024 columns, GELU and its argument kept, 40000 rows: 46 to 51 us, bound by the epilogue's instructions (59 % of the issue
+// slots); float32 40000 x 256 x 256: 36 us, bound by the tensor cores (54 %) and the loads in turn.
 constexpr int kAny = 4;
 
 template <int kPieces, typename TOUT, int kEpilogue, int MODE>
@@ -469,10 +478,11 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t full = smem_u32(bars), empty = full + 8 * kMostStages, acc_full = empty + 8 * kMostStages, acc_empty = acc_full + 8 * kAccs,
                    last = acc_empty + 8 * kAccs, kept_full = last + 8;
-    // Tensor memory.  Two to four accumulators, so that some are taken out while another is filled.  The tensor cores cut a sum off, not round it, at
-    // every instruction, by 3e-8 of the sum on the average.  So (1) pieces have a second accumulator for all products but p0 p0, which keeps the five
-    // small products of each step from cutting at the large sum; (2) after `run` blocks the sum is added to a running one that stays in tensor
-    // memory too, behind the accumulators, and so does the small products' then.
+    // Tensor memory.  Two to four accumulators, so that some are taken out while another is filled.  The tensor cores cut a sum
+    // off, not round it, at every instruction, by 3e-8 of the sum on the average.  So (1) pieces have a second accumulator for all
+    // products but p0 p0, which keeps the five small products of each step from cutting at the large sum; (2) after `run` blocks
+    // the sum is added to a running one that stays in tensor memory too, behind the accumulators, and so does the small products'
+    // then.
     constexpr int kParts = kPieces == 3 ? 2 : 1;
     const bool runs = MODE == kAny && p.run < p.kshare;  // (float32 results)
     const int acc_step = runs ? p.bn : kParts * p.bn, sum_at = 2 * p.bn;  // (with runs there are two accumulators)
@@ -593,7 +603,8 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
                         }
                         if (p.pre ? sizeof(TIN) == 4 || sizeof(TOUT) == 4 : odd && sizeof(TOUT) == 4) stores_done();
                         activate_row<std::is_same<TOUT, bf16>::value>(v, MODE == kAny ? p.act : MODE, buffer, lane);
-                        // (a bf16 result without z: both halves leave at once, in rows of 128 bytes, where no other CTA has the second half's columns)
+                        // (a bf16 result without z: both halves leave at once, in rows of 128 bytes, where no other CTA has the
+                        // second half's columns)
                         const int half = p.wide ? odd : -1;
                         unsigned char *const tile = buffer + (sizeof(TOUT) == 2 && odd && !p.pre && !p.wide ? 2048 : 0);
                         if (p.residual) {
@@ -792,8 +803,9 @@ __global__ void __launch_bounds__(256) column_sum_kernel(const ColumnSums<T> q)
     column_sums(q, blockIdx.x, part);
 }
 
-// Adds the shares up in a fixed order and does what the epilogue would have done.  Four columns of a row per thread; with few of them (`groups` > 1)
-// as many threads take every so manieth share, and the first of them joins their sums.  The first blocks (`sum_blocks`, which take longest) add up column sums.
+// Adds the shares up in a fixed order and does what the epilogue would have done.  Four columns of a row per thread; with few of
+// them (`groups` > 1) as many threads take every so manieth share, and the first of them joins their sums.  The first blocks
+// (`sum_blocks`, which take longest) add up column sums.  Bound by latency: 9 us for 19 MB of a 1024 x 256 gradient's shares.
 template <typename TIN, typename TOUT>
 __global__ void __launch_bounds__(256) join_kernel(const float *__restrict__ partial, long long ld_partial, int splits, int groups, int M, int N,
                                                    const TIN *__restrict__ bias, const TOUT *residual, long long ld_res, TOUT *out, long long ld_out,
@@ -920,7 +932,7 @@ __device__ __forceinline__ void lay_out(const LayoutJob &q, unsigned block, unsi
     }
 }
 
-// Two jobs, x and the weights: whole blocks of either.
+// Two jobs, x and the weights: whole blocks of either.  Bound by traffic: 15 us for 40000 x 256 float32 numbers and their pieces (102 MB).
 struct LayoutJobs {
     LayoutJob first, second;
     unsigned first_blocks, blocks;  // 0: none
@@ -945,8 +957,9 @@ __global__ void __launch_bounds__(256) layout_kernel(const __grid_constant__ Lay
 
 constexpr int kSlopeRows = 8;  // warps of a block: each takes every eighth row of the block's
 
-// A lane has VEC neighbouring columns, a warp a stretch of a row, the block `per` rows.  dz, in bf16 numbers or three pieces `layer` apart, may be NULL
-// (column sums only), sums too.
+// A lane has VEC neighbouring columns, a warp a stretch of a row, the block `per` rows.  dz, in bf16 numbers or three pieces
+// `layer` apart, may be NULL (column sums only), sums too.  One pass over g and z, bound by traffic: 43 us for the 246 MB of 40000 x 1024
+// bf16 numbers and GELU (5.7 TB/s; 55 % of the issue slots).
 template <typename TG, typename TZ, int VEC>
 __global__ void __launch_bounds__(32 * kSlopeRows) slope_kernel(const TG *__restrict__ g, long long ld_g, const TZ *__restrict__ z, long long ld_z,
                                                                 bf16 *__restrict__ dz, long long ld_dz, long long layer, float *__restrict__ sums, int M,
@@ -1038,6 +1051,7 @@ __global__ void __launch_bounds__(32 * kSlopeRows) slope_kernel(const TG *__rest
 // Up to R rows of x: bound by reading the weights once, so no tensor cores (their tiles would be empty rows).  A warp forms NC
 // neighbouring columns of all rows, its lanes 8 elements of the sum each at a time.  Where that leaves most SMs without a warp, the block's
 // eight warps share the sum of the same columns (`shared`).  VEC: bytes that every row's start is a multiple of, 16 or an element.
+// Measured: 1 x 1024 -> 4096, bf16: 5 us a call, of which launch and latency are most (the weights' 8 MB take 1.3 us at the card's rate).
 template <typename TIN, typename TOUT, int R, int NC, bool VEC>
 __global__ void __launch_bounds__(256) rows_kernel(const TIN *__restrict__ x, long long ld_x, const TIN *__restrict__ weight, long long ld_w, int M,
                                                    int N, int K, int shared, const TIN *__restrict__ bias, const TOUT *residual, long long ld_res,
@@ -1206,10 +1220,11 @@ Plan plan_product(bool b_mn, bool f32, bool out_f32, bool heavy, int M, int N, i
     constexpr int bk = kBK;
     q.kblocks = (K + bk - 1) / bk;
     const bool runs = out_f32 && K > kRun;
-    // Widths: the columns in equal parts, at most 256 (128 where accumulators for pieces or a running sum take tensor memory); and shares of
-    // long sums where there are few tiles.  By estimated cycles of the CTA with the most to do: a block of K as measured (8192 x 4096 x 4096 with 256
-    // columns, 40000 x 1024 x 256 with 128; pieces 40000 x 256 x 256), a tile's epilogue 12 cycles a column and 800 more, beside the products of the next
-    // tile if there is one; partial sums are written and read again by another kernel, all CTAs together at 2000 bytes a cycle.
+    // Widths: the columns in equal parts, at most 256 (128 where accumulators for pieces or a running sum take tensor memory); and
+    // shares of long sums where there are few tiles.  By estimated cycles of the CTA with the most to do: a block of K as measured
+    // (8192 x 4096 x 4096 with 256 columns, 40000 x 1024 x 256 with 128; pieces 40000 x 256 x 256), a tile's epilogue 12 cycles a
+    // column and 800 more, beside the products of the next tile if there is one; partial sums are written and read again by another
+    // kernel, all CTAs together at 2000 bytes a cycle.
     const int widest = f32 || runs ? 128 : 256;
     double best = 0.0;
     for (int t = (N + widest - 1) / widest; t <= (N + 63) / 64; ++t) {
@@ -1224,8 +1239,8 @@ Plan plan_product(bool b_mn, bool f32, bool out_f32, bool heavy, int M, int N, i
         if (t > 64) break;  // (wide results: the widest tiles)
     }
     q.tiles_n = (N + q.bn - 1) / q.bn;
-    // B stays in shared memory where all of K fits beside three stages of A and a CTA has several tiles: its loads are two thirds of a 128 x 256
-    // tile's.
+    // B stays in shared memory where all of K fits beside three stages of A and a CTA has several tiles: its loads are two thirds
+    // of a 128 x 256 tile's.
     const long long tiles = (long long)q.tiles_m * q.tiles_n;
     const long long kept = (long long)q.kblocks * q.bn * 2 * bk;
     const int a_bytes = kBM * 2 * bk, spread = sms / q.tiles_n * q.tiles_n;

@@ -10,9 +10,9 @@ namespace flashbev_sm100 {
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-// One thread of the warp, always the same.  The instructions of TMA and tcgen05 take their operands from uniform registers; behind this the
-// compiler knows that one thread runs, behind `lane == 0` it does not, and a product costs 146 cycles to issue whatever its size (M = 128, K = 16; 66,
-// 74 and 129 with 64, 128 and 256 columns so).
+// One thread of the warp, always the same.  The instructions of TMA and tcgen05 take their operands from uniform registers; behind
+// this the compiler knows that one thread runs, behind `lane == 0` it does not, and a product costs 146 cycles to issue whatever
+// its size (M = 128, K = 16; 66, 74 and 129 with 64, 128 and 256 columns so).
 __device__ __forceinline__ bool elect_one()
 {
     uint32_t one;
