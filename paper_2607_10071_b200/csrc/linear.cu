@@ -768,7 +768,8 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
 
 // ---- sums that several CTAs shared ----------------------------------------------------------------------------------------
 
-// Column sums of partial sums, `rows` rows of N: 32 columns per block of eight warps, which take every eighth row.
+// Column sums of partial sums, `rows` rows of N: 8 columns per block, whose threads have 32 rows of them at a time.
+constexpr int kSumColumns = 8;
 template <typename T>
 struct ColumnSums {
     const float *sums;
@@ -777,16 +778,18 @@ struct ColumnSums {
 };
 
 template <typename T>
-__device__ __forceinline__ void column_sums(const ColumnSums<T> &q, int block, float (&part)[8][33])
+__device__ __forceinline__ void column_sums(const ColumnSums<T> &q, int block, float (&part)[8][kSumColumns])
 {
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, col = block * 32 + lane;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, col = block * kSumColumns + lane % 8;
     float v = 0.0f;
     if (col < q.N)
-#pragma unroll 32
-        for (int r = warp; r < q.rows; r += 8) v += q.sums[(long long)r * q.N + col];
-    part[warp][lane] = v;
+#pragma unroll 20
+        for (int r = threadIdx.x / 8; r < q.rows; r += 32) v += q.sums[(long long)r * q.N + col];
+    v += __shfl_xor_sync(0xffffffffu, v, 8);
+    v += __shfl_xor_sync(0xffffffffu, v, 16);
+    if (lane < 8) part[warp][lane] = v;
     __syncthreads();
-    if (warp == 0 && col < q.N) {
+    if (threadIdx.x < 8 && col < q.N) {
         v = 0.0f;
 #pragma unroll
         for (int w = 0; w < 8; ++w) v += part[w][lane];
@@ -797,7 +800,7 @@ __device__ __forceinline__ void column_sums(const ColumnSums<T> &q, int block, f
 template <typename T>
 __global__ void __launch_bounds__(256) column_sum_kernel(const ColumnSums<T> q)
 {
-    __shared__ float part[8][33];
+    __shared__ float part[8][kSumColumns];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     column_sums(q, blockIdx.x, part);
@@ -817,7 +820,7 @@ __global__ void __launch_bounds__(256) join_kernel(const float *__restrict__ par
     asm volatile("griddepcontrol.launch_dependents;");
     const int block = (int)blockIdx.x - sum_blocks, blocks = (int)gridDim.x - sum_blocks;
     if (block < 0) {
-        column_sums(columns, blockIdx.x, reinterpret_cast<float (&)[8][33]>(joined));
+        column_sums(columns, blockIdx.x, reinterpret_cast<float (&)[8][kSumColumns]>(joined));
         return;
     }
     const int quads = (int)(ld_partial / 4), width = 256 / groups, group = threadIdx.x / width, t = threadIdx.x % width;
@@ -957,11 +960,30 @@ __global__ void __launch_bounds__(256) layout_kernel(const __grid_constant__ Lay
 
 constexpr int kSlopeRows = 8;  // warps of a block: each takes every eighth row of the block's
 
+// VEC neighbours, aligned as a whole; `once`: nobody else reads them.
+template <typename T, int VEC>
+struct Loaded {
+    using W = typename std::conditional<VEC * sizeof(T) >= 16, uint4,
+                                        typename std::conditional<VEC * sizeof(T) == 8, uint2,
+                                                                  typename std::conditional<VEC * sizeof(T) == 4, uint32_t, uint16_t>::type>::type>::type;
+    W w[VEC * sizeof(T) / sizeof(W)];
+};
+
+template <typename T, int VEC>
+__device__ __forceinline__ void load(Loaded<T, VEC> &to, const T *from, bool once)
+{
+    using W = typename Loaded<T, VEC>::W;
+    const W *const p = reinterpret_cast<const W *>(from);
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(to) / sizeof(W)); ++i) to.w[i] = once ? __ldcs(p + i) : __ldg(p + i);
+}
+
 // A lane has VEC neighbouring columns, a warp a stretch of a row, the block `per` rows.  dz, in bf16 numbers or three pieces
-// `layer` apart, may be NULL (column sums only), sums too.  One pass over g and z, bound by traffic: 43 us for the 246 MB of 40000 x 1024
-// bf16 numbers and GELU (5.7 TB/s; 55 % of the issue slots).
+// `layer` apart, may be NULL (column sums only), sums too.  One pass over g and z, bound by traffic: about 43 us for the 246 MB of
+// 40000 x 1024 bf16 numbers and GELU (5.7 TB/s).  Batches of rows whose loads are all under way, and few blocks for them, take 10 us
+// for sums of 40000 x 256 and the kernel that joins them, 14 by a loop of one row at a time.
 template <typename TG, typename TZ, int VEC>
-__global__ void __launch_bounds__(32 * kSlopeRows) slope_kernel(const TG *__restrict__ g, long long ld_g, const TZ *__restrict__ z, long long ld_z,
+__global__ void __launch_bounds__(32 * kSlopeRows, VEC == 8 && sizeof(TZ) == 2 ? 2 : 3) slope_kernel(const TG *__restrict__ g, long long ld_g, const TZ *__restrict__ z, long long ld_z,
                                                                 bf16 *__restrict__ dz, long long ld_dz, long long layer, float *__restrict__ sums, int M,
                                                                 int N, int per, int act, const __grid_constant__ LayoutJobs jobs)
 {
@@ -981,53 +1003,59 @@ __global__ void __launch_bounds__(32 * kSlopeRows) slope_kernel(const TG *__rest
     float acc[VEC];
 #pragma unroll
     for (int j = 0; j < VEC; ++j) acc[j] = 0.0f;
+    // (all loads of a batch of rows ahead of their arithmetic, the last batch's too)
+    constexpr int kBatch = VEC == 8 && sizeof(TZ) == 4 ? 2 : 4;
     if (col < N)
-#pragma unroll 4
-        for (long long row = (long long)blockIdx.y * per + warp; row < row1; row += kSlopeRows) {
-            TG gv[VEC];
-            TZ zv[VEC];
-            if constexpr (VEC > 1) {
-                constexpr int GQ = VEC * (int)sizeof(TG) / 16, ZQ = VEC * (int)sizeof(TZ) / 16;
-                uint4 q[GQ > ZQ ? GQ : ZQ];
+        for (long long first = (long long)blockIdx.y * per + warp; first < row1; first += kBatch * kSlopeRows) {
+            Loaded<TG, VEC> gq[kBatch];
+            Loaded<TZ, VEC> zq[kBatch];
 #pragma unroll
-                for (int i = 0; i < GQ; ++i) q[i] = __ldcs(reinterpret_cast<const uint4 *>(g + row * ld_g + col) + i);
-                memcpy(gv, q, sizeof(gv));
-                if (z) {
-#pragma unroll
-                    for (int i = 0; i < ZQ; ++i) q[i] = __ldcs(reinterpret_cast<const uint4 *>(z + row * ld_z + col) + i);
-                    memcpy(zv, q, sizeof(zv));
-                }
-            } else {
-                gv[0] = g[row * ld_g + col];
-                if (z) zv[0] = z[row * ld_z + col];
+            for (int k = 0; k < kBatch; ++k) {
+                const long long row = first + k * kSlopeRows;
+                if (row >= row1) break;
+                load(gq[k], g + row * ld_g + col, dz != nullptr);  // (without dz the products read it too)
+                if (z) load(zq[k], z + row * ld_z + col, true);
             }
-            float d[VEC];
-            if constexpr (VEC == 1) {
-                d[0] = z ? slope_times<kFast>(both(to_float(gv[0])), both(to_float(zv[0])), act).x : to_float(gv[0]);
-                acc[0] += d[0];
-            } else {
 #pragma unroll
-                for (int j = 0; j < VEC; j += 2) {
-                    float2 v = make_float2(to_float(gv[j]), to_float(gv[j + 1]));
-                    if (z) v = slope_times<kFast>(v, make_float2(to_float(zv[j]), to_float(zv[j + 1])), act);
-                    d[j] = v.x, d[j + 1] = v.y;
-                    v = __fadd2_rn(v, make_float2(acc[j], acc[j + 1]));
-                    acc[j] = v.x, acc[j + 1] = v.y;
-                }
-            }
-            if (dz) {
-                bf16 *const to = dz + row * ld_dz + col;
-                if constexpr (VEC == 8 && sizeof(TZ) == 4) {
-                    store_pieces(d, to, layer);
-                } else if constexpr (VEC == 8) {
-                    *reinterpret_cast<uint4 *>(to) = make_uint4(pack(d[0], d[1]), pack(d[2], d[3]), pack(d[4], d[5]), pack(d[6], d[7]));
-                } else if constexpr (sizeof(TZ) == 4) {
-                    uint32_t p[3];
-                    split(make_float2(d[0], 0.0f), p);
-#pragma unroll
-                    for (int j = 0; j < 3; ++j) to[j * layer] = __ushort_as_bfloat16((unsigned short)p[j]);
+            for (int k = 0; k < kBatch; ++k) {
+                const long long row = first + k * kSlopeRows;
+                if (row >= row1) break;
+                TG gv[VEC];
+                TZ zv[VEC];
+                memcpy(gv, &gq[k], sizeof(gv));
+                memcpy(zv, &zq[k], sizeof(zv));
+                float d[VEC];
+                if constexpr (VEC == 1) {
+                    d[0] = z ? slope_times<kFast>(both(to_float(gv[0])), both(to_float(zv[0])), act).x : to_float(gv[0]);
+                    acc[0] += d[0];
                 } else {
-                    *to = from_float<bf16>(d[0]);
+#pragma unroll
+                    for (int j = 0; j < VEC; j += 2) {
+                        float2 v = make_float2(to_float(gv[j]), to_float(gv[j + 1]));
+                        if (z) v = slope_times<kFast>(v, make_float2(to_float(zv[j]), to_float(zv[j + 1])), act);
+                        d[j] = v.x, d[j + 1] = v.y;
+                        v = __fadd2_rn(v, make_float2(acc[j], acc[j + 1]));
+                        acc[j] = v.x, acc[j + 1] = v.y;
+                    }
+                }
+                if (dz) {
+                    bf16 *const to = dz + row * ld_dz + col;
+                    if constexpr (VEC == 8 && sizeof(TZ) == 4) {
+                        store_pieces(d, to, layer);
+                    } else if constexpr (VEC == 8) {
+                        *reinterpret_cast<uint4 *>(to) = make_uint4(pack(d[0], d[1]), pack(d[2], d[3]), pack(d[4], d[5]), pack(d[6], d[7]));
+                    } else if constexpr (sizeof(TZ) == 4) {
+                        uint32_t p[3];
+                        split(make_float2(d[0], VEC > 1 ? d[VEC - 1] : 0.0f), p);
+#pragma unroll
+                        for (int j = 0; j < 3; ++j)
+                            if constexpr (VEC == 2) *reinterpret_cast<uint32_t *>(to + j * layer) = p[j];
+                            else to[j * layer] = __ushort_as_bfloat16((unsigned short)p[j]);
+                    } else if constexpr (VEC == 2) {
+                        *reinterpret_cast<uint32_t *>(to) = pack(d[0], d[1]);
+                    } else {
+                        *to = from_float<bf16>(d[0]);
+                    }
                 }
             }
         }
@@ -1347,7 +1375,7 @@ cudaError_t launch_join(const Plan &q, const float *partial, int M, int N, const
     while (groups < 16 && groups * 2 <= q.splits && quads * groups < 1024LL * sm_count()) groups *= 2;
     const unsigned blocks = (unsigned)std::min<long long>((quads * groups + 255) / 256, 8LL * sm_count());
     const ColumnSums<TIN> columns = {e.sums, e.sum_rows, e.sum_columns, static_cast<TIN *>(e.sum_out)};
-    const unsigned sum_blocks = e.sum_out ? (unsigned)(e.sum_columns + 31) / 32 : 0;
+    const unsigned sum_blocks = e.sum_out ? (unsigned)(e.sum_columns + kSumColumns - 1) / kSumColumns : 0;
     return launch_dependent(join_kernel<TIN, TOUT>, dim3(sum_blocks + blocks), dim3(256), 0, stream, partial, q.ld_partial, q.splits, groups, M, N,
                             static_cast<const TIN *>(e.bias), static_cast<const TOUT *>(e.residual), e.ld_res, static_cast<TOUT *>(e.out), e.ld_out,
                             static_cast<TIN *>(e.pre), e.ld_pre, e.act, columns, (int)sum_blocks);
@@ -1519,9 +1547,9 @@ BackwardPlan plan_backward(const flashbev_linear_backward_params *p)
     if (q.lay_x) q.x_at = at, at += laid_out_bytes(M, K, f32);
     if (q.lay_w) q.w_at = at, at += laid_out_bytes(N, K, f32);
     if (q.need_dz || q.need_b) {
-        // about four blocks per SM (two where only sums are wanted), but no fewer than 32 rows for each
+        // as many blocks as the SMs hold of slope_kernel's widest instance, but no fewer than 32 rows for each
         const int across = std::max(1, (N + 255) / 256);
-        const long long blocks = std::max(1, 4 * sm_count() / across);
+        const long long blocks = std::max(1, (f32 ? 3 : 2) * sm_count() / across);
         q.per = (int)std::max<long long>(32, (M + blocks - 1) / blocks);
         q.chunks = (int)(((long long)M + q.per - 1) / q.per);
         if (q.need_b) q.sums_at = at, at += round_up((size_t)q.chunks * N * sizeof(float));
@@ -1543,11 +1571,16 @@ cudaError_t launch_slope(const flashbev_linear_backward_params *p, const Backwar
     float *const sums = q.need_b ? reinterpret_cast<float *>(ws + q.sums_at) : nullptr;
     const TZ *const z = p->act == FLASHBEV_ACT_NONE ? nullptr : static_cast<const TZ *>(p->preact);
     const long long ld_g = dense(p->ld_grad_out, N), ld_z = dense(p->ld_preact, N);
-    const bool vec = N % 8 == 0 && vec_ok(p->grad_out, ld_g, sizeof(TG) == 4) && (!z || vec_ok(z, ld_z, sizeof(TZ) == 4));
-    const int width = 32 * (vec ? 8 : 1);
+    // (dz's rows start on 16-byte boundaries)
+    const auto starts_on = [&](int numbers) {
+        return N % numbers == 0 && ((uintptr_t)p->grad_out | (uintptr_t)(ld_g * (long long)sizeof(TG))) % (numbers == 8 ? 16 : numbers * sizeof(TG)) == 0 &&
+               (!z || ((uintptr_t)z | (uintptr_t)(ld_z * (long long)sizeof(TZ))) % (numbers == 8 ? 16 : numbers * sizeof(TZ)) == 0);
+    };
+    const int vec = starts_on(8) ? 8 : (starts_on(2) ? 2 : 1), width = 32 * vec;
+    const auto kernel = vec == 8 ? slope_kernel<TG, TZ, 8> : (vec == 2 ? slope_kernel<TG, TZ, 2> : slope_kernel<TG, TZ, 1>);
     const unsigned across = (unsigned)((N + width - 1) / width);
     const dim3 grid(across, (unsigned)q.chunks + (jobs.blocks + across - 1) / across);
-    return launch_dependent(vec ? slope_kernel<TG, TZ, 8> : slope_kernel<TG, TZ, 1>, grid, dim3(32 * kSlopeRows), 0, stream,
+    return launch_dependent(kernel, grid, dim3(32 * kSlopeRows), 0, stream,
                             static_cast<const TG *>(p->grad_out), ld_g, z, ld_z, dz, ld_dz, M * ld_dz, sums, M, N, q.per, p->act, jobs);
 }
 
@@ -1660,7 +1693,7 @@ flashbev_status flashbev_linear_backward(const flashbev_linear_backward_params *
     const float *const sums = reinterpret_cast<const float *>(ws + q.sums_at);
     const bool joins = q.need_w && q.gw.splits > 1;  // the bias' gradient from the kernel that joins the weights'
     if (q.need_b && !joins) {
-        const dim3 grid((unsigned)((N + 31) / 32));
+        const dim3 grid((unsigned)((N + kSumColumns - 1) / kSumColumns));
         if (f32) err = launch_dependent(column_sum_kernel<float>, grid, dim3(256), 0, stream, ColumnSums<float>{sums, q.chunks, N, static_cast<float *>(p->grad_bias)});
         else err = launch_dependent(column_sum_kernel<bf16>, grid, dim3(256), 0, stream, ColumnSums<bf16>{sums, q.chunks, N, static_cast<bf16 *>(p->grad_bias)});
         ++launches;
