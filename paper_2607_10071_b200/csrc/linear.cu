@@ -893,11 +893,12 @@ struct LayoutJob {
     bf16 *to;               // [pieces][rows][ld_to]
     long long ld, ld_to, layer;
     int rows, width;        // width 0: no job
-    int vec;                // 16-byte loads are allowed
-    unsigned lanes;         // threads of a row: one for eight elements, or for two
+    int vec;                // neighbours that a load may take at once: 8 (all of the row is in such eights), 2 or 1
+    unsigned lanes;         // threads of a row: one for eight elements
 };
 
-// Rows of whole vectors: a thread has eight elements; others: two, so that a warp touches each sector once.
+// A thread has eight elements of a row at a time and stores them as whole vectors, with zeros behind the row's end.  (184950 x 82 bf16
+// numbers, rows on 4-byte boundaries, and their product with 82 x 128: 34 us; with two elements for a thread 41.)
 template <typename T>
 __device__ __forceinline__ void lay_out(const LayoutJob &q, unsigned block, unsigned blocks)
 {
@@ -910,8 +911,8 @@ __device__ __forceinline__ void lay_out(const LayoutJob &q, unsigned block, unsi
     for (; row < (unsigned)q.rows; row += step_rows, lane += step_lanes, row += lane >= q.lanes, lane -= lane >= q.lanes ? q.lanes : 0) {
         const T *src = static_cast<const T *>(q.from) + row * q.ld;
         bf16 *dst = q.to + row * q.ld_to;
-        if (q.vec) {
-            src += 8 * lane, dst += 8 * lane;
+        src += 8 * lane, dst += 8 * lane;
+        if (q.vec == 8) {
             if constexpr (kP == 3) {
                 const uint4 a = __ldcs(reinterpret_cast<const uint4 *>(src)), b = __ldcs(reinterpret_cast<const uint4 *>(src) + 1);
                 const float v[8] = {__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
@@ -921,15 +922,24 @@ __device__ __forceinline__ void lay_out(const LayoutJob &q, unsigned block, unsi
                 *reinterpret_cast<uint4 *>(dst) = __ldcs(reinterpret_cast<const uint4 *>(src));
             }
         } else {
-            const int col = 2 * (int)lane;
-            const T a = __ldg(src + col), b = col + 1 < q.width ? __ldg(src + col + 1) : from_float<T>(0.0f);
-            if constexpr (kP == 3) {
-                uint32_t p[3];
-                split(make_float2(a, b), p);
+            using W = typename std::conditional<kP == 3, uint2, uint32_t>::type;  // two neighbours
+            const int have = q.width - 8 * (int)lane;
+            T v[8];
+            if (q.vec == 2) {
+                W w[4];
 #pragma unroll
-                for (int j = 0; j < 3; ++j) *reinterpret_cast<uint32_t *>(dst + j * q.layer + col) = p[j];
+                for (int i = 0; i < 4; ++i) w[i] = 2 * i < have ? __ldg(reinterpret_cast<const W *>(src) + i) : W{};
+                memcpy(v, w, sizeof(v));
             } else {
-                *reinterpret_cast<__nv_bfloat162 *>(dst + col) = __nv_bfloat162(a, b);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = i < have ? __ldg(src + i) : from_float<T>(0.0f);
+            }
+            if constexpr (kP == 3) {
+                store_pieces(v, dst, q.layer);
+            } else {
+                uint4 w;
+                memcpy(&w, v, sizeof(w));
+                *reinterpret_cast<uint4 *>(dst) = w;
             }
         }
     }
@@ -1355,8 +1365,9 @@ struct Layouts {
         LayoutJob &q = count++ ? jobs.second : jobs.first;
         q.from = o.p, q.to = reinterpret_cast<bf16 *>(to), q.ld = o.ld, q.rows = rows, q.width = width;
         q.ld_to = laid_out_ld(width), q.layer = rows * q.ld_to;
-        q.vec = width % 8 == 0 && ((uintptr_t)q.from | (uintptr_t)(q.ld * (f32 ? 4 : 2))) % 16 == 0;
-        q.lanes = (unsigned)(q.vec ? width / 8 : (width + 1) / 2);
+        const uintptr_t starts = (uintptr_t)q.from | (uintptr_t)(q.ld * (f32 ? 4 : 2));
+        q.vec = width % 8 == 0 && starts % 16 == 0 ? 8 : (width % 2 == 0 && starts % (f32 ? 8 : 4) == 0 ? 2 : 1);
+        q.lanes = (unsigned)(width + 7) / 8;
         jobs.blocks += (unsigned)std::min<long long>(((long long)rows * q.lanes + 255) / 256, 8LL * sm_count());
         if (count == 1) jobs.first_blocks = jobs.blocks;
         o = {q.to, q.ld_to, o.mn, q.layer};
