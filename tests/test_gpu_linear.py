@@ -265,3 +265,35 @@ def test_c_abi_without_scratch_and_its_error_word():
     assert int(word) == 0
     p.dtype = p.out_dtype = fb.F32   # float32 operands are laid out in scratch
     assert fb.flashbev_linear(p, None, check=False) == fb.TOO_SMALL
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("shape", [(200, 256, 256), (320, 1024, 256), (900, 300, 256), (100, 264, 1000), (64, 1024, 1600), (16, 2048, 64), (2500, 48, 32)])
+def test_sums_that_may_be_shared_and_need_not(shape, dtype):
+    """Sizes on either side of where blocks begin to share sums: forward, both products of the backward, and again without scratch."""
+    rows, K, N = shape
+    gen, x, w, b = inputs(rows, K, N, dtype, 11)
+    want, _, off, _ = ref.linear(x, w, b)
+    ref.check(fb.linear(x, w, b), want, off, shape)
+    g = draw(gen, rows, N, dtype=dtype)
+    wants, bounds = ref.linear_backward(g, x, w, fb.ACT_NONE, None)
+    for wanted in ((1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 1, 1)):
+        grads = fb.linear_backward(g, x, w, grad_x=wanted[0], grad_weight=wanted[1], grad_bias=wanted[2])
+        for got, a, bound, asked in zip(grads, wants, bounds, wanted):
+            assert (got is not None) == bool(asked)
+            if asked:
+                ref.check(got, a, bound, (shape, wanted))
+
+
+@pytest.mark.parametrize("types", [(BF16, BF16), (BF16, F32), (F32, F32)])
+@pytest.mark.parametrize("off, pad, N", [(0, 0, 130), (0, 3, 130), (1, 0, 130), (2, 2, 130), (0, 1, 129), (1, 7, 8), (0, 8, 264), (2, 6, 264)])
+def test_gradients_of_many_rows_at_any_alignment(off, pad, N, types):
+    dtype, grad_type = types
+    rows, K = 3001, 40
+    gen, x, w, b = inputs(rows, K, N, dtype, 13)
+    g = draw(gen, rows, off + N + pad, dtype=grad_type)[:, off:off + N]
+    z = draw(gen, rows, N + 2, dtype=dtype)[:, :N]
+    for act, pre in ((fb.ACT_NONE, None), (fb.ACT_GELU, z)):
+        wants, bounds = ref.linear_backward(g, x, w, act, pre)
+        for got, a, bound, what in zip(fb.linear_backward(g, x, w, act=act, preact=pre), wants, bounds, ("x", "weight", "bias")):
+            ref.check(got, a, bound, (off, pad, N, act, what))
