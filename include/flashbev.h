@@ -336,8 +336,8 @@ typedef enum flashbev_act {
  *
  * Enqueues one kernel; one before it where operands have to be laid out in the scratch (float32 ones, bf16 ones that are
  * not 16-byte aligned with strides of whole 16-byte vectors; not for up to eight rows), and one behind it where a long sum
- * is shared by several thread blocks.  rows = 0 is allowed and enqueues nothing.  `out` and `preact_out` may not overlap any input, but `out` may be
- * `residual` itself (same address and stride).  All pointers element-aligned, else FLASHBEV_MISALIGNED; 16-byte
+ * is shared by several thread blocks.  rows = 0 is allowed and enqueues nothing.  `out` and `preact_out` may not overlap any input or
+ * each other, but `out` may be `residual` itself (same address and stride).  All pointers element-aligned, else FLASHBEV_MISALIGNED; 16-byte
  * aligned addresses and strides of whole 16-byte vectors are the fast layout.  rows < 2^31
  * and in_features, out_features <= 2^24, else FLASHBEV_UNSUPPORTED.
  */
@@ -365,7 +365,9 @@ typedef struct flashbev_linear_params {
 } flashbev_linear_params;
 
 flashbev_status flashbev_linear(const flashbev_linear_params *p, void *stream);
-size_t flashbev_linear_workspace_bytes(const flashbev_linear_params *p); /* 0 if none is used, or `p` is invalid */
+/* Of the call as it will be made, pointers, strides and types filled in (the scratch itself aside): they decide what has to be laid
+ * out.  0 if none is used, or `p` is invalid.  The same holds for the gradients' queries. */
+size_t flashbev_linear_workspace_bytes(const flashbev_linear_params *p);
 
 /*
  * Gradients of flashbev_linear:

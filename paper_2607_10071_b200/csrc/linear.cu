@@ -968,7 +968,8 @@ __global__ void __launch_bounds__(256) layout_kernel(const __grid_constant__ Lay
 
 // ---- dz = grad_out act'(z), and its column sums ---------------------------------------------------------------------------
 
-constexpr int kSlopeRows = 8;  // warps of a block: each takes every eighth row of the block's
+constexpr int kSlopeRows = 8;    // warps of a block: each takes every eighth row of the block's
+constexpr int kSlopeBlocks = 3;  // blocks of an SM
 
 // VEC neighbours, aligned as a whole; `once`: nobody else reads them.
 template <typename T, int VEC>
@@ -989,11 +990,12 @@ __device__ __forceinline__ void load(Loaded<T, VEC> &to, const T *from, bool onc
 }
 
 // A lane has VEC neighbouring columns, a warp a stretch of a row, the block `per` rows.  dz, in bf16 numbers or three pieces
-// `layer` apart, may be NULL (column sums only), sums too.  One pass over g and z, bound by traffic: about 43 us for the 246 MB of
-// 40000 x 1024 bf16 numbers and GELU (5.7 TB/s).  Batches of rows whose loads are all under way, and few blocks for them, take 10 us
-// for sums of 40000 x 256 and the kernel that joins them, 14 by a loop of one row at a time.
-template <typename TG, typename TZ, int VEC>
-__global__ void __launch_bounds__(32 * kSlopeRows, VEC == 8 && sizeof(TZ) == 2 ? 2 : 3) slope_kernel(const TG *__restrict__ g, long long ld_g, const TZ *__restrict__ z, long long ld_z,
+// `layer` apart, may be NULL (column sums only), sums too; ACT: there is a z.  One pass over g and z, bound by traffic (column sums of
+// 40000 x 1024 bf16 numbers and the kernel that joins them: 19 us, 4.4 TB/s).  The loads of a batch of rows are under way together, and
+// all blocks are on the SMs at once: all gradients of 40000 x 256 -> 1024 with GELU take 106 us so, 112 with two blocks of longer
+// batches, 111 by a loop over single rows.
+template <typename TG, typename TZ, int VEC, bool ACT>
+__global__ void __launch_bounds__(32 * kSlopeRows, kSlopeBlocks) slope_kernel(const TG *__restrict__ g, long long ld_g, const TZ *__restrict__ z, long long ld_z,
                                                                 bf16 *__restrict__ dz, long long ld_dz, long long layer, float *__restrict__ sums, int M,
                                                                 int N, int per, int act, const __grid_constant__ LayoutJobs jobs)
 {
@@ -1014,7 +1016,7 @@ __global__ void __launch_bounds__(32 * kSlopeRows, VEC == 8 && sizeof(TZ) == 2 ?
 #pragma unroll
     for (int j = 0; j < VEC; ++j) acc[j] = 0.0f;
     // (all loads of a batch of rows ahead of their arithmetic, the last batch's too)
-    constexpr int kBatch = VEC == 8 && sizeof(TZ) == 4 ? 2 : 4;
+    constexpr int kBatch = VEC == 8 && (sizeof(TZ) == 4 || ACT) ? 2 : 4;
     if (col < N)
         for (long long first = (long long)blockIdx.y * per + warp; first < row1; first += kBatch * kSlopeRows) {
             Loaded<TG, VEC> gq[kBatch];
@@ -1024,25 +1026,25 @@ __global__ void __launch_bounds__(32 * kSlopeRows, VEC == 8 && sizeof(TZ) == 2 ?
                 const long long row = first + k * kSlopeRows;
                 if (row >= row1) break;
                 load(gq[k], g + row * ld_g + col, dz != nullptr);  // (without dz the products read it too)
-                if (z) load(zq[k], z + row * ld_z + col, true);
+                if constexpr (ACT) load(zq[k], z + row * ld_z + col, true);
             }
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
                 const long long row = first + k * kSlopeRows;
                 if (row >= row1) break;
                 TG gv[VEC];
-                TZ zv[VEC];
+                TZ zv[VEC] = {};
                 memcpy(gv, &gq[k], sizeof(gv));
-                memcpy(zv, &zq[k], sizeof(zv));
+                if constexpr (ACT) memcpy(zv, &zq[k], sizeof(zv));
                 float d[VEC];
                 if constexpr (VEC == 1) {
-                    d[0] = z ? slope_times<kFast>(both(to_float(gv[0])), both(to_float(zv[0])), act).x : to_float(gv[0]);
+                    d[0] = ACT ? slope_times<kFast>(both(to_float(gv[0])), both(to_float(zv[0])), act).x : to_float(gv[0]);
                     acc[0] += d[0];
                 } else {
 #pragma unroll
                     for (int j = 0; j < VEC; j += 2) {
                         float2 v = make_float2(to_float(gv[j]), to_float(gv[j + 1]));
-                        if (z) v = slope_times<kFast>(v, make_float2(to_float(zv[j]), to_float(zv[j + 1])), act);
+                        if constexpr (ACT) v = slope_times<kFast>(v, make_float2(to_float(zv[j]), to_float(zv[j + 1])), act);
                         d[j] = v.x, d[j + 1] = v.y;
                         v = __fadd2_rn(v, make_float2(acc[j], acc[j + 1]));
                         acc[j] = v.x, acc[j + 1] = v.y;
@@ -1558,9 +1560,9 @@ BackwardPlan plan_backward(const flashbev_linear_backward_params *p)
     if (q.lay_x) q.x_at = at, at += laid_out_bytes(M, K, f32);
     if (q.lay_w) q.w_at = at, at += laid_out_bytes(N, K, f32);
     if (q.need_dz || q.need_b) {
-        // as many blocks as the SMs hold of slope_kernel's widest instance, but no fewer than 32 rows for each
+        // as many blocks as the SMs hold, but no fewer than 32 rows for each
         const int across = std::max(1, (N + 255) / 256);
-        const long long blocks = std::max(1, (f32 ? 3 : 2) * sm_count() / across);
+        const long long blocks = std::max(1, kSlopeBlocks * sm_count() / across);
         q.per = (int)std::max<long long>(32, (M + blocks - 1) / blocks);
         q.chunks = (int)(((long long)M + q.per - 1) / q.per);
         if (q.need_b) q.sums_at = at, at += round_up((size_t)q.chunks * N * sizeof(float));
@@ -1588,7 +1590,9 @@ cudaError_t launch_slope(const flashbev_linear_backward_params *p, const Backwar
                (!z || ((uintptr_t)z | (uintptr_t)(ld_z * (long long)sizeof(TZ))) % (numbers == 8 ? 16 : numbers * sizeof(TZ)) == 0);
     };
     const int vec = starts_on(8) ? 8 : (starts_on(2) ? 2 : 1), width = 32 * vec;
-    const auto kernel = vec == 8 ? slope_kernel<TG, TZ, 8> : (vec == 2 ? slope_kernel<TG, TZ, 2> : slope_kernel<TG, TZ, 1>);
+    const auto pick = [&](auto eight, auto two, auto one) { return vec == 8 ? eight : (vec == 2 ? two : one); };
+    const auto kernel = z ? pick(slope_kernel<TG, TZ, 8, true>, slope_kernel<TG, TZ, 2, true>, slope_kernel<TG, TZ, 1, true>)
+                          : pick(slope_kernel<TG, TZ, 8, false>, slope_kernel<TG, TZ, 2, false>, slope_kernel<TG, TZ, 1, false>);
     const unsigned across = (unsigned)((N + width - 1) / width);
     const dim3 grid(across, (unsigned)q.chunks + (jobs.blocks + across - 1) / across);
     return launch_dependent(kernel, grid, dim3(32 * kSlopeRows), 0, stream,
