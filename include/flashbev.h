@@ -334,12 +334,12 @@ typedef enum flashbev_act {
  * pieces each and the six products above 2^-24 of the whole are summed (a finite operand beyond 3.38e38 and
  * an infinite one give NaN there).  The result is reproducible bit for bit.
  *
- * Enqueues one kernel; one before it where operands have to be laid out in the scratch (float32 ones, bf16 ones that are
- * not 16-byte aligned with strides of whole 16-byte vectors; not for up to eight rows), and one behind it where a long sum
- * is shared by several thread blocks.  rows = 0 is allowed and enqueues nothing.  `out` and `preact_out` may not overlap any input or
- * each other, but `out` may be `residual` itself (same address and stride).  All pointers element-aligned, else FLASHBEV_MISALIGNED; 16-byte
- * aligned addresses and strides of whole 16-byte vectors are the fast layout.  rows < 2^31
- * and in_features, out_features <= 2^24, else FLASHBEV_UNSUPPORTED.
+ * Enqueues one kernel; one before it where operands have to be laid out in the scratch (float32 ones, bf16 ones that
+ * are not 16-byte aligned with strides of whole 16-byte vectors; not for up to eight rows), and one behind it where a
+ * long sum is shared by several thread blocks.  rows = 0 is allowed and enqueues nothing.  `out` and `preact_out` may
+ * not overlap any input or each other, but `out` may be `residual` itself (same address and stride).  All pointers
+ * element-aligned, else FLASHBEV_MISALIGNED; 16-byte aligned addresses and strides of whole 16-byte vectors are the
+ * fast layout.  rows < 2^31 and in_features, out_features <= 2^24, else FLASHBEV_UNSUPPORTED.
  */
 typedef struct flashbev_linear_params {
     size_t struct_size;        /* sizeof(flashbev_linear_params) of the caller's header */
@@ -414,13 +414,13 @@ typedef enum flashbev_norm {
  *
  *     h = x + scale * gate * after(y),     n = before(h)
  *
- * y is the block's output, x the rows that passed it by, `after` the norm behind the block (or none), `before` the norm ahead of
- * the next block (or none).  gate has gate_groups rows of C, row g for the rows g * rows / gate_groups and up: 1 for a gate per
- * channel, a batch's size for one per sample, `rows` for one per row.  Without y, h = x and only n is computed.  Statistics and h are
- * fp32 and n is formed from the unrounded h; the mean is taken off before the squares are summed; h and n are rounded once.  One kernel;
- * rows = 0 enqueues nothing.  h may be x and n may be y (same address and stride); no other overlap.  Pointers element-aligned,
- * else FLASHBEV_MISALIGNED.  C <= FLASHBEV_NORM_MAX_CHANNELS, rows and strides < 2^31, else
- * FLASHBEV_UNSUPPORTED.
+ * y is the block's output, x the rows that passed it by, `after` the norm behind the block (or none), `before` the
+ * norm ahead of the next block (or none).  gate has gate_groups rows of C, row g for the rows g * rows / gate_groups
+ * and up: 1 for a gate per channel, a batch's size for one per sample, `rows` for one per row.  Without y, h = x and
+ * only n is computed.  Statistics and h are fp32 and n is formed from the unrounded h; the mean is taken off before
+ * the squares are summed; h and n are rounded once.  One kernel; rows = 0 enqueues nothing.  h may be x and n may be
+ * y (same address and stride); no other overlap.  Pointers element-aligned, else FLASHBEV_MISALIGNED.  C <=
+ * FLASHBEV_NORM_MAX_CHANNELS, rows and strides < 2^31, else FLASHBEV_UNSUPPORTED.
  */
 #define FLASHBEV_NORM_MAX_CHANNELS 4096
 typedef struct flashbev_block_norm_params {
@@ -444,10 +444,11 @@ typedef struct flashbev_block_norm_params {
 flashbev_status flashbev_block_norm(const flashbev_block_norm_params *p, void *stream);
 
 /*
- * Gradients of flashbev_block_norm at the same inputs, from those at h and n.  Nothing is kept from the forward call: the statistics
- * are taken again from x and y, which have to be read for the parameters' gradients anyway.  Enqueues one kernel, and a second one
- * where gradients of parameters are wanted (they are sums over rows).  Reproducible bit for bit.  Gradients may not overlap inputs or
- * one another, but grad_x may be grad_h and grad_y may be grad_n (same address and stride).  rows = 0 sets the parameters' gradients to zero.
+ * Gradients of flashbev_block_norm at the same inputs, from those at h and n.  Nothing is kept from the forward call:
+ * the statistics are taken again from x and y, which have to be read for the parameters' gradients anyway.  Enqueues
+ * one kernel, and a second one where gradients of parameters are wanted (they are sums over rows).  Reproducible bit
+ * for bit.  Gradients may not overlap inputs or one another, but grad_x may be grad_h and grad_y may be grad_n (same
+ * address and stride).  rows = 0 sets the parameters' gradients to zero.
  */
 typedef struct flashbev_block_norm_backward_params {
     size_t struct_size;        /* sizeof(flashbev_block_norm_backward_params) of the caller's header */
