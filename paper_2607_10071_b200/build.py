@@ -86,7 +86,9 @@ def build(force: bool = False, verbose: bool = False, debug_bounds: bool = False
 
     ``debug_bounds``: build libflashbev_debug_bounds.so instead, with -DFLASHBEV_DEBUG_BOUNDS: every index the
     tiled kernel computes is range-checked, violations are counted into the caller's ``debug_error_word`` and
-    the access is redirected to a safe slot (the stand-in for a memory checker on machines where none may run)."""
+    the access is redirected to a safe slot (the stand-in for a memory checker on machines where none may run).
+    The waits of the matrix products give up after the cycles that its environment names, FLASHBEV_WAIT_CYCLES=
+    loads,products,results."""
     lib = LIB_DEBUG_BOUNDS if debug_bounds else LIB
     if force or needs_build(lib):
         nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")

@@ -20,6 +20,8 @@
 
 #include <cuda_bf16.h>
 #include <math.h>
+#include <stdio.h>
+#include <stdlib.h>
 #include <string.h>
 
 #include <algorithm>
@@ -212,7 +214,22 @@ struct alignas(64) GemmParams {
     float *partial;             // instead of the epilogue: [splits][M][ld_partial] sums
     long long ld_partial;
     uint32_t *error_word;
+#ifdef FLASHBEV_DEBUG_BOUNDS
+    long long limits[3];        // of the waits of loads, products and epilogue
+#endif
 };
+
+// The cycles after which a wait gives up.  The checked build takes them from its environment, so that waits can be made to run out.
+enum Role { kLoads, kProducts, kResults };
+
+__device__ __forceinline__ long long wait_limit(const GemmParams &p, Role role)
+{
+#ifdef FLASHBEV_DEBUG_BOUNDS
+    return p.limits[role];
+#else
+    return kWaitCycles;
+#endif
+}
 
 // A tile of the epilogue is 32 rows x 32 columns of a result: rows of eight (float32) or four pieces of 16 bytes, swizzled as TMA has
 // them.  In tensor memory's layout a lane has a row; in global memory's neighbouring lanes have a row's pieces.  Neither side has bank
@@ -552,7 +569,7 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
                         stores_done();
                     }
                     if (!waited) {
-                        if (!(ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * a, u >> acc_shift & 1, &failed)))) break;
+                        if (!(ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * a, u >> acc_shift & 1, &failed, wait_limit(p, kResults))))) break;
                         tcgen05_fence_after();
                         waited = true;
                     }
@@ -617,7 +634,7 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
                         else if (odd || h + 1 == tiles) tile_leave<TOUT>(tile, tout, nullptr, 0, 16, row0, c0, p.M, p.N, 0, lane);
                     }
                 }
-                if (ok && !waited) ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * a, u >> acc_shift & 1, &failed));
+                if (ok && !waited) ok = __all_sync(0xffffffffu, mbar_wait(acc_full + 8 * a, u >> acc_shift & 1, &failed, wait_limit(p, kResults)));
                 if (!ok) break;
                 tcgen05_fence_before();
                 __syncwarp();
@@ -632,22 +649,23 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
             const uint32_t idesc = mma_idesc(p.bn, p.a_mn, p.b_mn);
             const int a_step = p.a_mn ? 2048 >> 4 : 32 >> 4, b_step = p.b_mn ? 2048 >> 4 : 32 >> 4;  // 16 of K further
             int stage = 0, phase = 0;
+            const long long limit = wait_limit(p, kProducts);
             Slots slots;
             unsigned u = 0;  // accumulators filled so far
-            bool ok = !p.kept || mbar_wait(kept_full, 0, &failed);
+            bool ok = !p.kept || mbar_wait(kept_full, 0, &failed, limit);
             for (Shares s(p); s.more(p) && ok; s.next(p)) {
                 for (int k0 = s.k; k0 < s.end && ok; k0 += p.run, ++u) {
                     const unsigned acc = u & acc_mask;
-                    ok = mbar_wait(acc_empty + 8 * acc, (u >> acc_shift & 1) ^ 1, &failed);
+                    ok = mbar_wait(acc_empty + 8 * acc, (u >> acc_shift & 1) ^ 1, &failed, limit);
                     // (the one accumulator of the small products: the tile before has been taken out)
-                    if (ok && kParts == 2 && runs && k0 == s.k) ok = mbar_wait(acc_empty + 8 * ((u + 1) & 1), ((u + 1) >> 1 & 1) ^ 1, &failed);
+                    if (ok && kParts == 2 && runs && k0 == s.k) ok = mbar_wait(acc_empty + 8 * ((u + 1) & 1), ((u + 1) >> 1 & 1) ^ 1, &failed, limit);
                     if (!ok) break;
                     tcgen05_fence_after();
                     const uint32_t d = tmem + acc * acc_step, small = runs ? tmem + 3 * p.bn : d + p.bn;
                     const int k1 = min(k0 + p.run, s.end);
                     for (int k = k0; k < k1; ++k) {
                         if constexpr (kPieces == 1) {
-                            if (!(ok = mbar_wait(full + 8 * stage, phase, &failed))) break;
+                            if (!(ok = mbar_wait(full + 8 * stage, phase, &failed, limit))) break;
                             tcgen05_fence_after();
                             const uint32_t at = stages_at + stage * stage_bytes, b_at = p.kept ? smem_u32(ring) + k * b_bytes : at + a_bytes;
                             const uint64_t a = smem_desc(at, p.a_mn, 128 * BK), b = smem_desc(b_at, p.b_mn, 128 * BK);
@@ -658,7 +676,7 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
                         } else {
                             const auto arrived = [&](int tile) {
                                 const int slot = slots.of(tile);
-                                ok = ok && mbar_wait(full + 8 * slot, slots.turn >> slot & 1, &failed);
+                                ok = ok && mbar_wait(full + 8 * slot, slots.turn >> slot & 1, &failed, limit);
                                 slots.turn ^= 1u << slot;
                             };
                             const auto multiply = [&](uint32_t to, int ta, int tb, bool add) {
@@ -697,16 +715,17 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
                     if (ok) mma_commit(acc_full + 8 * acc);
                 }
             }
-            if (!ok) {  // nothing of this CTA may be in flight when it gives its memory back
-                mma_commit(last);
-                mbar_drain(last, 0);
-            }
+            // No product may be under way when the CTA gives its memory back.  The epilogue has waited for every one of them, unless
+            // some wait ran out, whoever's it was.
+            mma_commit(last);
+            mbar_drain(last, 0, &failed);
         }
         __syncwarp();
     } else if (warp == kEpilogue + 1) {
         // ---- loads, by one thread
         if (elect_one()) {
             int stage = 0, phase = 0;
+            const long long limit = wait_limit(p, kLoads);
             bool ok = true;
             const auto load_b = [&](uint32_t at, int n0, int k, int piece, uint32_t bar) {  // (an operand whose rows run along M or N: 64 of it at a time)
                 if (!p.b_mn) tma_load_3d(at, &p.tb, k * BK, n0, piece, bar);
@@ -726,7 +745,7 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
             for (Shares s(p); s.more(p) && ok; s.next(p)) {
                 for (int k = s.k; k < s.end; ++k) {
                     if constexpr (kPieces == 1) {
-                        if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, &failed))) break;
+                        if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, &failed, limit))) break;
                         const uint32_t bar = full + 8 * stage, at = stages_at + stage * stage_bytes;
                         mbar_expect(bar, stage_bytes);
                         load_a(at, s.m0, k, 0, bar);
@@ -736,7 +755,7 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
 #pragma unroll
                         for (int tile = 0; tile < 6; ++tile) {
                             const int slot = slots.of(tile), piece = tile == kA0 || tile == kB0 ? 0 : (tile == kA1 || tile == kB1 ? 1 : 2);
-                            if (!(ok = ok && mbar_wait(empty + 8 * slot, (slots.turn >> slot & 1) ^ 1, &failed))) break;
+                            if (!(ok = ok && mbar_wait(empty + 8 * slot, (slots.turn >> slot & 1) ^ 1, &failed, limit))) break;
                             slots.turn ^= 1u << slot;
                             const bool is_a = tile == kA0 || tile == kA1 || tile == kA2;
                             const uint32_t bar = full + 8 * slot, at = smem_u32(ring) + slot * kSlot;
@@ -749,11 +768,13 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
                     }
                 }
             }
-            if (!ok && p.kept) mbar_drain(kept_full, 0);
-            if (!ok && kPieces == 1)  // the last load into every stage: the ones before `stage` in this round of the ring, the others in the round before
-                for (int i = 0; i < p.stages; ++i) mbar_drain(full + 8 * i, i < stage ? phase : phase ^ 1);
-            if (!ok && kPieces == 3)
-                for (int i = 0; i < kMostStages; ++i) mbar_drain(full + 8 * i, (slots.turn >> i & 1) ^ 1);
+            // Nor any load: the products have waited for them, unless some wait ran out.  The last one into every stage: the ones
+            // before `stage` in this round of the ring, the others in the round before.
+            if (p.kept) mbar_drain(kept_full, 0, &failed);
+            if (kPieces == 1)
+                for (int i = 0; i < p.stages; ++i) mbar_drain(full + 8 * i, i < stage ? phase : phase ^ 1, &failed);
+            else
+                for (int i = 0; i < kMostStages; ++i) mbar_drain(full + 8 * i, (slots.turn >> i & 1) ^ 1, &failed);
         }
         __syncwarp();
     }
@@ -1409,6 +1430,13 @@ flashbev_status run_product(const Plan &q, const Operand &a, const Operand &b, b
     g.ld_out = e.ld_out, g.ld_pre = e.ld_pre, g.ld_res = e.ld_res;
     g.out_vec = row_bytes(e.out, e.ld_out, e.out_f32), g.pre_vec = row_bytes(e.pre, e.ld_pre, f32), g.res_vec = row_bytes(e.residual, e.ld_res, e.out_f32);
     g.error_word = error_word;
+#ifdef FLASHBEV_DEBUG_BOUNDS
+    {
+        long long *const t = g.limits;
+        t[0] = t[1] = t[2] = kWaitCycles;
+        if (const char *given = getenv("FLASHBEV_WAIT_CYCLES")) sscanf(given, "%lld,%lld,%lld", t, t + 1, t + 2);
+    }
+#endif
     if (q.splits > 1) {
         g.partial = partial, g.ld_partial = q.ld_partial;
         // (partial sums have no other results)

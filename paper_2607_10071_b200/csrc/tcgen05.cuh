@@ -40,7 +40,11 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
+#ifdef FLASHBEV_DEBUG_BOUNDS  // (asks and does not sleep, so that a limit of a few cycles is one)
+    asm volatile("{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+#else
     asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+#endif
                  : "=r"(ok)
                  : "r"(bar), "r"(parity)
                  : "memory");
@@ -65,11 +69,16 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     return true;
 }
 
-// The wait of a CTA that has already failed, for what it still has in flight.
-__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity)
+// The wait for what a thread itself has started and has to see done before its CTA may end; whether the CTA has failed does not
+// matter to it.
+__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity, volatile int *failed)
 {
     const long long since = clock64();
-    while (!mbar_try(bar, parity) && clock64() - since < kWaitCycles / 8) {}
+    while (!mbar_try(bar, parity))
+        if (clock64() - since > kWaitCycles) {
+            *failed = 1;
+            return;
+        }
 }
 
 // ---- TMA ------------------------------------------------------------------------------------------------------------------
