@@ -403,6 +403,10 @@ typedef struct flashbev_linear_backward_params {
 flashbev_status flashbev_linear_backward(const flashbev_linear_backward_params *p, void *stream);
 size_t flashbev_linear_backward_workspace_bytes(const flashbev_linear_backward_params *p);
 
+/* How many thread blocks of these products, of any call on the current device since the library was loaded, have given up (see
+ * `error_word`); 0 unless something is badly wrong.  Waits for all work of the device, so not while a stream is being captured. */
+flashbev_status flashbev_linear_given_up(uint32_t *blocks);
+
 typedef enum flashbev_norm {
     FLASHBEV_NORM_NONE = 0,
     FLASHBEV_NORM_LAYER = 1, /* (v - mean) / sqrt(variance + eps) * weight + bias, variance over C (not C - 1) */

@@ -204,6 +204,8 @@ def _declare(L: ctypes.CDLL) -> ctypes.CDLL:
     L.flashbev_sampling_vt_multires.argtypes = [ctypes.POINTER(VtMultiresParams), ctypes.c_void_p]
     L.flashbev_sca.restype = ctypes.c_int
     L.flashbev_sca.argtypes = [ctypes.POINTER(ScaParams), ctypes.c_void_p]
+    L.flashbev_linear_given_up.restype = ctypes.c_int
+    L.flashbev_linear_given_up.argtypes = [ctypes.POINTER(ctypes.c_uint32)]
     L.flashbev_block_norm.restype = ctypes.c_int
     L.flashbev_block_norm.argtypes = [ctypes.POINTER(BlockNormParams), ctypes.c_void_p]
     for name, params in (("linear", LinearParams), ("linear_backward", LinearBackwardParams),
@@ -417,19 +419,38 @@ def flashbev_linear_backward_workspace_bytes(params: LinearBackwardParams) -> in
     return int(lib().flashbev_linear_backward_workspace_bytes(ctypes.byref(params)))
 
 
-def linear(x, weight, bias=None, act=ACT_NONE, residual=None, out=None, out_dtype=None, preact=None, stream=None):
+def flashbev_linear_given_up() -> int:
+    """Thread blocks of matrix products that have given up on the current device."""
+    blocks = ctypes.c_uint32()
+    st = lib().flashbev_linear_given_up(ctypes.byref(blocks))
+    if st != OK:
+        raise FlashBevError(st, "flashbev_linear_given_up")
+    return blocks.value
+
+
+def linear_given_up(device=None) -> int:
+    """How many thread blocks of ``linear`` and ``linear_backward`` have given up on a device (None: the current one) since the library
+    was loaded: a block whose waits for its own loads or products do not end within seconds stops waiting, and the results of its call
+    are not valid.  0 unless something is badly wrong.  Waits for all work of the device; not during a capture."""
+    import torch
+    with torch.cuda.device(device):
+        return flashbev_linear_given_up()
+
+
+def linear(x, weight, bias=None, act=ACT_NONE, residual=None, out=None, out_dtype=None, preact=None, stream=None, error_word=None):
     """``residual + act(x weight^T + bias)``: x CUDA [..., K], weight [N, K], bias [N] of one type (float32 or bfloat16), residual
     and result [..., N] of ``out_dtype`` (F32, BF16; None: that of ``out``, or of x).  Rows may be any equal distance apart.
     ``preact``: [..., N] tensor of x's type that receives ``x weight^T + bias``, for ``linear_backward``.  ``out`` may be
-    ``residual``.  ``stream``: a raw cudaStream_t, as for ``sampling_vt``."""
-    return _result((_native or native()).linear(x, weight, bias, act, residual, out, out_dtype, preact, stream), "flashbev_linear")
+    ``residual``.  ``stream``: a raw cudaStream_t, as for ``sampling_vt``.  ``error_word``: one int32 on the device, to which the call
+    adds the thread blocks that gave up (``linear_given_up`` counts those of all calls)."""
+    return _result((_native or native()).linear(x, weight, bias, act, residual, out, out_dtype, preact, stream, error_word), "flashbev_linear")
 
 
-def linear_backward(grad_out, x, weight, act=ACT_NONE, preact=None, grad_x=True, grad_weight=True, grad_bias=True, stream=None):
+def linear_backward(grad_out, x, weight, act=ACT_NONE, preact=None, grad_x=True, grad_weight=True, grad_bias=True, stream=None, error_word=None):
     """Gradients of ``linear`` at x, weight and bias from that at its result (float32 or bfloat16; the residual's is that gradient
     itself).  ``preact``: what the forward call kept; needed with an activation.  Returns (grad_x, grad_weight, grad_bias) of
-    x's type, None for those not wanted."""
-    return _result((_native or native()).linear_backward(grad_out, x, weight, act, preact, grad_x, grad_weight, grad_bias, stream),
+    x's type, None for those not wanted.  ``error_word``: as for ``linear``."""
+    return _result((_native or native()).linear_backward(grad_out, x, weight, act, preact, grad_x, grad_weight, grad_bias, stream, error_word),
                    "flashbev_linear_backward")
 
 

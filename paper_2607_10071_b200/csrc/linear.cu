@@ -481,6 +481,9 @@ struct Slots {
 // slots); float32 40000 x 256 x 256: 36 us, bound by the tensor cores (54 %) and the loads in turn.
 constexpr int kAny = 4;
 
+// Blocks that have given up on this device (flashbev_linear_given_up)
+__device__ unsigned given_up;
+
 template <int kPieces, typename TOUT, int kEpilogue, int MODE>
 __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const __grid_constant__ GemmParams p)
 {
@@ -784,7 +787,10 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
         tcgen05_fence_after();
         tmem_free(tmem, p.columns);
     }
-    if (threadIdx.x == 0 && failed && p.error_word) atomicAdd(p.error_word, 1u);
+    if (threadIdx.x == 0 && failed) {
+        atomicAdd(&given_up, 1u);
+        if (p.error_word) atomicAdd(p.error_word, 1u);
+    }
 }
 
 // ---- sums that several CTAs shared ----------------------------------------------------------------------------------------
@@ -1760,6 +1766,16 @@ flashbev_status flashbev_linear_backward(const flashbev_linear_backward_params *
     }
     t_last_launches = launches;
     t_last_kernel = f32 ? "linear_backward_f32" : "linear_backward_bf16";
+    return FLASHBEV_OK;
+}
+
+flashbev_status flashbev_linear_given_up(uint32_t *blocks)
+{
+    if (!blocks) return FLASHBEV_INVALID_ARG;
+    if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyFromSymbol(blocks, given_up, sizeof(*blocks)) != cudaSuccess) {
+        cudaGetLastError();
+        return FLASHBEV_CUDA_ERROR;
+    }
     return FLASHBEV_OK;
 }
 

@@ -499,6 +499,16 @@ at::Tensor rows_like(const at::Tensor &t, int64_t width, int32_t dtype)
     return at::empty(shape, at::TensorOptions().dtype(scalar_type(dtype)).device(t.device()));
 }
 
+// The word that counts thread blocks which gave up: one int32 on the device of `like`, or None
+uint32_t *word(PyObject *o, const at::Tensor &like)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = tensor(o, "error_word");
+    if (!t.is_cuda() || t.device() != like.device() || t.scalar_type() != at::kInt || t.numel() != 1)
+        value_error("error_word must be one int32 on the device of the others");
+    return static_cast<uint32_t *>(t.data_ptr());
+}
+
 bool truth(PyObject *o)
 {
     const int v = PyObject_IsTrue(o);
@@ -533,11 +543,11 @@ const at::Tensor &rows_argument(PyObject *o, const char *what)
     return t;
 }
 
-// x, weight, bias, act, residual, out, out_dtype, preact, stream
+// x, weight, bias, act, residual, out, out_dtype, preact, stream, error_word
 PyObject *py_linear(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return guarded([&]() -> PyObject * {
-        need_args(n, 9);
+        need_args(n, 10);
         const at::Tensor &x = rows_argument(a[0], "x");
         flashbev_linear_params p = {};
         p.struct_size = sizeof(p);
@@ -559,6 +569,7 @@ PyObject *py_linear(PyObject *, PyObject *const *a, Py_ssize_t n)
         p.ld_residual = matrix(residual, p.rows, p.out_features, "residual");
         p.ld_preact = matrix(pre, p.rows, p.out_features, "preact");
         const StreamArg stream(a[8]);
+        p.error_word = word(a[9], x);
         const flashbev_status st = unlocked([&] {
             const Place place(x, stream);
             if (!out.defined()) out = place.result(rows_like(x, p.out_features, p.out_dtype));
@@ -574,11 +585,11 @@ PyObject *py_linear(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// grad_out, x, weight, act, preact, grad_x, grad_weight, grad_bias (whether each is wanted), stream
+// grad_out, x, weight, act, preact, grad_x, grad_weight, grad_bias (whether each is wanted), stream, error_word
 PyObject *py_linear_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return guarded([&]() -> PyObject * {
-        need_args(n, 9);
+        need_args(n, 10);
         const at::Tensor &x = rows_argument(a[1], "x");
         flashbev_linear_backward_params p = {};
         p.struct_size = sizeof(p);
@@ -596,6 +607,7 @@ PyObject *py_linear_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         p.ld_preact = matrix(pre, p.rows, p.out_features, "preact");
         const bool want_x = truth(a[5]), want_w = truth(a[6]), want_b = truth(a[7]);
         const StreamArg stream(a[8]);
+        p.error_word = word(a[9], x);
         at::Tensor gx, gw, gb, scratch;
         const flashbev_status st = unlocked([&] {
             const Place place(x, stream);

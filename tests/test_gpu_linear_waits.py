@@ -127,3 +127,49 @@ def test_gradients_whose_waits_run_out(checked, monkeypatch):
             assert all(torch.equal(a, b) for a, b in zip(grads, want))
         monkeypatch.delenv("FLASHBEV_WAIT_CYCLES")
         assert run() == 0 and all(torch.equal(a, b) for a, b in zip(grads, want)), limits
+
+
+SCRIPT = """
+import os, sys
+import torch
+sys.path.insert(0, sys.argv[1])
+from paper_2607_10071_b200 import binding as fb
+assert fb.LIB_PATH.startswith(sys.argv[1])
+x, w, g = (torch.ones(s, dtype=torch.bfloat16, device="cuda") for s in ((600, 1024), (96, 1024), (600, 96)))
+words = [torch.zeros(1, dtype=torch.int32, device="cuda") for _ in range(4)]
+good = fb.linear(x, w, error_word=words[0])
+fb.linear_backward(g, x, w, error_word=words[1])
+assert bool((good == 1024).all()) and fb.linear_given_up() == 0
+os.environ["FLASHBEV_WAIT_CYCLES"] = "0,0,0"
+fb.linear(x, w, error_word=words[2])
+fb.linear_backward(g, x, w, error_word=words[3])
+fb.linear(x, w)
+torch.cuda.synchronize()
+counts = [int(v) for v in words]
+assert counts[:2] == [0, 0] and counts[2] > 0 and counts[3] > 0, counts
+assert fb.linear_given_up() > sum(counts) and fb.linear_given_up(0) == fb.linear_given_up(x.device)
+print("counted")
+"""
+
+
+def test_callers_with_tensors_learn_of_it(checked, tmp_path):
+    """The package over the checked build instead of the ordinary one, in a process of its own."""
+    import os
+    import shutil
+    import subprocess
+    import sys
+    package = os.path.dirname(os.path.abspath(fb.__file__))
+    copy = tmp_path / os.path.basename(package)
+    shutil.copytree(package, copy, ignore=shutil.ignore_patterns("csrc", "__pycache__", "libflashbev*.so"))
+    shutil.copy(fbuild.LIB_DEBUG_BOUNDS, copy / "libflashbev.so")
+    env = {k: v for k, v in os.environ.items() if k not in ("FLASHBEV_WAIT_CYCLES", "PYTHONPATH")}
+    done = subprocess.run([sys.executable, "-c", SCRIPT, str(tmp_path)], env=env, cwd=tmp_path, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0 and "counted" in done.stdout, done.stderr
+
+
+def test_nothing_has_given_up():
+    x, w = torch.ones(600, 96, dtype=BF16, device="cuda"), torch.ones(40, 96, dtype=BF16, device="cuda")
+    word = torch.zeros(1, dtype=torch.int32, device="cuda")
+    fb.linear(x, w, error_word=word)
+    fb.linear_backward(torch.ones(600, 40, dtype=BF16, device="cuda"), x, w, error_word=word)
+    assert int(word) == 0 and fb.linear_given_up() == 0

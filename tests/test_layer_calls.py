@@ -208,3 +208,15 @@ def test_block_norm_refuses_tensors():
     for error, call in calls:
         with pytest.raises(error):
             call()
+
+
+def test_linear_refuses_error_words():
+    x, w, g = _fake(4, 6, 32), _fake(48, 32), _fake(24, 48)
+    assert fb.lib().flashbev_linear_given_up(None) == fb.INVALID_ARG
+    for word in (_fake(1, dtype="int32", device="cpu"), _fake(1, dtype="float32"), _fake(2, dtype="int32"), _fake(0, dtype="int32")):
+        with pytest.raises(ValueError, match="error_word"):
+            fb.linear(x, w, error_word=word)
+        with pytest.raises(ValueError, match="error_word"):
+            fb.linear_backward(g, x, w, error_word=word)
+    with pytest.raises(TypeError):
+        fb.linear(x, w, error_word=4096)
