@@ -498,15 +498,15 @@ __global__ void __launch_bounds__(gemm_threads(kEpilogue), 1) gemm_kernel(const 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t full = smem_u32(bars), empty = full + 8 * kMostStages, acc_full = empty + 8 * kMostStages, acc_empty = acc_full + 8 * kAccs,
                    last = acc_empty + 8 * kAccs, kept_full = last + 8;
-    // Tensor memory.  Two to four accumulators, so that some are taken out while another is filled.  The tensor cores cut a sum
+    // Tensor memory.  Two or four accumulators, so that some are taken out while another is filled (long runs may have one).  The tensor cores cut a sum
     // off, not round it, at every instruction, by 3e-8 of the sum on the average (2e-7 where all terms have one sign).  So (1) pieces have a second accumulator for all
     // products but p0 p0, which keeps the five small products of each step from cutting at the large sum; (2) after `run` blocks
     // the sum is added to a running one that stays in tensor memory too, behind the accumulators, and so does the small products'
     // then.
     constexpr int kParts = kPieces == 3 ? 2 : 1;
     const bool runs = MODE == kAny && p.run < p.kshare;
-    const int acc_step = runs ? p.bn : kParts * p.bn, sum_at = 2 * p.bn;  // (with runs there are two accumulators)
-    const unsigned acc_mask = p.accs - 1, acc_shift = p.accs == 4 ? 2 : 1;
+    const int acc_step = runs ? p.bn : kParts * p.bn, sum_at = p.accs * p.bn;
+    const unsigned acc_mask = p.accs - 1, acc_shift = p.accs / 2;
 
     if (threadIdx.x == 0) {
         failed = 0;
@@ -1306,7 +1306,6 @@ Plan plan_product(bool b_mn, bool f32, bool out_f32, bool heavy, int M, int N, i
         int parts = may_split && tiles * 2 <= sms ? (int)std::min<long long>(sms / tiles, (long long)q.kblocks * bk / 128) : 1;
         for (parts = std::max(1, parts); parts >= 1; parts /= 2) {
             const int share = (q.kblocks + parts - 1) / parts, splits = (q.kblocks + share - 1) / share;
-            if (bn > 128 && share > kLongRun / bk) continue;  // (no place for a running sum)
             const double items = (double)((tiles * splits + sms - 1) / sms), main = share * (f32 ? 10.0 : 2.15) * std::max(kBM + bn, f32 ? 0 : 240);
             const double rest = 12.0 * bn + 800.0, join = splits > 1 ? 7000.0 + splits * 8.0 * M * N / 2000.0 : 0.0;
             const double cost = items * std::max(main, rest) + std::min(main, rest) + join;
@@ -1325,12 +1324,13 @@ Plan plan_product(bool b_mn, bool f32, bool out_f32, bool heavy, int M, int N, i
     q.ew = f32 || q.kept || q.kshare * bk > kShort ? 8 : 16;
     q.stages = std::min(8, (ring_bytes(q.ew) - q.kept) / (a_bytes + (q.kept ? 0 : q.bn * 2 * bk)));  // (of bf16 operands)
     q.run = std::min(q.kshare, (out_f32 ? kRun : kLongRun) / bk);
-    // Accumulators: with runs two, the running sum and, of float32 operands, that of the small products; else four where they fit (float32
-    // operands: pairs).  Groups of epilogue warps: as many 64-column parts as the tile has in each, and no more of them than accumulators.
+    // Accumulators: with runs two (one beside the running sum of more than 128 columns: its runs are long ones, and taking a sum out every 260000
+    // cycles takes a few thousand), the running sum and, of float32 operands, that of the small products; else four where they fit
+    // (float32 operands: pairs).  Groups of epilogue warps: as many 64-column parts as the tile has in each, and no more of them than accumulators.
     const int parts = f32 ? 2 : 1, warps = q.ew / 4, wide = (q.bn + 63) / 64;
     const bool in_runs = q.run < q.kshare;
-    q.accs = !in_runs && 4 * parts * q.bn <= 512 ? 4 : 2;
-    const int used = in_runs ? (2 + parts) * q.bn : q.accs * parts * q.bn;
+    q.accs = in_runs ? (q.bn > 128 ? 1 : 2) : (4 * parts * q.bn <= 512 ? 4 : 2);
+    const int used = in_runs ? (q.accs + parts) * q.bn : q.accs * parts * q.bn;
     for (q.columns = 32; q.columns < used;) q.columns *= 2;
     q.groups = 1;
     while (!in_runs && q.groups < q.accs && q.groups * 2 * wide <= warps) q.groups *= 2;

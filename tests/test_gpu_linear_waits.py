@@ -23,6 +23,7 @@ CALLS = dict(one_block=(100, 64, 64, BF16, BF16, fb.ACT_NONE, False, False),    
              kept_weights=(40000, 128, 256, BF16, BF16, fb.ACT_NONE, False, False),
              several_tiles=(40000, 200, 264, BF16, F32, fb.ACT_SILU, False, True),
              running_sums=(20000, 1000, 256, BF16, F32, fb.ACT_NONE, False, False),
+             one_accumulator=(1300, 40000, 2000, BF16, BF16, fb.ACT_NONE, False, False),
              pieces=(20000, 130, 200, F32, F32, fb.ACT_RELU, True, False),
              pieces_running_sums=(20000, 520, 128, F32, F32, fb.ACT_NONE, False, False))
 
