@@ -121,13 +121,15 @@ __device__ __forceinline__ float sigmoid(float z)
     return FAST ? rcp_approx(1.0f + exp2_approx(-1.44269504f * z)) : 1.0f / (1.0f + expf(-z));
 }
 
-// Two numbers at a time.  GELU as max(z, 0) - |z| Phi(-|z|): no difference of near numbers on either side, and no infinity times zero.
+// Two numbers at a time.  GELU, where it is FAST, as max(z, 0) - |z| Phi(-|z|): no difference of near numbers on either side.  (Phi(-20)
+// is 0 in float32, and no infinity is multiplied by it.)  FAST is for bf16 results whose kernel the special functions bound; GELU is
+// then 3e-5 of its negative part off, a hundredth of its rounding.
 template <bool FAST, int ACT>
 __device__ __forceinline__ float2 activate(float2 z)
 {
     if (ACT == FLASHBEV_ACT_RELU) return make_float2(max_nan(z.x, 0.0f), max_nan(z.y, 0.0f));
     if (ACT == FLASHBEV_ACT_GELU) {
-        if constexpr (!FAST) return make_float2(z.x * normal_cdf<false>(z.x), z.y * normal_cdf<false>(z.y));
+        if constexpr (!FAST) return make_float2(fmaxf(z.x, -20.0f) * normal_cdf<false>(z.x), fmaxf(z.y, -20.0f) * normal_cdf<false>(z.y));
         const float2 a = magnitude(z), s = normal_tail(a), m = make_float2(max_nan(z.x, 0.0f), max_nan(z.y, 0.0f));
         return __ffma2_rn(make_float2(-a.x, -a.y), s, m);
     }
@@ -145,11 +147,11 @@ __device__ __forceinline__ void activate(float (&v)[N])
     }
 }
 
-template <bool FAST, int N>
+template <bool FAST, bool FAST_GELU = FAST, int N>
 __device__ __forceinline__ void activate_all(float (&v)[N], int act)
 {
     if (act == FLASHBEV_ACT_RELU) activate<FAST, FLASHBEV_ACT_RELU>(v);
-    else if (act == FLASHBEV_ACT_GELU) activate<FAST, FLASHBEV_ACT_GELU>(v);
+    else if (act == FLASHBEV_ACT_GELU) activate<FAST_GELU, FLASHBEV_ACT_GELU>(v);
     else if (act == FLASHBEV_ACT_SILU) activate<FAST, FLASHBEV_ACT_SILU>(v);
 }
 
@@ -841,7 +843,6 @@ __global__ void __launch_bounds__(256) join_kernel(const float *__restrict__ par
                                                    const TIN *__restrict__ bias, const TOUT *residual, long long ld_res, TOUT *out, long long ld_out,
                                                    TIN *pre, long long ld_pre, int act, const ColumnSums<TIN> columns, int sum_blocks)
 {
-    constexpr bool kFast = std::is_same<TOUT, bf16>::value;
     __shared__ float4 joined[8 * 33];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
@@ -880,7 +881,7 @@ __global__ void __launch_bounds__(256) join_kernel(const float *__restrict__ par
             if (bias) v[j] += to_float(bias[col + j]);
             if (pre) pre[row * ld_pre + col + j] = from_float<TIN>(v[j]);
         }
-        activate_all<kFast>(v, act);
+        activate_all<std::is_same<TOUT, bf16>::value, false>(v, act);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (col + j >= N) break;
@@ -1124,7 +1125,6 @@ __global__ void __launch_bounds__(256) rows_kernel(const TIN *__restrict__ x, lo
                                                    int N, int K, int shared, const TIN *__restrict__ bias, const TOUT *residual, long long ld_res,
                                                    TOUT *out, long long ld_out, TIN *pre, long long ld_pre, int act)
 {
-    constexpr bool kFast = std::is_same<TOUT, bf16>::value;
     constexpr int Q = 8 * (int)sizeof(TIN) / 16;
     __shared__ float joined[8][R * NC];
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -1172,29 +1172,25 @@ __global__ void __launch_bounds__(256) rows_kernel(const TIN *__restrict__ x, lo
         for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int d = 16; d; d /= 2) acc[r][c] += __shfl_xor_sync(0xffffffffu, acc[r][c], d);
+    // lane r NC + c has row r's column c
+    const int r = lane / NC, n = n0 + lane % NC;
+    float z[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < R * NC; ++i)
+        if (lane == i) z[0] = acc[i / NC][i % NC];
     if (shared) {
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int c = 0; c < NC; ++c)
-                if (lane == r * NC + c) joined[warp][lane] = acc[r][c];
+        if (lane < R * NC) joined[warp][lane] = z[0];
         __syncthreads();
         if (warp) return;
+        if (lane < R * NC)
+            for (int w = 1; w < 8; ++w) z[0] += joined[w][lane];
     }
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            if (lane != r * NC + c || r >= M || n0 + c >= N) continue;
-            float z[2] = {acc[r][c], 0.0f};
-            if (shared)
-                for (int w = 1; w < 8; ++w) z[0] += joined[w][lane];
-            if (bias) z[0] += to_float(bias[n0 + c]);
-            if (pre) pre[r * ld_pre + n0 + c] = from_float<TIN>(z[0]);
-            activate_all<kFast>(z, act);
-            if (residual) z[0] += to_float(residual[r * ld_res + n0 + c]);
-            out[r * ld_out + n0 + c] = from_float<TOUT>(z[0]);
-        }
+    if (r >= min(R, M) || n >= N) return;
+    if (bias) z[0] += to_float(bias[n]);
+    if (pre) pre[r * ld_pre + n] = from_float<TIN>(z[0]);
+    activate_all<std::is_same<TOUT, bf16>::value, false>(z, act);
+    if (residual) z[0] += to_float(residual[r * ld_res + n]);
+    out[r * ld_out + n] = from_float<TOUT>(z[0]);
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------------------
