@@ -750,9 +750,13 @@ BackwardShape backward_shape(const flashbev_block_norm_backward_params *p)
     s.team = team_threads(p->C), s.threads = std::max(256, s.team), s.teams = s.threads / s.team;
     s.gates = p->gate ? p->gate_groups : 1;
     const long long per = p->rows / s.gates;
-    const long long resident = s.threads > 512 ? sm_count() : 2LL * sm_count();
-    // More gates than teams, or a good many with few rows each: a team sums a gate's rows by itself.
-    s.direct = p->gate && (s.gates >= resident * s.teams || (per <= 4 && s.gates >= resident));
+    const long long resident = s.threads >= 512 ? sm_count() : 2LL * sm_count();
+    // More gates than teams: a team sums a gate's rows by itself.  More than blocks: whichever takes fewer rows' time, the team, all of the
+    // gate's rows one after another, or rounds of blocks, each the rows of a team and three rows' time to begin and end with.  (float32
+    // stream, a norm on either side, us by teams and by blocks: 18000 gates of 5 rows of 32: 22 and 420, 3000 of 20: 40 and 77, 1000 of 64: 105
+    // and 34; 600 gates of 20 rows of 256: 47 and 48, 2360 of 64: 185 and 269; in 51 such cases the choice is 15 % off at most.)
+    s.direct = p->gate && s.gates >= resident &&
+               (s.gates >= resident * s.teams || per < (s.gates + resident - 1) / resident * (3 + (per + s.teams - 1) / s.teams));
     const void *const outs[5] = {p->grad_after_weight, p->grad_after_bias, p->grad_before_weight, p->grad_before_bias, p->grad_gate};
     for (int i = 0; i < 5; ++i)
         if (outs[i] && !(i == 4 && s.direct)) s.want |= 1 << i, ++s.arrays;
@@ -789,7 +793,7 @@ flashbev_status flashbev_block_norm(const flashbev_block_norm_params *p, void *s
     al.rows(p->x, k.ld_x, p->dtype), al.rows(p->h, k.ld_h, p->dtype), al.rows(p->y, k.ld_y, p->branch_dtype), al.rows(p->n, k.ld_n, p->branch_dtype);
     al.rows(p->gate, p->C, p->param_dtype);
     const int threads = std::max(256, k.team), teams = threads / k.team;
-    const long long blocks = std::min<long long>((p->rows + teams - 1) / teams, (long long)sm_count() * (threads > 512 ? 2 : 6));
+    const long long blocks = std::min<long long>((p->rows + teams - 1) / teams, (long long)sm_count() * (threads >= 512 ? 2 : 6));
     const cudaError_t e = launch_norm<false>(k, p->dtype, p->branch_dtype, p->param_dtype, al.vec, (unsigned)blocks, threads, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess || cudaGetLastError() != cudaSuccess) {
         cudaGetLastError();

@@ -220,3 +220,17 @@ def test_linear_refuses_error_words():
             fb.linear_backward(g, x, w, error_word=word)
     with pytest.raises(TypeError):
         fb.linear(x, w, error_word=4096)
+
+
+@pytest.mark.parametrize("C, gates, per, blocks", [(64, 0, 50000, 296), (4096, 0, 5000, 148), (2050, 0, 5000, 148), (2048, 0, 5000, 296),
+                                                   (32, 18000, 5, 282), (256, 600, 5, 75), (256, 100, 50, 200), (32, 1000, 64, 1000), (4096, 40, 100, 120)])
+def test_block_norm_backward_scratch_is_that_of_the_blocks_that_run_at_once(C, gates, per, blocks):
+    """Partial sums of the norms' parameters, and of the gates where no team has one to itself: a row for each thread block.  Blocks of 512
+    threads (more than 2048 channels) are one to an SM; many gates with few rows each are for teams, not blocks."""
+    if fb.flashbev_block_norm_backward_workspace_bytes(norm_backward_params(C=2048, rows=1 << 20, gate=None, grad_gate=None)) != 4 * 296 * 2048 * 4:
+        pytest.skip("not 148 SMs")
+    rows = (gates or 1) * per
+    over = dict(C=C, rows=rows, gate_groups=gates) if gates else dict(C=C, rows=rows, gate=None, grad_gate=None)
+    need = fb.flashbev_block_norm_backward_workspace_bytes(norm_backward_params(**over))
+    assert need in (4 * blocks * C * 4, 5 * blocks * C * 4), need / (4 * C * 4)
+    assert (need == 4 * blocks * C * 4) == (gates == 0 or (C, gates) in ((32, 18000), (256, 600)))
