@@ -329,8 +329,10 @@ typedef enum flashbev_act {
 /*
  *     z = x weight^T + bias,     out = residual + act(z)
  *
- * Sums are fp32 in tensor memory, bias, activation and residual are applied to them unrounded, `out` and
- * `preact_out` are rounded once.  bf16 products are exact; float32 operands are taken apart into three bf16
+ * Sums are fp32 in tensor memory, which cuts them off, by 3e-8 to 2e-7 of the sum for every 16 terms, until they are
+ * taken out: every 384 terms where `out` is float32, every 32768 where it is bf16.  Bias, activation and residual are
+ * applied to them unrounded, `out` and `preact_out` are rounded once.  GELU of bf16 results of large calls is off by 3e-5
+ * of its negative part, a hundredth of that rounding.  bf16 products are exact; float32 operands are taken apart into three bf16
  * pieces each and the six products above 2^-24 of the whole are summed (a finite operand beyond 3.38e38 and
  * an infinite one give NaN there).  The result is reproducible bit for bit.
  *

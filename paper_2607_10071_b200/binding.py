@@ -438,7 +438,7 @@ def linear_given_up(device=None) -> int:
 
 
 def linear(x, weight, bias=None, act=ACT_NONE, residual=None, out=None, out_dtype=None, preact=None, stream=None, error_word=None):
-    """``residual + act(x weight^T + bias)``: x CUDA [..., K], weight [N, K], bias [N] of one type (float32 or bfloat16), residual
+    """``residual + act(x weight^T + bias)``, outside of autograd: x CUDA [..., K], weight [N, K], bias [N] of one type (float32 or bfloat16), residual
     and result [..., N] of ``out_dtype`` (F32, BF16; None: that of ``out``, or of x).  Rows may be any equal distance apart.
     ``preact``: [..., N] tensor of x's type that receives ``x weight^T + bias``, for ``linear_backward``.  ``out`` may be
     ``residual``.  ``stream``: a raw cudaStream_t, as for ``sampling_vt``.  ``error_word``: one int32 on the device, to which the call
@@ -476,7 +476,7 @@ def flashbev_block_norm_backward_workspace_bytes(params: BlockNormBackwardParams
 
 def block_norm(x, y=None, gate=None, scale=1.0, after=NORM_NONE, after_weight=None, after_bias=None, before=NORM_LAYER,
                before_weight=None, before_bias=None, eps=1e-5, h=None, n=None, keep_h=True, stream=None):
-    """Between two residual blocks: ``h = x + scale * gate * after(y)``, ``n = before(h)``; returns (h, n).
+    """Between two residual blocks: ``h = x + scale * gate * after(y)``, ``n = before(h)``; returns (h, n), outside of autograd.
 
     x, h: CUDA [..., C], float32 or bfloat16; y, n: the same shape, of x's type or bfloat16; rows may be any equal distance apart.
     gate: [C], or [gates, C] for equal runs of rows (one per sample, or one per row).  ``after`` and ``before``: NORM_NONE,
@@ -488,7 +488,8 @@ def block_norm(x, y=None, gate=None, scale=1.0, after=NORM_NONE, after_weight=No
 
 def block_norm_backward(grad_h, grad_n, x, y=None, gate=None, scale=1.0, after=NORM_NONE, after_weight=None, after_bias=None,
                         before=NORM_LAYER, before_weight=None, before_bias=None, eps=1e-5, stream=None):
-    """Gradients of ``block_norm`` at the same arguments from those at h and n (None: no such gradient).  Returns those at (x, y,
+    """Gradients of ``block_norm`` at the same arguments from those at h (None: no such gradient) and n (None exactly if ``before`` is
+    NORM_NONE).  Returns those at (x, y,
     gate, after_weight, after_bias, before_weight, before_bias), None for arguments that are None."""
     return _result((_native or native()).block_norm_backward(x, y, gate, scale, after, after_weight, after_bias, before, before_weight,
                                                              before_bias, eps, grad_h, grad_n, stream), "flashbev_block_norm_backward")

@@ -374,8 +374,9 @@ __device__ __forceinline__ T *row_of(const void *base, unsigned row, unsigned ld
 //
 // Measured, 256 columns: 40000 bf16 rows, a norm ahead only, 18 us (4.4 TB/s); with x and h in float32 23 us (5.5 TB/s); 184950 bf16
 // rows 68 us (5.6 TB/s); 80000 bf16 rows, two norms and a gate, 33 us (4.9 TB/s, 59 % of the issue slots).  Bound by traffic and, close
-// behind, by the instructions of the conversions and shuffles: two-wide arithmetic (Eight) made the last 45 -> 34 us.  Rows of an odd C,
-// element by element, reach 0.9 TB/s.  A ring of asynchronous copies in place of the prefetch in registers was slower.
+// behind, by the instructions of the conversions and shuffles: two-wide arithmetic (Eight) made the last 45 -> 34 us.  Rows of more than
+// 2048 columns have one block of 512 threads to an SM (20000 x 4096, bf16, sum and norm: 156 us, 4.2 TB/s).  Rows of an odd C, element by
+// element, take twice as long as those of an even one (40000 x 255: 25 us).  A ring of asynchronous copies in place of the prefetch in registers was slower.
 template <typename S, typename T, typename P, int VEC, bool WIDE>
 __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 3) norm_kernel(const __grid_constant__ NormParams p)
 {
@@ -433,8 +434,9 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 3) norm_
 // rows, and a team takes the rows of one gate after another and writes the gate's gradient itself.
 //
 // Measured, 256 columns: 40000 bf16 rows, a norm ahead only, 37 us (3.3 TB/s); 184950 of them 119 us (4.7 TB/s); 80000 with two norms
-// and a gate 71 us (3.4 TB/s, 50 % of the issue slots); 14927 x 936, float32 stream, two norms: 113 us (1.7 TB/s).  Bound by latency:
-// five sums over rows beside this row and the next take 128 registers, which leaves 16 warps on an SM; in wide rows by the barriers too.
+// and a gate 71 us (3.4 TB/s, 50 % of the issue slots); 14927 x 936, float32 stream, two norms: 113 us (1.7 TB/s); 20000 x 4096, bf16, a norm
+// ahead: 290 us (3.4 TB/s).  Bound by latency: five sums over rows beside this row and the next do not fit the 128 registers that leave 16
+// warps on an SM (16 to 280 bytes of them are spilled); in wide rows by the barriers too.
 template <typename S, typename T, typename P, int VEC, bool WIDE>
 __global__ void __launch_bounds__(WIDE ? kMostThreads : 256, WIDE ? 1 : 2) norm_backward_kernel(const __grid_constant__ NormParams p)
 {

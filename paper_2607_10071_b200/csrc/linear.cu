@@ -39,7 +39,7 @@ constexpr int kSmemLimit = 227 * 1024;
 constexpr int kControlBytes = 512;  // barriers and the like
 
 // Elements of float32 operands: x = p0 + p1 + p2, each piece the bf16 number nearest to what is left.  Every difference is exact and
-// 8 + 8 + 8 bits hold the 24 of x.  Of the nine products the three left out, p1 p2, p2 p1 and p2 p2, are below 2^-25 |a| |b|.  Two tf32
+// 8 + 8 + 8 bits hold the 24 of x.  Of the nine products the three left out, p1 p2, p2 p1 and p2 p2, are at most 2^-24 |a| |b|.  Two tf32
 // pieces cost the same tensor time (three products at half the rate) and lose two bits.
 __device__ __forceinline__ uint32_t pack(float lo, float hi)
 {
@@ -198,7 +198,7 @@ struct alignas(64) GemmParams {
     CUtensorMap ta, tb;         // operands
     CUtensorMap tout, tpre;     // results, with store_tma
     int a_mn, b_mn;             // the operand's rows run along M / N, one per k
-    int M, N, K;
+    int M, N;
     int bn, stages;             // columns of a tile; stages in the ring
     int tiles_n, tiles, kblocks, kshare, splits;  // a tile's sum is cut into `splits` of `kshare` blocks of K (the last may have fewer)
     int run;                    // blocks after which the sum is added to the running one; kshare or more: never
@@ -456,8 +456,8 @@ struct Shares {
 // float32 operands: every tile of a piece has a slot of shared memory and barriers of its own, twelve in all, six of one block and
 // six of the next.  A block's tiles come in the order below, and are released, from the first product that is their last on, in the
 // order of `released`; the tiles of the block after the next take the slots in that order, so that they are on their way while the
-// last two sixths of this block's products and all of the next one's run.  (40000 x 256 x 256: 31 us, of which the loads by
-// themselves take 17 and loads and products 25; stages of 32 of K in a ring of four, their rows of 64 bytes, 36.)
+// last two sixths of this block's products and all of the next one's run.  (40000 x 256 x 256: 36 us, of which the loads by
+// themselves take 17 and loads and products 25.)
 enum PieceTile { kA0 = 0, kB0 = 1, kB1 = 2, kA1 = 3, kB2 = 4, kA2 = 5 };
 
 struct Slots {
@@ -477,10 +477,12 @@ struct Slots {
 // does not need would be in its way: the code of the other activations and of rows of any alignment, skipped, cost 8 of 37 us
 // (184950 x 64 x 256) in instruction fetches.
 //
-// Measured: 8192 x 4096 x 4096, bf16, SiLU: 185 us by itself, the tensor cores busy for 85 % (237 us and 1.16 PFLOP/s in a long
-// run, where the power limit holds the clock down); 184950 x 256 x 256: 34 to 39 us, 4.8 TB/s, bound by what is read and written;
-// with 1024 columns, GELU and its argument kept, 40000 rows: 46 to 51 us, bound by the epilogue's instructions (59 % of the issue
-// slots); float32 40000 x 256 x 256: 36 us, bound by the tensor cores (54 %) and the loads in turn.
+// Measured: 8192 x 4096 x 4096, bf16, SiLU: 180 to 190 us by itself, the tensor cores busy for 85 % (232 us and 1.18 PFLOP/s in a long
+// run, where the power limit holds the clock down); 184950 x 256 x 256: 34 to 39 us, 4.9 TB/s, bound by what is read and written;
+// with 1024 columns, GELU and its argument kept, 40000 rows: 42 to 50 us, bound by the 164 MB that it writes (a memset of as much takes
+// 45 us; without the activation 37) and, where z is not kept, by the epilogue's instructions (38 us, 28 without the activation); float32
+// 40000 x 256 x 256: 36 to 38 us, bound by the tensor cores (54 %) and the loads in turn.  20 warps on an SM leave a
+// thread 96 registers: the instances of 16 epilogue warps with float32 results spill 48 to 68 bytes, those for anything 108 and 304.
 constexpr int kAny = 4;
 
 // Blocks that have given up on this device (flashbev_linear_given_up)
@@ -837,7 +839,7 @@ __global__ void __launch_bounds__(256) column_sum_kernel(const ColumnSums<T> q)
 
 // Adds the shares up in a fixed order and does what the epilogue would have done.  Four columns of a row per thread; with few of
 // them (`groups` > 1) as many threads take every so manieth share, and the first of them joins their sums.  The first blocks
-// (`sum_blocks`, which take longest) add up column sums.  Bound by latency: 8 to 9 us for the shares of a 1024 x 256 gradient (19 MB).
+// (`sum_blocks`, which take longest) add up column sums.  Bound by latency: 8 to 9 us for nine shares of a 1024 x 256 gradient (9.4 MB).
 template <typename TIN, typename TOUT>
 __global__ void __launch_bounds__(256) join_kernel(const float *__restrict__ partial, long long ld_partial, int splits, int groups, int M, int N,
                                                    const TIN *__restrict__ bias, const TOUT *residual, long long ld_res, TOUT *out, long long ld_out,
@@ -1018,7 +1020,9 @@ __device__ __forceinline__ void load(Loaded<T, VEC> &to, const T *from, bool onc
 }
 
 // A lane has VEC neighbouring columns, a warp a stretch of a row, the block `per` rows.  dz, in bf16 numbers or three pieces
-// `layer` apart, may be NULL (column sums only), sums too; ACT: there is a z.  One pass over g and z, bound by traffic (column sums of
+// `layer` apart, may be NULL (column sums only), sums too; ACT: there is a z.  Of bf16 operands dz is rounded once, to bf16, also where
+// grad_out is float32: half a step for each of its numbers, as large as the roundings of the operands and gradients (which are 2.4e-3 off by
+// both, 1.7e-3 by their own alone).  Two pieces of it would double both products and what is written here.  One pass over g and z, bound by traffic (column sums of
 // 40000 x 1024 bf16 numbers and the kernel that joins them: 19 us, 4.4 TB/s).  The loads of a batch of rows are under way together, and
 // all blocks are on the SMs at once: all gradients of 40000 x 256 -> 1024 with GELU take 106 us so, 112 with two blocks of longer
 // batches, 111 by a loop over single rows.
@@ -1430,7 +1434,7 @@ flashbev_status run_product(const Plan &q, const Operand &a, const Operand &b, b
     const int pieces = f32 ? 3 : 1;
     if (!make_map(g.ta, a, pieces, M, K, kBM) || !make_map(g.tb, b, pieces, N, K, q.bn)) return FLASHBEV_CUDA_ERROR;
     g.a_mn = a.mn, g.b_mn = b.mn;
-    g.M = M, g.N = N, g.K = K, g.bn = q.bn, g.stages = q.stages;
+    g.M = M, g.N = N, g.bn = q.bn, g.stages = q.stages;
     g.run = q.run, g.columns = q.columns, g.accs = q.accs, g.groups = q.groups, g.kept = q.kept;
     g.tiles_n = q.tiles_n, g.tiles = q.tiles_m * q.tiles_n, g.kblocks = q.kblocks, g.kshare = q.kshare, g.splits = q.splits;
     g.out = e.out, g.pre = e.pre, g.residual = e.residual, g.bias = e.bias, g.act = e.act;
