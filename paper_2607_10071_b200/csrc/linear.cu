@@ -1252,6 +1252,10 @@ bool make_map(CUtensorMap &map, const Operand &o, int pieces, int across, int K,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// A TMA store clips a row's end to 16 bytes, not to its last element, and writes zeros behind that: rows that have something else there
+// are not for it.
+bool whole(int width, bool f32) { return width % (f32 ? 4 : 8) == 0; }
+
 // Results: `layers` matrices of M rows, stored in tiles of 32 x 32 (wide: 64 columns of bf16)
 bool make_store_map(CUtensorMap &map, void *p, bool f32, bool wide, int M, int N, long long ld, int layers)
 {
@@ -1450,9 +1454,9 @@ flashbev_status run_product(const Plan &q, const Operand &a, const Operand &b, b
 #endif
     if (q.splits > 1) {
         g.partial = partial, g.ld_partial = q.ld_partial;
-        // (partial sums have no other results)
+        // (partial sums have no other results; what lies behind their rows' ends is nobody's)
         if (!make_store_map(g.tout, partial, true, false, M, N, q.ld_partial, q.splits)) return FLASHBEV_CUDA_ERROR;
-    } else if (g.out_vec == 16 && (!e.pre || g.pre_vec == 16)) {
+    } else if (g.out_vec == 16 && whole(N, e.out_f32) && (!e.pre || (g.pre_vec == 16 && whole(N, f32)))) {
         g.store_tma = 1;
         g.wide = !e.out_f32 && !e.pre && (q.bn % 64 == 0 || q.tiles_n == 1);
         if (!make_store_map(g.tout, e.out, e.out_f32, g.wide, M, N, e.ld_out, 1)) return FLASHBEV_CUDA_ERROR;
