@@ -27,3 +27,33 @@ def test_few_rows_and_shared_sums_are_rounded_once(rows, K, N, launches, act):
     step = 2.0 ** (torch.floor(torch.log2(want.abs().clamp_min(1e-30))) - 7)
     over = (out.double() - want).abs() - 0.5 * step - (z * z + 8) * 2.0 ** -23 * want.abs()
     assert over.max().item() <= 0, (int((over > 0).sum()), over.numel())
+
+
+EXTREMES = [0.0, -0.0, 1e-30, -1e-30, 0.7, -0.7, -0.75, 5.9, -5.9, 6.1, -6.1, 13.9, -13.9, 14.1, -14.1, 60.0, -60.0, 90.0, -90.0, 1e19, -1e19, 2e19, -2e19, 3e38, -3e38]
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+@pytest.mark.parametrize("act", [fb.ACT_RELU, fb.ACT_GELU, fb.ACT_SILU])
+def test_slopes_at_extreme_values(act, dtype):
+    """z^2 beyond what float32 holds, exponentials of 0 and infinity.  The slopes' formulas are 3.1e-5 off for bf16 numbers, eight roundings of
+    terms up to 1.3 for float32 ones; the bf16 gradient is rounded twice, the three pieces of a float32 one hold it."""
+    z = torch.tensor(EXTREMES, device="cuda").to(dtype).reshape(-1, 1)
+    one = torch.ones(1, 1, dtype=dtype, device="cuda")
+    gx, _, gb = fb.linear_backward(torch.ones_like(z), z, one, act=act, preact=z)
+    want = ref.activation_slope(z.double(), act)
+    off = 3.1e-5 if dtype is BF16 else 1.3 * 8 * 2.0 ** -24
+    half = ref.HALF_STEP[dtype]
+    assert ((gx.double() - want).abs() - off - 2 * half * want.abs()).max().item() <= 0
+    assert abs(gb.item() - want.sum().item()) <= len(EXTREMES) * off + (half + 2.0 ** -20) * want.abs().sum().item()
+
+
+@pytest.mark.parametrize("rows", [1, 8, 300])
+def test_infinite_sums(rows):
+    """GELU and ReLU of minus infinity are 0, their limit, whichever kernel forms them."""
+    x = torch.full((rows, 1), float("-inf"), dtype=BF16, device="cuda")
+    w = torch.ones(3, 1, dtype=BF16, device="cuda")
+    for act in (fb.ACT_RELU, fb.ACT_GELU):
+        for out_dtype in (fb.BF16, fb.F32):
+            assert bool((fb.linear(x, w, act=act, out_dtype=out_dtype) == 0).all()), (act, out_dtype)
+            assert bool((fb.linear(-x, w, act=act, out_dtype=out_dtype) == float("inf")).all())
+    assert bool((fb.linear(x, w) == float("-inf")).all())
